@@ -318,6 +318,163 @@ s2moe_status s2moe_expand(const s2moe_expand_shape *shape, const int32_t *parent
 s2moe_status s2moe_expand_max_nodes(int32_t n_layers, int32_t n_experts, int32_t k,
                                     int32_t *max_nodes);
 
+/* ---------------------------------------------------------------------------
+   The attention side of a verify step: a paged cache of keys and values, the
+   attention of drafted trees over it, the attention of whole prompts that
+   fill it, and the page operations of branched decoding.
+
+   A cache serves all layers of a model: one page table for the sequences, one
+   pool of pages per layer.  A page holds page_size tokens of every kv head,
+     k  [n_layers][n_pages][n_kv_heads][page_size][head_dim]
+     v  [n_layers][n_pages][n_kv_heads][page_size / 8][head_dim][8]
+   in `dtype`: eight neighbouring tokens of one coordinate of v lie together,
+   which is the order in which the matrix cores take the operand of the second
+   product, so that neither product needs a transposition.  Token t of
+   sequence s is slot t % page_size of page table[s][t / page_size].
+
+   Sequences may share pages (s2moe_kv_fork); refs[p] counts the sequences that
+   hold page p, and a page is free when it is 0.  Everything below the
+   pointers lives in device memory and belongs to the caller: the calls keep no
+   state of their own, wait for nothing, and can be captured in a graph.  A
+   page operation's outcome is a function of the state and of its arguments
+   alone, whatever the timing: free pages are taken lowest id first, in the
+   order of the requests.
+
+   A drafted tree's keys and values occupy the slots after the sequence's
+   length, one per node in node order: s2moe_kv_reserve makes room for them,
+   s2moe_kv_append writes them, s2moe_tree_attention reads them and
+   s2moe_kv_commit keeps the accepted path.
+
+   Sequence ids, page ids, lengths and offsets are read on the device, where
+   each is checked or clamped before it is used as an index: inconsistent
+   values give wrong results, but no access outside the arrays.  Integer
+   arrays need 4-byte alignment only. */
+typedef struct s2moe_kv_cache {
+  int32_t n_layers;   /* >= 1                                              */
+  int32_t n_kv_heads; /* Hkv: 1 .. 256                                     */
+  int32_t head_dim;   /* D: 64 or 128                                      */
+  int32_t n_pages;    /* pages of each layer's pool, 1 .. 2^24             */
+  int32_t page_size;  /* P: 16, 32, 64, 128 or 256 tokens                  */
+  int32_t max_seqs;   /* rows of the table, 1 .. 2^20                      */
+  int32_t max_pages;  /* pages a sequence can hold, P * max_pages < 2^31   */
+  int32_t dtype;      /* F32 or BF16                                       */
+  void *k, *v;        /* pools, 16-byte aligned                            */
+  int32_t *table;     /* [max_seqs][max_pages] page ids, -1 = none         */
+  int32_t *length;    /* [max_seqs] tokens kept (drafted ones not counted) */
+  int32_t *refs;      /* [n_pages] sequences that hold the page            */
+} s2moe_kv_cache;
+
+/* Bits of the status word of each request of a page operation (0: done; a
+   refused request changes nothing). */
+enum {
+  S2MOE_KV_NO_PAGES = 1, /* not enough free pages left                      */
+  S2MOE_KV_TOO_LONG = 2, /* more tokens than the table row can hold, or < 0 */
+  S2MOE_KV_BAD_SEQ = 4,  /* id out of range, or named before in this call   */
+  S2MOE_KV_BUSY = 8,     /* fork: the target already holds pages            */
+  S2MOE_KV_BAD_PATH = 16 /* commit: path not ascending, or a slot of it in
+                            no page that the sequence holds alone          */
+};
+#define S2MOE_KV_MAX_REQUESTS 1024 /* n: requests per page operation        */
+
+/* Empty cache: every sequence of length 0 without pages, every page free.
+   The pools are left as they are. */
+s2moe_status s2moe_kv_init(const s2moe_kv_cache *cache, void *stream);
+
+/* dst[i] becomes a copy of src[i]: the pages that hold src's length tokens are
+   shared, nothing is copied.  dst must hold no pages, and no src may be a dst
+   of the same call.  src, dst, status: [n] int32. */
+s2moe_status s2moe_kv_fork(const s2moe_kv_cache *cache, int32_t n, const int32_t *src,
+                           const int32_t *dst, int32_t *status, void *stream);
+
+/* Room for extra[i] tokens after the length of sequence seqs[i].  Where the
+   first of them falls into a page that other sequences hold too, that page is
+   copied first (its used slots, rounded up to a multiple of 8, in every
+   layer), so that later writes reach no other sequence; of the sequences
+   that share a page, the last to ask keeps it.  Pages already reserved are
+   counted.  Requests are granted in order until the free pages run out: the
+   first that does not fit and every later one that needs a page get
+   S2MOE_KV_NO_PAGES.  Lengths do not change.
+   seqs, extra, status: [n] int32; copied [n][2] int32 receives the page copied
+   from and to, or -1 (the list of the copying launch). */
+s2moe_status s2moe_kv_reserve(const s2moe_kv_cache *cache, int32_t n, const int32_t *seqs,
+                              const int32_t *extra, int32_t *copied, int32_t *status,
+                              void *stream);
+
+/* Writes keys and values of new tokens of one layer into the slots after the
+   lengths.  Tokens are packed: those of sequence seqs[i] are rows tok_off[i]
+   .. tok_off[i + 1] - 1 of k and v, [n_tokens][n_kv_heads][head_dim] in the
+   cache's dtype with ldk and ldv elements from one token to the next (a slice
+   of a fused projection's output will do).  k and v 16-byte aligned, and so
+   ldk and ldv in bytes; ldk, ldv >= n_kv_heads * head_dim.  Tokens whose slot
+   lies in no page that the sequence holds alone are dropped: reserve first. */
+s2moe_status s2moe_kv_append(const s2moe_kv_cache *cache, int32_t layer, int32_t n,
+                             int32_t n_tokens, const int32_t *seqs, const int32_t *tok_off,
+                             const void *k, int64_t ldk, const void *v, int64_t ldv,
+                             void *stream);
+
+/* Keeps the accepted path of each drafted tree: slot length + path[i][j] moves
+   to slot length + j for j < n_accept[i] in every layer (path ascending), the
+   length grows by n_accept[i], and pages past it are given back.  With path
+   0, 1, 2, ... nothing moves (a prompt after its append).  path [n][max_path]
+   int32, 0 <= max_path <= S2MOE_MAX_TOKENS; path may be NULL, which stands for
+   0, 1, 2, ... of any length; seqs, n_accept, status: [n] int32. */
+s2moe_status s2moe_kv_commit(const s2moe_kv_cache *cache, int32_t n, int32_t max_path,
+                             const int32_t *seqs, const int32_t *path, const int32_t *n_accept,
+                             int32_t *status, void *stream);
+
+/* Empties the sequences: every page is given back, and is free once no other
+   sequence holds it.  A sequence named twice is emptied once.  seqs, status:
+   [n] int32. */
+s2moe_status s2moe_kv_free(const s2moe_kv_cache *cache, int32_t n, const int32_t *seqs,
+                           int32_t *status, void *stream);
+
+/* Query heads of an attention call.  Query head h uses kv head h / (n_heads /
+   n_kv_heads).  Strides are in elements from one token to the next, at least
+   heads * head_dim, their bytes a multiple of 16; heads lie together. */
+typedef struct s2moe_attn {
+  int32_t n_heads;    /* Hq: a multiple of n_kv_heads, <= 1024                */
+  int32_t n_kv_heads; /* Hkv (tree attention: the cache's)                    */
+  int32_t head_dim;   /* D: 64 or 128 (tree attention: the cache's)           */
+  int32_t dtype;      /* F32 or BF16, of q, k, v and out alike                */
+  float scale;        /* of the scores, finite and > 0; 1 / sqrt(D) as a rule */
+  int64_t ldq, ldk, ldv, ldo; /* strides of q, k, v, out (ldk, ldv: prompts only) */
+} s2moe_attn;
+
+/* Attention of drafted tokens over the cache (a verify batch's, or with one
+   node per sequence a decoding step's).  Node i of sequence seqs[t]'s tree is
+   row tok_off[t] + i of q, parent and out; parent[i] is the index within the
+   tree of an earlier node, or -1 below the last kept token.  With C the
+   sequence's length tokens and A(i) the node and its ancestors,
+     out_{i,h} = sum_{j in C u A(i)} softmax_j(scale q_{i,h} . k_{j,g}) v_{j,g}
+   with g the kv head of h.  A node whose parent is neither -1 nor an earlier
+   node, and every node below it, gets zeros.  What masked slots hold does not
+   matter, infinities and NaN included.  Sums and softmax statistics are fp32;
+   the softmax numerators of BF16 caches enter the second product as bf16.
+   q [n_tokens][n_heads][D], parent [n_tokens] int32, seqs [n], tok_off
+   [n + 1], out [n_tokens][n_heads][D]; max_nodes is the largest tree of the
+   call, at most S2MOE_MAX_TOKENS (further nodes of a tree are left out), and n
+   at most S2MOE_KV_MAX_REQUESTS.  workspace must hold
+   s2moe_tree_attention_workspace_bytes (0 on bad arguments) for n, max_nodes
+   or more; its contents do not matter.  out must not overlap q. */
+size_t s2moe_tree_attention_workspace_bytes(const s2moe_kv_cache *cache, const s2moe_attn *attn,
+                                            int32_t n, int32_t max_nodes);
+s2moe_status s2moe_tree_attention(const s2moe_kv_cache *cache, int32_t layer,
+                                  const s2moe_attn *attn, int32_t n, int32_t n_tokens,
+                                  int32_t max_nodes, const void *q, const int32_t *seqs,
+                                  const int32_t *tok_off, const int32_t *parent,
+                                  void *workspace, size_t workspace_bytes, void *out,
+                                  void *stream);
+
+/* Causal attention within each of n whole prompts, packed one after another:
+   rows tok_off[t] .. tok_off[t + 1] - 1 of q, k, v and out are prompt t, and
+   row i sees the rows of its prompt up to itself.  k, v [n_tokens][n_kv_heads]
+   [D].  tok_off [n + 1] int32, ascending from 0 to n_tokens; rows outside
+   it are not written.  n <= S2MOE_KV_MAX_REQUESTS.  out must not overlap q, k
+   or v. */
+s2moe_status s2moe_prompt_attention(const s2moe_attn *attn, int32_t n, int32_t n_tokens,
+                                    const void *q, const void *k, const void *v,
+                                    const int32_t *tok_off, void *out, void *stream);
+
 /* Diagnostic, not a step of the verify pass: read `bytes` of device memory
    at `src` once, front to back, with the same 16-byte nontemporal loads the
    expert-FFN kernels stream weights with, so that the rate a caller times

@@ -1,5 +1,6 @@
-"""S2-MoE verify-MoE hot path for AMD Instinct MI355X (gfx950), and the
-routing-aware draft-tree expansion that selects its tokens.
+"""S2-MoE verify-MoE hot path for AMD Instinct MI355X (gfx950), the
+routing-aware draft-tree expansion that selects its tokens, and the cache and
+attention of the same verify step.
 
 The work happens in libs2moe.so (hand-written HIP, C ABI in include/s2moe.h);
 this package is its thin Python binding.
@@ -41,4 +42,15 @@ from .pipeline import (  # noqa: F401
     pack_expert_weights,
     to_device,
     weights_to_device,
+)
+from .attention import (  # noqa: F401
+    KV_BAD_PATH,
+    KV_BAD_SEQ,
+    KV_BUSY,
+    KV_MAX_REQUESTS,
+    KV_NO_PAGES,
+    KV_TOO_LONG,
+    KVCache,
+    TreeAttention,
+    prompt_attention,
 )

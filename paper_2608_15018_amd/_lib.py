@@ -65,6 +65,22 @@ class ExpandShape(ctypes.Structure):
                 ("t_ar", ctypes.c_double), ("t_exp", ctypes.c_double)]
 
 
+class KvCacheStruct(ctypes.Structure):
+    _fields_ = [("n_layers", ctypes.c_int32), ("n_kv_heads", ctypes.c_int32),
+                ("head_dim", ctypes.c_int32), ("n_pages", ctypes.c_int32),
+                ("page_size", ctypes.c_int32), ("max_seqs", ctypes.c_int32),
+                ("max_pages", ctypes.c_int32), ("dtype", ctypes.c_int32),
+                ("k", ctypes.c_void_p), ("v", ctypes.c_void_p), ("table", ctypes.c_void_p),
+                ("length", ctypes.c_void_p), ("refs", ctypes.c_void_p)]
+
+
+class Attn(ctypes.Structure):
+    _fields_ = [("n_heads", ctypes.c_int32), ("n_kv_heads", ctypes.c_int32),
+                ("head_dim", ctypes.c_int32), ("dtype", ctypes.c_int32),
+                ("scale", ctypes.c_float), ("ldq", ctypes.c_int64), ("ldk", ctypes.c_int64),
+                ("ldv", ctypes.c_int64), ("ldo", ctypes.c_int64)]
+
+
 _lib = None
 
 
@@ -98,6 +114,20 @@ def load():
     lib.s2moe_expand_max_nodes.argtypes = [ctypes.c_int32, ctypes.c_int32, ctypes.c_int32,
                                            ctypes.POINTER(ctypes.c_int32)]
     lib.s2moe_expand_max_nodes.restype = ctypes.c_int
+    Cp, Ap, I, N = (ctypes.POINTER(KvCacheStruct), ctypes.POINTER(Attn), ctypes.c_int32,
+                    ctypes.c_int64)
+    for name, types in (
+            ("kv_init", [Cp, P]), ("kv_fork", [Cp, I, P, P, P, P]),
+            ("kv_reserve", [Cp, I, P, P, P, P, P]),
+            ("kv_append", [Cp, I, I, I, P, P, P, N, P, N, P]),
+            ("kv_commit", [Cp, I, I, P, P, P, P, P]), ("kv_free", [Cp, I, P, P, P]),
+            ("tree_attention", [Cp, I, Ap, I, I, I, P, P, P, P, P, ctypes.c_size_t, P, P]),
+            ("prompt_attention", [Ap, I, I, P, P, P, P, P, P])):
+        f = getattr(lib, "s2moe_" + name)
+        f.argtypes = types
+        f.restype = ctypes.c_int
+    lib.s2moe_tree_attention_workspace_bytes.argtypes = [Cp, Ap, I, I]
+    lib.s2moe_tree_attention_workspace_bytes.restype = ctypes.c_size_t
     lib.s2moe_stream_read.argtypes = [P, ctypes.c_size_t, P, P]
     lib.s2moe_stream_read.restype = ctypes.c_int
     for f in ("s2moe_route", "s2moe_reuse_gate", "s2moe_verify_moe", "s2moe_verify_moe_noalloc",

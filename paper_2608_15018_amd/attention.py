@@ -1,0 +1,208 @@
+"""The attention side of a verify step: the paged cache of keys and values, the
+attention of drafted trees over it, and that of whole prompts.  Argument
+marshalling only; every step is a call into libs2moe.so.
+
+A verify step of one layer, for sequences `seqs` whose trees' tokens are packed
+one after another (`tok_off` their offsets, `parent` the index of each node's
+parent within its tree, -1 below the last kept token):
+
+    cache.reserve(seqs, n_nodes)                  # once per step, all layers
+    cache.append(layer, k, v, seqs, tok_off)      # the drafted tokens' K and V
+    o = attention(layer, q, seqs, tok_off, parent)
+    ...                                           # the layer's experts, the other layers
+    cache.commit(seqs, path, n_accept)            # once per step: keep the accepted path
+"""
+
+from __future__ import annotations
+
+import ctypes
+
+import torch
+
+from . import _lib
+
+KV_NO_PAGES, KV_TOO_LONG, KV_BAD_SEQ, KV_BUSY, KV_BAD_PATH = 1, 2, 4, 8, 16
+KV_MAX_REQUESTS = 1024
+
+_CODES = {torch.float32: _lib.F32, torch.bfloat16: _lib.BF16}
+
+
+def _code(dtype) -> int:
+    if dtype not in _CODES:
+        raise TypeError(f"expected torch.float32 or torch.bfloat16, got {dtype}")
+    return _CODES[dtype]
+
+
+def _ints(t, name, shape):
+    if t.dtype != torch.int32 or t.shape != shape:
+        raise ValueError(f"{name}: expected int32 {tuple(shape)}, got {t.dtype} {tuple(t.shape)}")
+    return _lib._ptr(t)
+
+
+def _rows(t, name, heads, head_dim, dtype):
+    """(pointer, elements from one token to the next) of [n, heads, head_dim]
+    whose heads lie together."""
+    if t.dtype != dtype or t.dim() != 3 or t.shape[1] != heads or t.shape[2] != head_dim:
+        raise ValueError(f"{name}: expected {dtype} [n, {heads}, {head_dim}], got {t.dtype} "
+                         f"{tuple(t.shape)}")
+    n, s0, s1, s2 = t.shape[0], *t.stride()
+    if s2 != 1 or (s1 != head_dim and heads > 1):
+        raise ValueError(f"{name}: the heads of a token must lie together (strides {t.stride()})")
+    return t.data_ptr(), s0 if n > 1 else heads * head_dim
+
+
+class KVCache:
+    """Pages of keys and values of `n_layers` layers for up to `max_seqs`
+    sequences of up to `max_pages` pages each.  Allocates the arrays that are
+    not given and then empties the cache; given all five (k, v, table, length,
+    refs) it takes them as they are.
+
+    `status` holds one word per request of the last page operation (bits KV_*,
+    0: done) and `copied` the pages that the last reserve copied, both on the
+    device."""
+
+    def __init__(self, n_layers: int, n_kv_heads: int, head_dim: int, n_pages: int,
+                 page_size: int, max_seqs: int, max_pages: int, dtype=torch.bfloat16,
+                 device="cuda", k=None, v=None, table=None, length=None, refs=None):
+        code = _code(dtype)
+        i32 = torch.int32
+        want = {"k": ((n_layers, n_pages, n_kv_heads, page_size, head_dim), dtype),
+                "v": ((n_layers, n_pages, n_kv_heads, page_size // 8, head_dim, 8), dtype),
+                "table": ((max_seqs, max_pages), i32), "length": ((max_seqs,), i32),
+                "refs": ((n_pages,), i32)}
+        given = {"k": k, "v": v, "table": table, "length": length, "refs": refs}
+        fresh = any(t is None for t in given.values())
+        for name, (shape, dt) in want.items():
+            t = given[name]
+            if t is None:
+                t = torch.empty(shape, dtype=dt, device=device)
+            else:
+                _lib._expect(t, name, dt, shape)
+            setattr(self, name, t)
+        self.n_layers, self.n_kv_heads, self.head_dim = n_layers, n_kv_heads, head_dim
+        self.n_pages, self.page_size = n_pages, page_size
+        self.max_seqs, self.max_pages, self.dtype = max_seqs, max_pages, dtype
+        dev = self.k.device
+        self.status = torch.zeros(KV_MAX_REQUESTS, dtype=i32, device=dev)
+        self.copied = torch.full((KV_MAX_REQUESTS, 2), -1, dtype=i32, device=dev)
+        self.struct = _lib.KvCacheStruct(n_layers, n_kv_heads, head_dim, n_pages, page_size,
+                                         max_seqs, max_pages, code,
+                                         *[_lib._ptr(getattr(self, n))
+                                           for n in ("k", "v", "table", "length", "refs")])
+        self._ref = ctypes.byref(self.struct)
+        self._lib = _lib.load()
+        self._status, self._copied = self.status.data_ptr(), self.copied.data_ptr()
+        if fresh:
+            self.clear()
+
+    def clear(self, stream=None):
+        """Every sequence empty, every page free."""
+        _lib._check(self._lib.s2moe_kv_init(self._ref, _lib._stream(stream)))
+
+    def fork(self, src, dst, stream=None):
+        """Sequence dst[i] becomes a copy of src[i] on the same pages."""
+        n = src.shape[0]
+        _lib._check(self._lib.s2moe_kv_fork(self._ref, n, _ints(src, "src", (n,)),
+                                            _ints(dst, "dst", (n,)), self._status,
+                                            _lib._stream(stream)))
+
+    def reserve(self, seqs, extra, stream=None):
+        """Pages for extra[i] more tokens of seqs[i]; a shared page that they
+        would be written to is copied."""
+        n = seqs.shape[0]
+        _lib._check(self._lib.s2moe_kv_reserve(self._ref, n, _ints(seqs, "seqs", (n,)),
+                                               _ints(extra, "extra", (n,)), self._copied,
+                                               self._status, _lib._stream(stream)))
+
+    def append(self, layer: int, k, v, seqs, tok_off, stream=None):
+        """New tokens' keys and values [n_tokens, n_kv_heads, head_dim] into
+        the slots after the lengths."""
+        n, t = seqs.shape[0], k.shape[0]
+        kp, ldk = _rows(k, "k", self.n_kv_heads, self.head_dim, self.dtype)
+        vp, ldv = _rows(v, "v", self.n_kv_heads, self.head_dim, self.dtype)
+        if v.shape[0] != t:
+            raise ValueError(f"v holds {v.shape[0]} tokens, k {t}")
+        _lib._check(self._lib.s2moe_kv_append(self._ref, layer, n, t, _ints(seqs, "seqs", (n,)),
+                                              _ints(tok_off, "tok_off", (n + 1,)), kp, ldk, vp,
+                                              ldv, _lib._stream(stream)))
+
+    def commit(self, seqs, path, n_accept, stream=None):
+        """Keeps nodes path[i, :n_accept[i]] of each drafted tree (ascending);
+        path None: the first n_accept[i] tokens as they lie."""
+        n = seqs.shape[0]
+        most = 0 if path is None else path.shape[1]
+        pp = None if path is None else _ints(path, "path", (n, most))
+        _lib._check(self._lib.s2moe_kv_commit(self._ref, n, most, _ints(seqs, "seqs", (n,)), pp,
+                                              _ints(n_accept, "n_accept", (n,)), self._status,
+                                              _lib._stream(stream)))
+
+    def free(self, seqs, stream=None):
+        """Empties the sequences."""
+        n = seqs.shape[0]
+        _lib._check(self._lib.s2moe_kv_free(self._ref, n, _ints(seqs, "seqs", (n,)),
+                                            self._status, _lib._stream(stream)))
+
+
+class TreeAttention:
+    """Attention of drafted trees over `cache`, with the workspace of calls of
+    up to `max_seqs` sequences and `max_nodes` nodes each."""
+
+    def __init__(self, cache: KVCache, n_heads: int, max_seqs: int, max_nodes: int,
+                 scale: float | None = None):
+        self.cache, self.n_heads = cache, n_heads
+        self.max_seqs, self.max_nodes = max_seqs, max_nodes
+        D = cache.head_dim
+        self.attn = _lib.Attn(n_heads, cache.n_kv_heads, D, cache.struct.dtype,
+                              D ** -0.5 if scale is None else scale, n_heads * D, 0, 0,
+                              n_heads * D)
+        self._ref = ctypes.byref(self.attn)
+        self._lib = _lib.load()
+        self.bytes = self._lib.s2moe_tree_attention_workspace_bytes(cache._ref, self._ref,
+                                                                    max_seqs, max_nodes)
+        if self.bytes == 0:
+            raise _lib.S2moeError(_lib.EINVAL, _lib.last_error())
+        self.workspace = torch.empty(self.bytes, dtype=torch.uint8, device=cache.k.device)
+
+    def __call__(self, layer: int, q, seqs, tok_off, parent, out=None, stream=None):
+        """q [n_tokens, n_heads, head_dim] -> out of the same shape."""
+        c, n, t = self.cache, seqs.shape[0], q.shape[0]
+        if n > self.max_seqs:
+            raise ValueError(f"{n} sequences, the workspace is for {self.max_seqs}")
+        qp, ldq = _rows(q, "q", self.n_heads, c.head_dim, c.dtype)
+        if out is None:
+            out = torch.empty((t, self.n_heads, c.head_dim), dtype=c.dtype, device=q.device)
+        op, ldo = _rows(out, "out", self.n_heads, c.head_dim, c.dtype)
+        if out.shape[0] != t:
+            raise ValueError(f"out holds {out.shape[0]} tokens, q {t}")
+        self.attn.ldq, self.attn.ldo = ldq, ldo
+        _lib._check(self._lib.s2moe_tree_attention(
+            c._ref, layer, self._ref, n, t, self.max_nodes, qp, _ints(seqs, "seqs", (n,)),
+            _ints(tok_off, "tok_off", (n + 1,)), _ints(parent, "parent", (t,)),
+            self.workspace.data_ptr(), self.bytes, op, _lib._stream(stream)))
+        return out
+
+
+def prompt_attention(q, k, v, tok_off, out=None, scale: float | None = None, stream=None):
+    """Causal attention within packed prompts: q [n_tokens, n_heads, head_dim],
+    k and v [n_tokens, n_kv_heads, head_dim], tok_off [n + 1] int32."""
+    if q.dim() != 3 or k.dim() != 3:
+        raise ValueError("q, k, v: expected [n_tokens, heads, head_dim]")
+    t, Hq, D = q.shape
+    Hkv = k.shape[1]
+    qp, ldq = _rows(q, "q", Hq, D, q.dtype)
+    kp, ldk = _rows(k, "k", Hkv, D, q.dtype)
+    vp, ldv = _rows(v, "v", Hkv, D, q.dtype)
+    if out is None:
+        out = torch.empty((t, Hq, D), dtype=q.dtype, device=q.device)
+    op, ldo = _rows(out, "out", Hq, D, q.dtype)
+    if not (k.shape[0] == v.shape[0] == out.shape[0] == t):
+        raise ValueError(f"q, k, v, out hold {t}, {k.shape[0]}, {v.shape[0]}, {out.shape[0]} tokens")
+    if tok_off.dim() != 1 or tok_off.shape[0] < 1:
+        raise ValueError("tok_off: expected int32 [n + 1]")
+    a = _lib.Attn(Hq, Hkv, D, _code(q.dtype), D ** -0.5 if scale is None else scale, ldq, ldk, ldv,
+                  ldo)
+    n = tok_off.shape[0] - 1
+    _lib._check(_lib.load().s2moe_prompt_attention(
+        ctypes.byref(a), n, t, qp, kp, vp, _ints(tok_off, "tok_off", (n + 1,)), op,
+        _lib._stream(stream)))
+    return out

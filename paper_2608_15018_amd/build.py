@@ -18,7 +18,8 @@ CSRC = os.path.join(PKG, "csrc")
 INCLUDE = os.path.join(ROOT, "include")
 OBJDIR = os.path.join(PKG, "_build")
 LIB = os.path.join(PKG, "libs2moe.so")
-SOURCES = ["api.cpp", "route.hip", "gate.hip", "ffn.hip", "ffn_bf16.hip", "ffn_bf16_wide.hip", "ffn_q4.hip", "combine.hip", "pack.hip", "probe.hip", "expand.hip", "noalloc.hip"]
+SOURCES = ["api.cpp", "route.hip", "gate.hip", "ffn.hip", "ffn_bf16.hip", "ffn_bf16_wide.hip", "ffn_q4.hip", "combine.hip", "pack.hip", "probe.hip", "expand.hip", "noalloc.hip",
+           "api_cache.cpp", "kv_cache.hip", "tree_attention.hip", "prompt_attention.hip"]
 ARCH = "gfx950"
 ROCM_INC = os.path.join(os.environ.get("ROCM_PATH", "/opt/rocm"), "include")
 
@@ -79,14 +80,16 @@ def build_host_sanitized(verbose: bool = True) -> str:
     if not all(os.path.exists(o) for o in objs):
         build(verbose)
     rocm = os.environ.get("ROCM_PATH", "/opt/rocm")
-    api_obj = os.path.join(OBJDIR, "api_hostsan.o")
-    cc = ["g++", "-std=c++17", "-O1", "-g", "-fPIC", *SAN_FLAGS, "-D__HIP_PLATFORM_AMD__=1",
-          "-I", ROCM_INC, "-I", INCLUDE, "-I", CSRC, "-c", os.path.join(CSRC, "api.cpp"),
-          "-o", api_obj]
-    link = ["g++", "-shared", *SAN_FLAGS, api_obj, *[o for o in objs if not o.endswith("api.o")],
+    host = {s: os.path.join(OBJDIR, os.path.splitext(s)[0] + "_hostsan.o")
+            for s in SOURCES if s.endswith(".cpp")}
+    cc = [["g++", "-std=c++17", "-O1", "-g", "-fPIC", *SAN_FLAGS, "-D__HIP_PLATFORM_AMD__=1",
+           "-I", ROCM_INC, "-I", INCLUDE, "-I", CSRC, "-c", os.path.join(CSRC, src), "-o", obj]
+          for src, obj in host.items()]
+    link = ["g++", "-shared", *SAN_FLAGS, *host.values(),
+            *[o for s, o in zip(SOURCES, objs) if s not in host],
             "-L", os.path.join(rocm, "lib"), "-lamdhip64", "-Wl,-rpath," + os.path.join(rocm, "lib"),
             "-o", SAN_LIB]
-    for cmd in (cc, link):
+    for cmd in (*cc, link):
         r = subprocess.run(cmd, capture_output=True, text=True)
         if r.returncode != 0:
             raise RuntimeError(f"sanitized build failed:\n{' '.join(cmd)}\n{r.stdout}{r.stderr}")

@@ -3,42 +3,21 @@
 #include <hip/hip_runtime.h>
 
 #include <cmath>
-#include <cstdarg>
 #include <cstdint>
-#include <cstdio>
-#include <string>
 
 #include "kernels.h"
 #include "s2moe.h"
+#include "status.h"
 
 static_assert(s2moe::kMaxShared == S2MOE_MAX_SHARED, "shared-expert limit");
 
 namespace {
 
-thread_local std::string g_last_error;
-
-s2moe_status fail(s2moe_status st, const char* fmt, ...) {
-  char buf[512];
-  va_list ap;
-  va_start(ap, fmt);
-  vsnprintf(buf, sizeof(buf), fmt, ap);
-  va_end(ap);
-  g_last_error = buf;
-  return st;
-}
-
-s2moe_status ok() {
-  g_last_error.clear();
-  return S2MOE_OK;
-}
-
-bool aligned16(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 15u) == 0; }
-
-#define S2MOE_REQUIRE_PTR(p)                                                     \
-  do {                                                                           \
-    if ((p) == nullptr) return fail(S2MOE_EINVAL, "%s: %s is NULL", fn, #p);     \
-    if (!aligned16(p)) return fail(S2MOE_EINVAL, "%s: %s is not 16-byte aligned", fn, #p); \
-  } while (0)
+using s2moe::aligned;
+using s2moe::aligned16;
+using s2moe::fail;
+using s2moe::hip_status;
+using s2moe::ok;
 
 s2moe_status check_layer(const char* fn, const s2moe_layer* L, int32_t B) {
   if (L == nullptr) return fail(S2MOE_EINVAL, "%s: layer is NULL", fn);
@@ -136,11 +115,6 @@ size_t workspace_bytes(const s2moe_layer* L, int32_t B) {
   size_t n = hh_bytes(L, B);
   if (L->w_dtype == S2MOE_Q4G32) n += x16_bytes(L, B) + part_bytes(L, B);
   return n;
-}
-
-s2moe_status hip_status(const char* fn, hipError_t err) {
-  if (err != hipSuccess) return fail(S2MOE_EHIP, "%s: %s", fn, hipGetErrorString(err));
-  return ok();
 }
 
 // Checks of each step's arguments, then its launch struct.  The single
@@ -260,7 +234,7 @@ extern "C" {
 
 int32_t s2moe_abi_version(void) { return S2MOE_ABI_VERSION; }
 
-const char* s2moe_last_error(void) { return g_last_error.c_str(); }
+const char* s2moe_last_error(void) { return s2moe::g_last_error.c_str(); }
 
 const char* s2moe_status_string(s2moe_status st) {
   switch (st) {
@@ -427,8 +401,6 @@ s2moe_status s2moe_verify_moe_noalloc(const s2moe_layer* layer, int32_t n_tokens
 }
 
 namespace {
-
-bool aligned(const void* p, size_t a) { return (reinterpret_cast<uintptr_t>(p) & (a - 1)) == 0; }
 
 // LDS available to one workgroup on the current device.
 s2moe_status device_lds(const char* fn, size_t* bytes) {
