@@ -341,6 +341,9 @@ s2moe_status s2moe_prompt_attention(const s2moe_attn* attn, int32_t n, int32_t n
   if (st == S2MOE_OK) st = check_requests(fn, n);
   if (st != S2MOE_OK) return st;
   if (n_tokens < 0) return fail(S2MOE_EINVAL, "%s: n_tokens = %d < 0", fn, n_tokens);
+  if ((int64_t)n_tokens * attn->n_heads >= (int64_t)1 << 31)
+    return fail(S2MOE_EUNSUPPORTED, "%s: n_tokens = %d of %d heads: 2^31 rows or more", fn,
+                n_tokens, attn->n_heads);
   if (n == 0 || n_tokens == 0) return ok();
   S2MOE_REQUIRE_PTR(q);
   S2MOE_REQUIRE_PTR(k);

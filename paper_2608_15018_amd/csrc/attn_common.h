@@ -1,0 +1,87 @@
+// Device helpers shared by the attention kernels (gfx950, wave64).
+#pragma once
+
+#include "common.h"
+
+namespace s2moe {
+
+typedef __attribute__((__vector_size__(2 * sizeof(__bf16)))) __bf16 bf16x2;
+typedef __attribute__((__vector_size__(4 * sizeof(__bf16)))) __bf16 bf16x4;
+typedef __attribute__((__vector_size__(2 * sizeof(float)))) float f32x2;
+typedef __attribute__((__vector_size__(16 * sizeof(float)))) float f32x16;
+typedef __attribute__((address_space(3))) void lds_void;
+typedef const __attribute__((address_space(1))) void global_void;
+
+// A running maximum may lag behind by this much (base-2 logarithm) before the
+// accumulators are rescaled: weights stay below 2^8, far inside fp32 and of
+// the same relative precision in bf16.
+constexpr float kLag = 8.f;
+
+__device__ __forceinline__ float exp2_fast(float x) { return __builtin_amdgcn_exp2f(x); }
+
+__device__ __forceinline__ float max3(float a, float b, float c) {
+  return fmaxf(fmaxf(a, b), c);
+}
+
+// The other half-wave's value combined with this one's: lanes l and l ^ 32.
+__device__ __forceinline__ float max_halves(float x) {
+  const auto r = __builtin_amdgcn_permlane32_swap(__float_as_uint(x), __float_as_uint(x), false, false);
+  return fmaxf(__uint_as_float(r[0]), __uint_as_float(r[1]));
+}
+__device__ __forceinline__ float sum_halves(float x) {
+  const auto r = __builtin_amdgcn_permlane32_swap(__float_as_uint(x), __float_as_uint(x), false, false);
+  return __uint_as_float(r[0]) + __uint_as_float(r[1]);
+}
+// Over the four 16-lane groups.
+__device__ __forceinline__ float max_groups(float x) {
+  const auto r = __builtin_amdgcn_permlane16_swap(__float_as_uint(x), __float_as_uint(x), false, false);
+  return max_halves(fmaxf(__uint_as_float(r[0]), __uint_as_float(r[1])));
+}
+__device__ __forceinline__ float sum_groups(float x) {
+  const auto r = __builtin_amdgcn_permlane16_swap(__float_as_uint(x), __float_as_uint(x), false, false);
+  return sum_halves(__uint_as_float(r[0]) + __uint_as_float(r[1]));
+}
+
+__device__ __forceinline__ bf16x8 pack8(const float* x) {
+  bf16x8 out;
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    const f32x2 v = {x[2 * i], x[2 * i + 1]};
+    const bf16x2 b = __builtin_convertvector(v, bf16x2);
+    out[2 * i] = b[0];
+    out[2 * i + 1] = b[1];
+  }
+  return out;
+}
+
+// Whether any of eight bf16 values is an infinity or NaN, and the values with
+// those replaced by zero.
+__device__ __forceinline__ bool any_nonfinite(bf16x8 x) {
+  const u32x4 u = __builtin_bit_cast(u32x4, x);
+  bool bad = false;
+#pragma unroll
+  for (int i = 0; i < 4; ++i)
+    bad |= (u[i] & 0x7F80u) == 0x7F80u || (u[i] & 0x7F800000u) == 0x7F800000u;
+  return bad;
+}
+__device__ __forceinline__ bf16x8 finite_only(bf16x8 x) {
+  u32x4 u = __builtin_bit_cast(u32x4, x);
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    if ((u[i] & 0x7F80u) == 0x7F80u) u[i] &= 0xFFFF0000u;
+    if ((u[i] & 0x7F800000u) == 0x7F800000u) u[i] &= 0xFFFFu;
+  }
+  return __builtin_bit_cast(bf16x8, u);
+}
+
+// 1 where a value is an infinity or NaN, else 0.
+__device__ __forceinline__ bf16x8 nonfinite_ones(bf16x8 x) {
+  u32x4 u = __builtin_bit_cast(u32x4, x);
+#pragma unroll
+  for (int i = 0; i < 4; ++i)
+    u[i] = ((u[i] & 0x7F80u) == 0x7F80u ? 0x3F80u : 0u) |
+           ((u[i] & 0x7F800000u) == 0x7F800000u ? 0x3F800000u : 0u);
+  return __builtin_bit_cast(bf16x8, u);
+}
+
+}  // namespace s2moe

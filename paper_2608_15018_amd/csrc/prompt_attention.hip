@@ -1,6 +1,6 @@
 // Causal attention of packed prompts: one wave per (token, query head).
 #include "attention.h"
-#include "common.h"
+#include "attn_common.h"
 
 namespace s2moe {
 namespace {
@@ -59,6 +59,330 @@ __global__ __launch_bounds__(64) void prompt_kernel(PromptArgs a) {
   for (int i = 0; i < D / 64; ++i) store(o + lane + 64 * i, acc[i] / l);
 }
 
+// Workgroup b of a kv head: which rows of which prompt.  Prompts take
+// ceil(len G / rows) workgroups each, last ones first (they see the most
+// keys); 256 threads share the offsets.
+__device__ bool find_block(const PromptArgs& a, int b, int rows, int* first, int* len, int* qb) {
+  __shared__ int wave_s[4], found_s[3];
+  const int tid = threadIdx.x, lane = tid & 63, w = tid >> 6;
+  int n[4], f[4], mine = 0;
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    const int s = 4 * tid + i;
+    int x = 0, y = 0;
+    if (s < a.n) {
+      x = a.tok_off[s];
+      y = a.tok_off[s + 1];
+    }
+    const bool good = x >= 0 && x < y && y <= a.n_tokens;
+    f[i] = x;
+    n[i] = good ? y - x : 0;
+    mine += (n[i] * a.G + rows - 1) / rows;
+  }
+  int inc = mine;
+#pragma unroll
+  for (int d = 1; d < 64; d <<= 1) {
+    const int y = __shfl_up(inc, d);
+    if (lane >= d) inc += y;
+  }
+  if (lane == 63) wave_s[w] = inc;
+  __syncthreads();
+  int at = inc - mine, total = 0;
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    at += i < w ? wave_s[i] : 0;
+    total += wave_s[i];
+  }
+  if (b >= total) return false;
+  b = total - 1 - b;
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    const int blocks = (n[i] * a.G + rows - 1) / rows;
+    if (b >= at && b < at + blocks) {
+      found_s[0] = f[i];
+      found_s[1] = n[i];
+      found_s[2] = b - at;
+    }
+    at += blocks;
+  }
+  __syncthreads();
+  *first = __builtin_amdgcn_readfirstlane(found_s[0]);
+  *len = __builtin_amdgcn_readfirstlane(found_s[1]);
+  *qb = __builtin_amdgcn_readfirstlane(found_s[2]);
+  return true;
+}
+
+// ---------------------------------------------------------------- bf16
+template <int D>
+struct PromptTile {
+  static constexpr int kRows = 256;          // rows of a workgroup, 64 a wave
+  static constexpr int kStage = 64 * D * 2;  // bytes of 64 keys, or of their values
+  static constexpr int kLoads = D / 32;      // 1 KB loads a wave makes for it
+  static constexpr int kLds = 6 * kStage;    // three stages of each
+};
+
+template <int D>
+__global__ __launch_bounds__(256, D == 64 ? 2 : 1) void prompt_bf16_kernel(PromptArgs a) {
+  constexpr int kStage = PromptTile<D>::kStage, kLoads = PromptTile<D>::kLoads;
+  constexpr int KS = D / 16, MT = D / 32, CH = D / 8;  // k steps, tiles of D, 16-byte chunks of a row
+  extern __shared__ __attribute__((aligned(16))) char smem[];
+  char* const k_lds = smem;               // three stages of keys
+  char* const v_lds = smem + 3 * kStage;  // three of values
+
+  const int tid = threadIdx.x, lane = tid & 63, w = wave_id();
+  const int hk = blockIdx.x % a.Hkv;
+  int first, len, qb;
+  if (!find_block(a, blockIdx.x / a.Hkv, PromptTile<D>::kRows, &first, &len, &qb))
+    return;
+  const int R = len * a.G, row0 = qb * PromptTile<D>::kRows + w * 64;
+  const int l32 = lane & 31, h = lane >> 5;
+  const int last_row = min(qb * PromptTile<D>::kRows + PromptTile<D>::kRows, R) - 1;
+  const int n_stage = (last_row / a.G) / 64 + 1, n_sub = 2 * n_stage;
+
+  // This wave's rows: 32 steps of keys [0, n_full) that all of them see, and
+  // up to n_all that some do.
+  int n_full = 0, n_all = 0;
+  if (row0 < R) {
+    n_full = (row0 / a.G + 1) / 32;
+    n_all = (min(row0 + 63, R - 1) / a.G) / 32 + 1;
+  }
+  int tok[2];
+  const uint16_t* q = reinterpret_cast<const uint16_t*>(a.q);
+  bf16x8 qf[KS][2];
+#pragma unroll
+  for (int nt = 0; nt < 2; ++nt) {
+    const int r = min(row0 + 32 * nt + l32, R - 1);
+    tok[nt] = r / a.G;
+    const uint16_t* p = q + (int64_t)(first + tok[nt]) * a.ldq + (hk * a.G + r % a.G) * D + 8 * h;
+#pragma unroll
+    for (int ks = 0; ks < KS; ++ks) qf[ks][nt] = *reinterpret_cast<const bf16x8*>(p + 16 * ks);
+  }
+
+  // Staging: chunk c of row r of a stage lies at chunk c ^ swizzle(r), so that
+  // the reads below spread over all banks.
+  const char* const kg = a.k + ((int64_t)first * a.ldk + hk * D) * 2;
+  const char* const vg = a.v + ((int64_t)first * a.ldv + hk * D) * 2;
+  const int64_t ldk = a.ldk * 2, ldv = a.ldv * 2;
+  const auto load_stage = [&](const char* g, int64_t ld, char* lds, int s, bool keys) {
+#pragma unroll
+    for (int i = 0; i < kLoads; ++i) {
+      const int r = (w * kLoads + i) * (64 / CH) + lane / CH;
+      const int x = keys ? (D == 128 ? r & 15 : (r >> 1) & 7) : (D == 128 ? (r & 3) << 2 : ((r >> 1) & 1) << 2);
+      const int key = min(64 * s + r, len - 1);
+      __builtin_amdgcn_global_load_lds((global_void*)(g + key * ld + (((lane % CH) ^ x) << 4)),
+                                       (lds_void*)(lds + (w * kLoads + i) * 1024), 16, 0, 0);
+    }
+  };
+  const auto load_k = [&](int s) { load_stage(kg, ldk, k_lds + (s % 3) * kStage, s, true); };
+  const auto load_v = [&](int s) { load_stage(vg, ldv, v_lds + (s % 3) * kStage, s, false); };
+  // Stage s of the keys and s - 1 of the values are there for everybody, and
+  // what the stage after next overwrites is read by nobody any more.
+  const auto sync = [&](int s) {
+    if (kLoads == 4) __builtin_amdgcn_s_waitcnt(0x0F70 | 8); else __builtin_amdgcn_s_waitcnt(0x0F70 | 4);
+    __builtin_amdgcn_s_barrier();
+    load_k(s + 2);
+    load_v(s + 1);
+  };
+
+  // Row m of a key tile is key m with bits 2 and 3 exchanged: then a lane's
+  // scores 8 s .. 8 s + 7 belong to keys 16 s + 8 h + 0 .. 7, the order in
+  // which the second product takes them.
+  const int key_row = (l32 & 0x13) | ((l32 & 4) << 1) | ((l32 & 8) >> 1);
+  const int k_at = key_row * D * 2, k_x = ((D == 128 ? key_row & 15 : (key_row >> 1) & 7) ^ h) << 4;
+  const int v_r = (lane & 15) >> 2;
+  const int v_at = (8 * h + v_r) * D * 2 + ((lane >> 4) & 1) * 32 + (lane & 3) * 8;
+
+  f32x16 O[MT][2];
+#pragma unroll
+  for (int mt = 0; mt < MT; ++mt)
+#pragma unroll
+    for (int nt = 0; nt < 2; ++nt) O[mt][nt] = f32x16{};
+  float shift[2] = {0.f, 0.f}, limit[2] = {-INFINITY, -INFINITY}, l[2] = {0.f, 0.f};
+  const float c = a.scale * 1.44269504088896340736f;
+
+  const auto products_k = [&](int j, f32x16(&T)[2]) {
+    const char* kt = k_lds + ((j >> 1) % 3) * kStage + (j & 1) * 32 * D * 2 + k_at;
+#pragma unroll
+    for (int nt = 0; nt < 2; ++nt) T[nt] = f32x16{};
+#pragma unroll
+    for (int ks = 0; ks < KS; ++ks) {
+      const bf16x8 kf = *reinterpret_cast<const bf16x8*>(kt + (k_x ^ (ks << 5)));
+#pragma unroll
+      for (int nt = 0; nt < 2; ++nt) T[nt] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(kf, qf[ks][nt], T[nt], 0, 0, 0);
+    }
+  };
+  const auto value_tile = [&](int j, int ks, int mt) -> bf16x8 {
+    const char* vt = v_lds + ((j >> 1) % 3) * kStage + ((j & 1) * 32 + 16 * ks) * D * 2 + v_at +
+                     ((mt ^ (D == 128 ? v_r : v_r >> 1)) << 6);
+    const bf16x4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4bf16((__attribute__((address_space(3))) bf16x4*)vt);
+    const bf16x4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4bf16((__attribute__((address_space(3))) bf16x4*)(vt + 4 * D * 2));
+    return __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7);
+  };
+  const auto products_v = [&](int j, const bf16x8(&W)[2][2]) {
+#pragma unroll
+    for (int ks = 0; ks < 2; ++ks)
+#pragma unroll
+      for (int mt = 0; mt < MT; ++mt) {
+        const bf16x8 vf = value_tile(j, ks, mt);
+#pragma unroll
+        for (int nt = 0; nt < 2; ++nt) O[mt][nt] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(vf, W[ks][nt], O[mt][nt], 0, 0, 0);
+      }
+  };
+  // The weights of one step, by the maximum as it stands.
+  const auto weights = [&](const f32x16(&T)[2], bf16x8(&W)[2][2]) {
+#pragma unroll
+    for (int nt = 0; nt < 2; ++nt) {
+      float p[16];
+#pragma unroll
+      for (int i = 0; i < 16; ++i) {
+        p[i] = exp2_fast(fmaf(T[nt][i], c, -shift[nt]));
+        l[nt] += p[i];
+      }
+#pragma unroll
+      for (int ks = 0; ks < 2; ++ks) W[ks][nt] = pack8(p + 8 * ks);
+    }
+  };
+  const auto largest = [&](const f32x16& T) {
+    float m = max3(T[0], T[1], T[2]);
+#pragma unroll
+    for (int i = 3; i < 15; i += 2) m = max3(m, T[i], T[i + 1]);
+    return fmaxf(m, T[15]) * c;
+  };
+  // Scores T of the next step: a row with one past its limit moves its maximum
+  // there, and what it has summed so far, W's step included, shrinks by 2^-8 or
+  // more (so rounding W once more does not count).
+  const auto raise = [&](const f32x16(&T)[2], bf16x8(&W)[2][2]) {
+    const float m[2] = {largest(T[0]), largest(T[1])};
+    if (__builtin_expect(__any(m[0] > limit[0] || m[1] > limit[1]), 0)) {
+#pragma unroll
+      for (int nt = 0; nt < 2; ++nt) {
+        const float top = max_halves(m[nt]);
+        const bool moves = top > limit[nt], fresh = limit[nt] == -INFINITY;
+        const float f = moves && !fresh ? exp2_fast(shift[nt] - top) : 1.f;
+        shift[nt] = moves ? top : shift[nt];
+        limit[nt] = moves ? top + kLag : limit[nt];
+        l[nt] *= f;
+#pragma unroll
+        for (int mt = 0; mt < MT; ++mt) O[mt][nt] *= f;
+#pragma unroll
+        for (int ks = 0; ks < 2; ++ks) {
+          float p[8];
+#pragma unroll
+          for (int i = 0; i < 8; ++i) p[i] = (float)W[ks][nt][i] * f;
+          W[ks][nt] = pack8(p);
+        }
+      }
+    }
+  };
+  const auto mask = [&](int j, f32x16(&T)[2]) {
+#pragma unroll
+    for (int nt = 0; nt < 2; ++nt)
+#pragma unroll
+      for (int i = 0; i < 16; ++i)
+        if (32 * j + 16 * (i >> 3) + 8 * h + (i & 7) > tok[nt]) T[nt][i] = -INFINITY;
+  };
+  // The second product where some rows do not see some keys: a weight of zero
+  // does not hide an infinity or NaN, so those values count as zero, and where a
+  // weight meets one the row's sum becomes NaN.
+  const auto products_v_masked = [&](int j, const bf16x8(&W)[2][2]) {
+    bool bad = false;
+#pragma unroll
+    for (int ks = 0; ks < 2; ++ks)
+#pragma unroll
+      for (int mt = 0; mt < MT; ++mt) {
+        const bf16x8 vf = value_tile(j, ks, mt);
+        bad |= any_nonfinite(vf);
+        const bf16x8 fine = finite_only(vf);
+#pragma unroll
+        for (int nt = 0; nt < 2; ++nt)
+          O[mt][nt] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(fine, W[ks][nt], O[mt][nt], 0, 0, 0);
+      }
+    if (__builtin_expect(__any(bad), 0)) {
+#pragma unroll
+      for (int mt = 0; mt < MT; ++mt)
+#pragma unroll
+        for (int nt = 0; nt < 2; ++nt) {
+          f32x16 met = {};
+#pragma unroll
+          for (int ks = 0; ks < 2; ++ks)
+            met = __builtin_amdgcn_mfma_f32_32x32x16_bf16(nonfinite_ones(value_tile(j, ks, mt)), W[ks][nt], met, 0, 0, 0);
+#pragma unroll
+          for (int i = 0; i < 16; ++i) O[mt][nt][i] = met[i] != 0.f ? NAN : O[mt][nt][i];
+        }
+    }
+  };
+  const auto step = [&](int j, const f32x16(&now)[2], f32x16(&next)[2], const bf16x8(&before)[2][2],
+                        bf16x8(&W)[2][2]) {
+    products_k(j + 1, next);
+    weights(now, W);
+    products_v(j - 1, before);
+    raise(next, W);
+  };
+
+  load_k(0);
+  load_k(1);
+  load_v(0);
+  f32x16 SA[2], SB[2];
+  bf16x8 PA[2][2] = {}, PB[2][2];
+  // Step j makes the weights of step j, the scores of step j + 1 and the
+  // products with the values of step j - 1, which depend on none of each
+  // other: the matrix cores work while the weights are made.
+  for (int j = -1; j < n_sub;) {
+    if ((j & 1) && j > 0 && j + 2 < n_full) {  // every row sees every key
+      do {
+        sync((j + 1) >> 1);
+        step(j, SB, SA, PA, PB);
+        step(j + 1, SA, SB, PB, PA);
+        j += 2;
+      } while (j + 2 < n_full);
+      continue;
+    }
+    if (j & 1) sync((j + 1) >> 1);
+    if (j <= n_all) {
+      if (j > 0) products_v_masked(j - 1, PA);
+      if (j >= 0 && j < n_all) weights(SB, PA);
+      if (j + 1 < n_all) {
+        products_k(j + 1, SB);
+        if (j + 1 >= n_full) mask(j + 1, SB);
+        raise(SB, PA);
+      }
+    }
+    ++j;
+  }
+  if (n_all == n_sub) products_v_masked(n_sub - 1, PA);
+  __builtin_amdgcn_s_waitcnt(0x0F70);  // no load into this workgroup's LDS outlives it
+
+  uint16_t* out = reinterpret_cast<uint16_t*>(a.out);
+#pragma unroll
+  for (int nt = 0; nt < 2; ++nt) {
+    const int r = row0 + 32 * nt + l32;
+    const float inv = 1.f / sum_halves(l[nt]);
+    if (r >= R) continue;
+    uint16_t* p = out + (int64_t)(first + tok[nt]) * a.ldo + (hk * a.G + r % a.G) * D + 4 * h;
+#pragma unroll
+    for (int mt = 0; mt < MT; ++mt)
+#pragma unroll
+      for (int b = 0; b < 4; ++b) {
+        const f32x2 x = {O[mt][nt][4 * b] * inv, O[mt][nt][4 * b + 1] * inv};
+        const f32x2 y = {O[mt][nt][4 * b + 2] * inv, O[mt][nt][4 * b + 3] * inv};
+        const bf16x2 xb = __builtin_convertvector(x, bf16x2), yb = __builtin_convertvector(y, bf16x2);
+        *reinterpret_cast<bf16x4*>(p + 32 * mt + 8 * b) = __builtin_shufflevector(xb, yb, 0, 1, 2, 3);
+      }
+  }
+}
+
+template <int D>
+hipError_t launch_bf16(const PromptArgs& a, hipStream_t s) {
+  static const hipError_t ready = hipFuncSetAttribute(
+      reinterpret_cast<const void*>(prompt_bf16_kernel<D>),
+      hipFuncAttributeMaxDynamicSharedMemorySize, PromptTile<D>::kLds);
+  if (ready != hipSuccess) return ready;
+  // At most one unfilled workgroup per prompt.
+  const int64_t blocks = ((int64_t)a.n_tokens * a.G / PromptTile<D>::kRows + a.n) * a.Hkv;
+  prompt_bf16_kernel<D><<<(unsigned)blocks, 256, PromptTile<D>::kLds, s>>>(a);
+  return hipGetLastError();
+}
+
 }  // namespace
 
 hipError_t launch_prompt_attention(const PromptArgs& a, hipStream_t s) {
@@ -67,8 +391,7 @@ hipError_t launch_prompt_attention(const PromptArgs& a, hipStream_t s) {
     if (a.D == 64) prompt_kernel<float, 64><<<grid, 64, 0, s>>>(a);
     else prompt_kernel<float, 128><<<grid, 64, 0, s>>>(a);
   } else {
-    if (a.D == 64) prompt_kernel<uint16_t, 64><<<grid, 64, 0, s>>>(a);
-    else prompt_kernel<uint16_t, 128><<<grid, 64, 0, s>>>(a);
+    return a.D == 64 ? launch_bf16<64>(a, s) : launch_bf16<128>(a, s);
   }
   return hipGetLastError();
 }
