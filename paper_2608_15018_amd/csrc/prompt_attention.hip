@@ -118,7 +118,7 @@ struct PromptTile {
   static constexpr int kRows = 256;          // rows of a workgroup, 64 a wave
   static constexpr int kStage = 64 * D * 2;  // bytes of 64 keys, or of their values
   static constexpr int kLoads = D / 32;      // 1 KB loads a wave makes for it
-  static constexpr int kLds = 6 * kStage;    // three stages of each
+  static constexpr int kLds = 8 * kStage;    // four stages of each
 };
 
 template <int D>
@@ -126,8 +126,8 @@ __global__ __launch_bounds__(256, D == 64 ? 2 : 1) void prompt_bf16_kernel(Promp
   constexpr int kStage = PromptTile<D>::kStage, kLoads = PromptTile<D>::kLoads;
   constexpr int KS = D / 16, MT = D / 32, CH = D / 8;  // k steps, tiles of D, 16-byte chunks of a row
   extern __shared__ __attribute__((aligned(16))) char smem[];
-  char* const k_lds = smem;               // three stages of keys
-  char* const v_lds = smem + 3 * kStage;  // three of values
+  char* const k_lds = smem;               // four stages of keys
+  char* const v_lds = smem + 4 * kStage;  // four of values
 
   const int tid = threadIdx.x, lane = tid & 63, w = wave_id();
   const int hk = blockIdx.x % a.Hkv;
@@ -137,7 +137,7 @@ __global__ __launch_bounds__(256, D == 64 ? 2 : 1) void prompt_bf16_kernel(Promp
   const int R = len * a.G, row0 = qb * PromptTile<D>::kRows + w * 64;
   const int l32 = lane & 31, h = lane >> 5;
   const int last_row = min(qb * PromptTile<D>::kRows + PromptTile<D>::kRows, R) - 1;
-  const int n_stage = (last_row / a.G) / 64 + 1, n_sub = 2 * n_stage;
+  const int n_stage = (last_row / a.G) / 64 + 1;
 
   // This wave's rows: 32 steps of keys [0, n_full) that all of them see, and
   // up to n_all that some do.
@@ -173,15 +173,16 @@ __global__ __launch_bounds__(256, D == 64 ? 2 : 1) void prompt_bf16_kernel(Promp
                                        (lds_void*)(lds + (w * kLoads + i) * 1024), 16, 0, 0);
     }
   };
-  const auto load_k = [&](int s) { load_stage(kg, ldk, k_lds + (s % 3) * kStage, s, true); };
-  const auto load_v = [&](int s) { load_stage(vg, ldv, v_lds + (s % 3) * kStage, s, false); };
-  // Stage s of the keys and s - 1 of the values are there for everybody, and
-  // what the stage after next overwrites is read by nobody any more.
+  const auto load_k = [&](int s) { load_stage(kg, ldk, k_lds + (s & 3) * kStage, s, true); };
+  const auto load_v = [&](int s) { load_stage(vg, ldv, v_lds + (s & 3) * kStage, s, false); };
+  // Stages up to s + 1 of the keys and s of the values are there for
+  // everybody, and what is loaded now overwrites stages that nobody reads any
+  // more (s - 1 and s - 2).
   const auto sync = [&](int s) {
     if (kLoads == 4) __builtin_amdgcn_s_waitcnt(0x0F70 | 8); else __builtin_amdgcn_s_waitcnt(0x0F70 | 4);
     __builtin_amdgcn_s_barrier();
-    load_k(s + 2);
-    load_v(s + 1);
+    load_k(s + 3);
+    load_v(s + 2);
   };
 
   // Row m of a key tile is key m with bits 2 and 3 exchanged: then a lane's
@@ -201,7 +202,7 @@ __global__ __launch_bounds__(256, D == 64 ? 2 : 1) void prompt_bf16_kernel(Promp
   const float c = a.scale * 1.44269504088896340736f;
 
   const auto products_k = [&](int j, f32x16(&T)[2]) {
-    const char* kt = k_lds + ((j >> 1) % 3) * kStage + (j & 1) * 32 * D * 2 + k_at;
+    const char* kt = k_lds + ((j >> 1) & 3) * kStage + (j & 1) * 32 * D * 2 + k_at;
 #pragma unroll
     for (int nt = 0; nt < 2; ++nt) T[nt] = f32x16{};
 #pragma unroll
@@ -212,7 +213,7 @@ __global__ __launch_bounds__(256, D == 64 ? 2 : 1) void prompt_bf16_kernel(Promp
     }
   };
   const auto value_tile = [&](int j, int ks, int mt) -> bf16x8 {
-    const char* vt = v_lds + ((j >> 1) % 3) * kStage + ((j & 1) * 32 + 16 * ks) * D * 2 + v_at +
+    const char* vt = v_lds + ((j >> 1) & 3) * kStage + ((j & 1) * 32 + 16 * ks) * D * 2 + v_at +
                      ((mt ^ (D == 128 ? v_r : v_r >> 1)) << 6);
     const bf16x4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4bf16((__attribute__((address_space(3))) bf16x4*)vt);
     const bf16x4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4bf16((__attribute__((address_space(3))) bf16x4*)(vt + 4 * D * 2));
@@ -311,45 +312,54 @@ __global__ __launch_bounds__(256, D == 64 ? 2 : 1) void prompt_bf16_kernel(Promp
         }
     }
   };
-  const auto step = [&](int j, const f32x16(&now)[2], f32x16(&next)[2], const bf16x8(&before)[2][2],
-                        bf16x8(&W)[2][2]) {
-    products_k(j + 1, next);
-    weights(now, W);
-    products_v(j - 1, before);
-    raise(next, W);
-  };
-
   load_k(0);
   load_k(1);
   load_v(0);
-  f32x16 SA[2], SB[2];
-  bf16x8 PA[2][2] = {}, PB[2][2];
-  // Step j makes the weights of step j, the scores of step j + 1 and the
-  // products with the values of step j - 1, which depend on none of each
-  // other: the matrix cores work while the weights are made.
-  for (int j = -1; j < n_sub;) {
-    if ((j & 1) && j > 0 && j + 2 < n_full) {  // every row sees every key
-      do {
-        sync((j + 1) >> 1);
-        step(j, SB, SA, PA, PB);
-        step(j + 1, SA, SB, PB, PA);
-        j += 2;
-      } while (j + 2 < n_full);
-      continue;
+  load_k(2);
+  load_v(1);
+  f32x16 SA[2];
+  bf16x8 PA[2][2] = {};
+  int s = 0;
+  if (D == 128 && n_full >= 4) {
+    // Steps whose keys every row of the wave sees, two a stage, as far as they
+    // are even in number.  Each makes the weights of step j, the scores of step
+    // j + 1 and the products with the values of step j - 1, which depend on
+    // none of each other: the matrix cores work while the weights are made.
+    // (At D = 64 two waves share a SIMD and do this for each other.)
+    f32x16 SB[2];
+    bf16x8 PB[2][2];
+    const int n_fast = n_full >> 1;
+    sync(0);
+    products_k(0, SA);
+    raise(SA, PA);
+    products_k(1, SB);
+    weights(SA, PA);
+    raise(SB, PA);
+    for (s = 1; s < n_fast; ++s) {
+      products_k(2 * s, SA);
+      weights(SB, PB);
+      products_v(2 * s - 2, PA);
+      raise(SA, PB);
+      sync(s);
+      products_k(2 * s + 1, SB);
+      weights(SA, PA);
+      products_v(2 * s - 1, PB);
+      raise(SB, PA);
     }
-    if (j & 1) sync((j + 1) >> 1);
-    if (j <= n_all) {
-      if (j > 0) products_v_masked(j - 1, PA);
-      if (j >= 0 && j < n_all) weights(SB, PA);
-      if (j + 1 < n_all) {
-        products_k(j + 1, SB);
-        if (j + 1 >= n_full) mask(j + 1, SB);
-        raise(SB, PA);
-      }
-    }
-    ++j;
+    weights(SB, PB);
+    products_v(2 * s - 2, PA);
+    products_v(2 * s - 1, PB);
   }
-  if (n_all == n_sub) products_v_masked(n_sub - 1, PA);
+  for (; s < n_stage; ++s) {
+    sync(s);
+    for (int j = 2 * s; j < 2 * s + 2 && j < n_all; ++j) {
+      products_k(j, SA);
+      if (j >= n_full) mask(j, SA);
+      raise(SA, PA);
+      weights(SA, PA);
+      if (j < n_full) products_v(j, PA); else products_v_masked(j, PA);
+    }
+  }
   __builtin_amdgcn_s_waitcnt(0x0F70);  // no load into this workgroup's LDS outlives it
 
   uint16_t* out = reinterpret_cast<uint16_t*>(a.out);
