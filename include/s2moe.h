@@ -405,7 +405,7 @@ s2moe_status s2moe_kv_reserve(const s2moe_kv_cache *cache, int32_t n, const int3
    .. tok_off[i + 1] - 1 of k and v, [n_tokens][n_kv_heads][head_dim] in the
    cache's dtype with ldk and ldv elements from one token to the next (a slice
    of a fused projection's output will do).  k and v 16-byte aligned, and so
-   ldk and ldv in bytes; ldk, ldv >= n_kv_heads * head_dim.  Tokens whose slot
+   ldk and ldv in bytes; n_kv_heads * head_dim <= ldk, ldv <= 2^22.  Tokens whose slot
    lies in no page that the sequence holds alone are dropped: reserve first. */
 s2moe_status s2moe_kv_append(const s2moe_kv_cache *cache, int32_t layer, int32_t n,
                              int32_t n_tokens, const int32_t *seqs, const int32_t *tok_off,

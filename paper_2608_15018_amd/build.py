@@ -26,13 +26,16 @@ ROCM_INC = os.path.join(os.environ.get("ROCM_PATH", "/opt/rocm"), "include")
 HIPCC = shutil.which("hipcc") or "/opt/rocm/bin/hipcc"
 # Packed fp32 VALU instructions are switched off for all device code.
 DEVICE_FLAGS = ["-Xclang", "-target-feature", "-Xclang", "-packed-fp32-ops"]
+# Kernels that read their matrix products with vector instructions in the same
+# step want those results in ordinary registers, not in accumulation registers.
+SOURCE_FLAGS = {"prompt_attention.hip": ["-mllvm", "-amdgpu-mfma-vgpr-form=1"]}
 COMMON = ["-O3", "-std=c++17", "-fPIC", f"--offload-arch={ARCH}", "-I", INCLUDE, "-I", CSRC,
           "-Wall", "-Wno-unused-function"]
 
 
 def _compile(src: str, objdir: str = OBJDIR, defines=()) -> str:
     out = os.path.join(objdir, os.path.splitext(src)[0] + ".o")
-    cmd = [HIPCC, *COMMON, *DEVICE_FLAGS, *defines, "-c", os.path.join(CSRC, src), "-o", out]
+    cmd = [HIPCC, *COMMON, *DEVICE_FLAGS, *SOURCE_FLAGS.get(src, []), *defines, "-c", os.path.join(CSRC, src), "-o", out]
     if src.endswith(".cpp"):
         cmd = [HIPCC, *COMMON, "-x", "c++", "-D__HIP_PLATFORM_AMD__=1", "-I", ROCM_INC, *defines,
                "-c", os.path.join(CSRC, src), "-o", out]

@@ -96,9 +96,11 @@ s2moe_status check_layer_index(const char* fn, const s2moe::KvCache& c, int32_t 
 
 // Rows of `heads` heads, `ld` elements apart.
 s2moe_status check_rows(const char* fn, const char* name, int64_t ld, int heads, int D, int elt) {
-  if (ld < (int64_t)heads * D || ld > (int64_t)1 << 40)
+  if (ld < (int64_t)heads * D)
     return fail(S2MOE_EINVAL, "%s: %s = %lld must be at least %d heads of %d", fn, name,
                 (long long)ld, heads, D);
+  if (ld > (int64_t)1 << 22)
+    return fail(S2MOE_EUNSUPPORTED, "%s: %s = %lld exceeds 2^22 elements", fn, name, (long long)ld);
   if (ld * elt % 16 != 0)
     return fail(S2MOE_EINVAL, "%s: %s = %lld elements is not a multiple of 16 bytes", fn, name,
                 (long long)ld);

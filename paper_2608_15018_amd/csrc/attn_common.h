@@ -54,6 +54,27 @@ __device__ __forceinline__ bf16x8 pack8(const float* x) {
   return out;
 }
 
+// 16 bytes per lane from base + off (off per lane) to 1 KB of LDS at `lds`,
+// lane after lane, without a register between.  In asm, because the compiler
+// would wait for every such load before the next read of LDS; whoever reads
+// the data waits for it by count and passes a barrier first.
+__device__ __forceinline__ void load_to_lds(const char* base, uint32_t off, const char* lds) {
+  const uint32_t at = __builtin_amdgcn_readfirstlane((uint32_t)(uintptr_t)(lds_void*)lds);
+  asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %2"
+               :
+               : "s"(at), "v"(off), "s"(base)
+               : "memory");
+}
+template <int N>
+__device__ __forceinline__ void wait_loads() {  // until at most N are in flight
+  asm volatile("s_waitcnt vmcnt(%0)" : : "n"(N) : "memory");
+}
+
+__device__ __forceinline__ bf16x2 pack2(float a, float b) {
+  const f32x2 v = {a, b};
+  return __builtin_convertvector(v, bf16x2);
+}
+
 // Whether any of eight bf16 values is an infinity or NaN, and the values with
 // those replaced by zero.
 __device__ __forceinline__ bool any_nonfinite(bf16x8 x) {

@@ -159,27 +159,37 @@ __global__ __launch_bounds__(256, D == 64 ? 2 : 1) void prompt_bf16_kernel(Promp
   }
 
   // Staging: chunk c of row r of a stage lies at chunk c ^ swizzle(r), so that
-  // the reads below spread over all banks.
+  // the reads below spread over all banks.  A lane's place in a stage is the
+  // same for all stages; only in the last are rows past the prompt its last.
   const char* const kg = a.k + ((int64_t)first * a.ldk + hk * D) * 2;
   const char* const vg = a.v + ((int64_t)first * a.ldv + hk * D) * 2;
-  const int64_t ldk = a.ldk * 2, ldv = a.ldv * 2;
-  const auto load_stage = [&](const char* g, int64_t ld, char* lds, int s, bool keys) {
-#pragma unroll
-    for (int i = 0; i < kLoads; ++i) {
-      const int r = (w * kLoads + i) * (64 / CH) + lane / CH;
-      const int x = keys ? (D == 128 ? r & 15 : (r >> 1) & 7) : (D == 128 ? (r & 3) << 2 : ((r >> 1) & 1) << 2);
-      const int key = min(64 * s + r, len - 1);
-      __builtin_amdgcn_global_load_lds((global_void*)(g + key * ld + (((lane % CH) ^ x) << 4)),
-                                       (lds_void*)(lds + (w * kLoads + i) * 1024), 16, 0, 0);
-    }
+  const uint32_t ldk = (uint32_t)a.ldk * 2, ldv = (uint32_t)a.ldv * 2;
+  const auto place = [&](int i, uint32_t ld, bool keys, int rows) {
+    const int r = (w * kLoads + i) * (64 / CH) + lane / CH;
+    const int x = keys ? (D == 128 ? r & 15 : (r >> 1) & 7) : (D == 128 ? (r & 3) << 2 : ((r >> 1) & 1) << 2);
+    return (uint32_t)min(r, rows - 1) * ld + (((lane % CH) ^ x) << 4);
   };
-  const auto load_k = [&](int s) { load_stage(kg, ldk, k_lds + (s & 3) * kStage, s, true); };
-  const auto load_v = [&](int s) { load_stage(vg, ldv, v_lds + (s & 3) * kStage, s, false); };
+  uint32_t k_off[kLoads], v_off[kLoads];
+#pragma unroll
+  for (int i = 0; i < kLoads; ++i) {
+    k_off[i] = place(i, ldk, true, 64);
+    v_off[i] = place(i, ldv, false, 64);
+  }
+  const auto load_stage = [&](const char* g, uint32_t ld, const uint32_t(&off)[kLoads], char* lds, int s, bool keys) {
+    s = min(s, (len - 1) >> 6);  // past the end: the last stage again, unused
+    const char* from = g + (uint64_t)s * 64 * ld;
+    const int rows = len - 64 * s;
+#pragma unroll
+    for (int i = 0; i < kLoads; ++i)
+      load_to_lds(from, rows >= 64 ? off[i] : place(i, ld, keys, rows), lds + (w * kLoads + i) * 1024);
+  };
+  const auto load_k = [&](int s) { load_stage(kg, ldk, k_off, k_lds + (s & 3) * kStage, s, true); };
+  const auto load_v = [&](int s) { load_stage(vg, ldv, v_off, v_lds + (s & 3) * kStage, s, false); };
   // Stages up to s + 1 of the keys and s of the values are there for
   // everybody, and what is loaded now overwrites stages that nobody reads any
   // more (s - 1 and s - 2).
   const auto sync = [&](int s) {
-    if (kLoads == 4) __builtin_amdgcn_s_waitcnt(0x0F70 | 8); else __builtin_amdgcn_s_waitcnt(0x0F70 | 4);
+    wait_loads<2 * kLoads>();
     __builtin_amdgcn_s_barrier();
     load_k(s + 3);
     load_v(s + 2);
@@ -201,13 +211,16 @@ __global__ __launch_bounds__(256, D == 64 ? 2 : 1) void prompt_bf16_kernel(Promp
   float shift[2] = {0.f, 0.f}, limit[2] = {-INFINITY, -INFINITY}, l[2] = {0.f, 0.f};
   const float c = a.scale * 1.44269504088896340736f;
 
+  const auto key_tile = [&](int j, int ks) {
+    return *reinterpret_cast<const bf16x8*>(k_lds + ((j >> 1) & 3) * kStage + (j & 1) * 32 * D * 2 + k_at +
+                                            (k_x ^ (ks << 5)));
+  };
   const auto products_k = [&](int j, f32x16(&T)[2]) {
-    const char* kt = k_lds + ((j >> 1) & 3) * kStage + (j & 1) * 32 * D * 2 + k_at;
 #pragma unroll
     for (int nt = 0; nt < 2; ++nt) T[nt] = f32x16{};
 #pragma unroll
     for (int ks = 0; ks < KS; ++ks) {
-      const bf16x8 kf = *reinterpret_cast<const bf16x8*>(kt + (k_x ^ (ks << 5)));
+      const bf16x8 kf = key_tile(j, ks);
 #pragma unroll
       for (int nt = 0; nt < 2; ++nt) T[nt] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(kf, qf[ks][nt], T[nt], 0, 0, 0);
     }
@@ -249,11 +262,10 @@ __global__ __launch_bounds__(256, D == 64 ? 2 : 1) void prompt_bf16_kernel(Promp
     for (int i = 3; i < 15; i += 2) m = max3(m, T[i], T[i + 1]);
     return fmaxf(m, T[15]) * c;
   };
-  // Scores T of the next step: a row with one past its limit moves its maximum
-  // there, and what it has summed so far, W's step included, shrinks by 2^-8 or
-  // more (so rounding W once more does not count).
-  const auto raise = [&](const f32x16(&T)[2], bf16x8(&W)[2][2]) {
-    const float m[2] = {largest(T[0]), largest(T[1])};
+  // Scores of the next step whose largest are m: a row with one past its limit
+  // moves its maximum there, and what it has summed so far, W's step included,
+  // shrinks by 2^-8 or more (so rounding W once more does not count).
+  const auto raise_to = [&](const float(&m)[2], bf16x8(&W)[2][2]) {
     if (__builtin_expect(__any(m[0] > limit[0] || m[1] > limit[1]), 0)) {
 #pragma unroll
       for (int nt = 0; nt < 2; ++nt) {
@@ -264,7 +276,10 @@ __global__ __launch_bounds__(256, D == 64 ? 2 : 1) void prompt_bf16_kernel(Promp
         limit[nt] = moves ? top + kLag : limit[nt];
         l[nt] *= f;
 #pragma unroll
-        for (int mt = 0; mt < MT; ++mt) O[mt][nt] *= f;
+        for (int mt = 0; mt < MT; ++mt) {
+          O[mt][nt] *= f;
+          if (D == 128) asm volatile("" : "+a"(O[mt][nt]));
+        }
 #pragma unroll
         for (int ks = 0; ks < 2; ++ks) {
           float p[8];
@@ -274,6 +289,10 @@ __global__ __launch_bounds__(256, D == 64 ? 2 : 1) void prompt_bf16_kernel(Promp
         }
       }
     }
+  };
+  const auto raise = [&](const f32x16(&T)[2], bf16x8(&W)[2][2]) {
+    const float m[2] = {largest(T[0]), largest(T[1])};
+    raise_to(m, W);
   };
   const auto mask = [&](int j, f32x16(&T)[2]) {
 #pragma unroll
@@ -312,6 +331,73 @@ __global__ __launch_bounds__(256, D == 64 ? 2 : 1) void prompt_bf16_kernel(Promp
         }
     }
   };
+  // One step of the overlapped loop: the scores of step j + 1 into `next`, the
+  // weights of step j from `now` into W, and the products of the weights
+  // `before` with the values of step j - 1.  Sixteen fragments of keys and
+  // values, read four ahead, with two matrix instructions each; between those,
+  // two scores become weights, and then the new scores' maximum is taken.
+  const auto step = [&](int j, const f32x16(&now)[2], f32x16(&next)[2], const bf16x8(&before)[2][2],
+                        bf16x8(&W)[2][2], bf16x8(&ahead)[4]) {
+    constexpr int NF = KS + 2 * MT, EL = 32 / NF;  // fragments, scores each
+    bf16x8 f[NF + 4];
+    bf16x2 w2[16];
+    float m[2];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) f[i] = ahead[i];
+#pragma unroll
+    for (int i = 0; i < NF; ++i) {
+      const int n = i + 4;
+      if (n < KS) f[n] = key_tile(j + 1, n);
+      else if (n < NF) f[n] = value_tile(j - 1, (n - KS) / MT, (n - KS) % MT);
+      else f[n] = key_tile(j + 2, n - NF);
+#pragma unroll
+      for (int nt = 0; nt < 2; ++nt) {
+        if (i < KS) {
+          next[nt] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(f[i], qf[i < KS ? i : 0][nt], i == 0 ? f32x16{} : next[nt], 0, 0, 0);
+        } else {
+          constexpr int dummy = 0;
+          const int ks = i < KS ? dummy : (i - KS) / MT, mt = i < KS ? dummy : (i - KS) % MT;
+          O[mt][nt] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(f[i], before[ks][nt], O[mt][nt], 0, 0, 0);
+        }
+      }
+#pragma unroll
+      for (int e = i * EL; e < i * EL + EL; e += 2) {
+        const int nt = e >> 4, x = e & 15;
+        const float p = exp2_fast(fmaf(now[nt][x], c, -shift[nt]));
+        const float r = exp2_fast(fmaf(now[nt][x + 1], c, -shift[nt]));
+        l[nt] += p;
+        l[nt] += r;
+        w2[e >> 1] = pack2(p, r);
+      }
+      if (i >= KS + 2) {  // sixteen maxima over the last fragments
+        constexpr int per = (16 + NF - KS - 3) / (NF - KS - 2);
+#pragma unroll
+        for (int g = (i - KS - 2) * per; g < (i - KS - 1) * per && g < 16; ++g) {
+          const int nt = g >> 3, x = 2 * (g & 7);
+          m[nt] = x == 0 ? fmaxf(next[nt][0], next[nt][1]) : max3(m[nt], next[nt][x], next[nt][x + 1]);
+        }
+      }
+      __builtin_amdgcn_sched_barrier(0);
+    }
+#pragma unroll
+    for (int nt = 0; nt < 2; ++nt)
+#pragma unroll
+      for (int ks = 0; ks < 2; ++ks)
+#pragma unroll
+        for (int x = 0; x < 4; ++x) {
+          W[ks][nt][2 * x] = w2[8 * nt + 4 * ks + x][0];
+          W[ks][nt][2 * x + 1] = w2[8 * nt + 4 * ks + x][1];
+        }
+#pragma unroll
+    for (int i = 0; i < 4; ++i) ahead[i] = f[NF + i];
+    asm volatile("" : "+v"(next[0]), "+v"(next[1]));
+#pragma unroll
+    for (int mt = 0; mt < MT; ++mt) asm volatile("" : "+a"(O[mt][0]), "+a"(O[mt][1]));
+    m[0] *= c;
+    m[1] *= c;
+    raise_to(m, W);
+  };
+
   load_k(0);
   load_k(1);
   load_v(0);
@@ -322,29 +408,26 @@ __global__ __launch_bounds__(256, D == 64 ? 2 : 1) void prompt_bf16_kernel(Promp
   int s = 0;
   if (D == 128 && n_full >= 4) {
     // Steps whose keys every row of the wave sees, two a stage, as far as they
-    // are even in number.  Each makes the weights of step j, the scores of step
-    // j + 1 and the products with the values of step j - 1, which depend on
-    // none of each other: the matrix cores work while the weights are made.
-    // (At D = 64 two waves share a SIMD and do this for each other.)
+    // are even in number.  What a step does depends on nothing else in it, so
+    // the matrix cores work while the weights are made.  (At D = 64 two waves
+    // share a SIMD and do this for each other.)
     f32x16 SB[2];
-    bf16x8 PB[2][2];
+    bf16x8 PB[2][2], ahead[4];
     const int n_fast = n_full >> 1;
+#pragma unroll
+    for (int ks = 0; ks < KS; ++ks) asm volatile("" : "+a"(qf[ks][0]), "+a"(qf[ks][1]));
     sync(0);
     products_k(0, SA);
     raise(SA, PA);
     products_k(1, SB);
     weights(SA, PA);
     raise(SB, PA);
+#pragma unroll
+    for (int i = 0; i < 4; ++i) ahead[i] = key_tile(2, i);
     for (s = 1; s < n_fast; ++s) {
-      products_k(2 * s, SA);
-      weights(SB, PB);
-      products_v(2 * s - 2, PA);
-      raise(SA, PB);
+      step(2 * s - 1, SB, SA, PA, PB, ahead);
       sync(s);
-      products_k(2 * s + 1, SB);
-      weights(SA, PA);
-      products_v(2 * s - 1, PB);
-      raise(SB, PA);
+      step(2 * s, SA, SB, PB, PA, ahead);
     }
     weights(SB, PB);
     products_v(2 * s - 2, PA);
@@ -360,7 +443,7 @@ __global__ __launch_bounds__(256, D == 64 ? 2 : 1) void prompt_bf16_kernel(Promp
       if (j < n_full) products_v(j, PA); else products_v_masked(j, PA);
     }
   }
-  __builtin_amdgcn_s_waitcnt(0x0F70);  // no load into this workgroup's LDS outlives it
+  wait_loads<0>();  // no load into this workgroup's LDS outlives it
 
   uint16_t* out = reinterpret_cast<uint16_t*>(a.out);
 #pragma unroll
