@@ -12,6 +12,12 @@ typedef __attribute__((__vector_size__(16 * sizeof(float)))) float f32x16;
 typedef __attribute__((address_space(3))) void lds_void;
 typedef const __attribute__((address_space(1))) void global_void;
 
+// p[i] by a scalar load where i is the same in all lanes; nothing writes p while
+// the kernel runs.
+__device__ __forceinline__ int constant(const int32_t* p, int64_t i) {
+  return reinterpret_cast<const __attribute__((address_space(4))) int32_t*>(reinterpret_cast<uintptr_t>(p))[i];
+}
+
 // A running maximum may lag behind by this much (base-2 logarithm) before the
 // accumulators are rescaled: weights stay below 2^8, far inside fp32 and of
 // the same relative precision in bf16.
@@ -93,6 +99,25 @@ __device__ __forceinline__ bf16x8 finite_only(bf16x8 x) {
     if ((u[i] & 0x7F800000u) == 0x7F800000u) u[i] &= 0xFFFFu;
   }
   return __builtin_bit_cast(bf16x8, u);
+}
+
+__device__ __forceinline__ bool any_nonfinite(f32x4 x) {
+  const u32x4 u = __builtin_bit_cast(u32x4, x);
+  bool bad = false;
+#pragma unroll
+  for (int i = 0; i < 4; ++i) bad |= (u[i] & 0x7F800000u) == 0x7F800000u;
+  return bad;
+}
+__device__ __forceinline__ f32x4 finite_only(f32x4 x) {
+#pragma unroll
+  for (int i = 0; i < 4; ++i)
+    if ((__float_as_uint(x[i]) & 0x7F800000u) == 0x7F800000u) x[i] = 0.f;
+  return x;
+}
+__device__ __forceinline__ f32x4 nonfinite_ones(f32x4 x) {
+#pragma unroll
+  for (int i = 0; i < 4; ++i) x[i] = (__float_as_uint(x[i]) & 0x7F800000u) == 0x7F800000u ? 1.f : 0.f;
+  return x;
 }
 
 // 1 where a value is an infinity or NaN, else 0.

@@ -1,111 +1,567 @@
-// Attention of drafted tokens over the cache: one wave per (node, query head).
+// Attention of drafted tokens over the paged cache.
+//
+// Rows.  The query heads of one kv head read the same keys, so the G = Hq / Hkv
+// heads of a sequence's T nodes are T G rows of one product with the keys,
+// taken 16 NT at a time by a workgroup.
+//
+// Products.  S^T = K Q^T and O^T = V^T P^T, so that a lane holds scores of one
+// row: the maximum and the sum of a row need no exchange but over the four
+// 16-lane groups, and the scores are, in the registers where the first product
+// leaves them, the operand of the second.  That takes row m of the x-th of two
+// 16-key tiles to be key 8 (m / 4) + 4 x + m % 4 of the step: lane group g then
+// holds keys 8 g .. 8 g + 7, and the cache keeps eight neighbouring tokens of one
+// coordinate of V together, so V is read in the order in which it is needed.
+// No operand passes through LDS.
+//
+// Softmax.  One pass with a running maximum per row; it may lag behind the true
+// one by 2^8, so that the accumulators are rescaled about once a row.
+//
+// Split.  The work is a list of units (sequence, kv head, row block, 128 keys),
+// cut into equal stretches, one for each of a fixed number of workgroups,
+// whatever the lengths are: the host does not know them.  Within a workgroup
+// the four waves take 32 keys each.  A row block that one workgroup does not
+// finish goes to the workspace in parts, and a second launch joins them.
 #include "attention.h"
-#include "common.h"
+#include "attn_common.h"
 
 namespace s2moe {
 namespace {
 
-__device__ __forceinline__ float load(const float* p) { return *p; }
-__device__ __forceinline__ float load(const uint16_t* p) { return bf16_to_f32(*p); }
-__device__ __forceinline__ void store(float* p, float x) { *p = x; }
-__device__ __forceinline__ void store(uint16_t* p, float x) { *p = (uint16_t)f32_to_bf16(x); }
+constexpr int kTile = 128;  // keys of a unit, 32 a wave
 
+// A row block whose parts the joining launch adds, as the workgroup that has
+// its first keys leaves it.
+struct Split {
+  int parts;  // 0: none starts here
+  int slot;   // of this workgroup's part; the following workgroups' is their first
+  int first;  // first token of the tree
+  int head;   // kv head
+  int row0;   // first row
+  int rows;
+};
+
+template <typename E>
+struct Type;
+template <>
+struct Type<uint16_t> {
+  typedef bf16x8 frag;          // 8 of k
+  static constexpr int kK = 8;  // elements of 16 bytes
+};
+template <>
+struct Type<float> {
+  typedef f32x4 frag;
+  static constexpr int kK = 4;
+};
+
+__device__ __forceinline__ f32x4 mma(bf16x8 a, bf16x8 b, f32x4 c) {
+  return __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, b, c, 0, 0, 0);
+}
+// Four products of one k step of 4 each: element j of the fragments.
+__device__ __forceinline__ f32x4 mma(f32x4 a, f32x4 b, f32x4 c) {
+#pragma unroll
+  for (int j = 0; j < 4; ++j) c = __builtin_amdgcn_mfma_f32_16x16x4f32(a[j], b[j], c, 0, 0, 0);
+  return c;
+}
+
+template <typename E, int D, int NT>
+struct TreePlan {
+  static constexpr int kRows = 16 * NT;
+  // Workgroups that fit a compute unit.
+  static constexpr int kPerCu = NT == 4 || (NT == 2 && D * sizeof(E) == 512) ? 1 : 2;
+  static constexpr int kGroups = 256 * kPerCu;
+  static constexpr size_t kPartFloats = (size_t)kRows * (D + 2);
+  static constexpr size_t kBytes = kGroups * (2 * kPartFloats * 4 + sizeof(Split));
+};
+
+__device__ __forceinline__ bool sane(const TreeArgs& a, int first, int end) {
+  return first >= 0 && first < end && end <= a.n_tokens;
+}
+
+// Tree and context of request i: first token, nodes, cached tokens, table row.
+struct Request {
+  int first, T, len, total;
+  const int32_t* row;
+};
+__device__ __forceinline__ Request request(const TreeArgs& a, int i) {
+  Request r{};
+  r.first = constant(a.tok_off, i);
+  const int end = constant(a.tok_off, i + 1), s = constant(a.seqs, i);
+  if (!sane(a, r.first, end) || s < 0 || s >= a.max_seqs) return r;
+  r.T = min(end - r.first, a.max_nodes);
+  const int cap = a.max_pages << a.log_p;
+  r.len = min(max(constant(a.length, s), 0), cap);
+  r.total = r.len + min(r.T, cap - r.len);
+  r.row = a.table + (int64_t)s * a.max_pages;
+  return r;
+}
+
+// Ancestors of every node of a tree by pointer doubling: word 0 of a row of
+// kMaskRow is all ones (cached tokens), 1 .. 8 the node's own bit and its
+// ancestors', the rest zeros.  Nodes that hang below an invalid parent get
+// dead_s != 0.
+constexpr int kMaskRow = 11;
+__device__ void ancestors(const int32_t* parent, int T, uint32_t* mask_s, int* jump_s,
+                          uint8_t* dead_s) {
+  const int i = threadIdx.x;
+  int jump = -1, dead = 0;
+  uint32_t word[kMaxNodes / 32];
+#pragma unroll
+  for (int x = 0; x < kMaxNodes / 32; ++x) word[x] = 0;
+  if (i < T) {
+    const int p = parent[i];
+    dead = p != -1 && (p < 0 || p >= i);
+    jump = dead ? -1 : p;
+#pragma unroll
+    for (int x = 0; x < kMaxNodes / 32; ++x) word[x] = x == i >> 5 ? 1u << (i & 31) : 0u;
+    mask_s[i * kMaskRow] = ~0u;
+    mask_s[i * kMaskRow + 9] = 0;
+    mask_s[i * kMaskRow + 10] = 0;
+  }
+  for (;;) {
+    if (i < T) {
+#pragma unroll
+      for (int x = 0; x < kMaxNodes / 32; ++x) mask_s[i * kMaskRow + 1 + x] = word[x];
+      jump_s[i] = jump;
+      dead_s[i] = dead;
+    }
+    if (!__syncthreads_or(jump >= 0)) break;
+    if (jump >= 0) {
+#pragma unroll
+      for (int x = 0; x < kMaxNodes / 32; ++x) word[x] |= mask_s[jump * kMaskRow + 1 + x];
+      dead |= dead_s[jump];
+      jump = jump_s[jump];
+    }
+    __syncthreads();
+  }
+}
+
+// Which of eight slots from node k0 on a row sees, k0 < 0 being cached tokens.
+__device__ __forceinline__ uint32_t seen8(const uint32_t* mask, int k0) {
+  k0 = min(max(k0, -32), kMaxNodes);
+  const int x = (k0 + 32) >> 5;
+  const uint64_t two = (uint64_t)mask[x + 1] << 32 | mask[x];
+  return (uint32_t)(two >> (k0 & 31)) & 0xFFu;
+}
+
+// D / 16 elements of an output row, times `inv`; zeros where inv is 0.
 template <typename E, int D>
-__global__ __launch_bounds__(64) void tree_kernel(TreeArgs a) {
-  __shared__ float q_s[D], p_s[64];
-  __shared__ uint32_t seen_s[kMaxNodes / 32];
-  const int t = blockIdx.x, h = blockIdx.y, lane = threadIdx.x;
-  int lo = 0, hi = a.n;
-  while (hi - lo > 1) {
-    const int mid = (lo + hi) / 2;
-    if (a.tok_off[mid] <= t) lo = mid; else hi = mid;
+__device__ __forceinline__ void write_row(const TreeArgs& a, int first, int hk, int row, int od,
+                                          const float* o, float inv) {
+  const int64_t at = (int64_t)(first + row / a.G) * a.ldo + (hk * a.G + row % a.G) * D + od;
+#pragma unroll
+  for (int y = 0; y < D / 16; y += 4) {
+    f32x4 v;
+#pragma unroll
+    for (int e = 0; e < 4; ++e) v[e] = inv == 0.f ? 0.f : o[y + e] * inv;
+    if constexpr (sizeof(E) == 4)
+      *reinterpret_cast<f32x4*>(reinterpret_cast<float*>(a.out) + at + y) = v;
+    else
+      *reinterpret_cast<bf16x4*>(reinterpret_cast<uint16_t*>(a.out) + at + y) = __builtin_convertvector(v, bf16x4);
   }
-  const int first = a.tok_off[lo];
-  int T = a.tok_off[lo + 1] - first;
-  const int s = a.seqs[lo], node = t - first;
-  if (first < 0 || node < 0 || node >= T || node >= a.max_nodes || s < 0 || s >= a.max_seqs) return;
-  T = T < a.max_nodes ? T : a.max_nodes;
-  if (lane < kMaxNodes / 32) seen_s[lane] = 0;
-  const E* q = reinterpret_cast<const E*>(a.q) + t * a.ldq + h * D;
-  for (int d = lane; d < D; d += 64) q_s[d] = load(q + d);
+}
+
+template <typename E, int D, int NT>
+__global__ __launch_bounds__(256, (TreePlan<E, D, NT>::kPerCu)) void tree_kernel(TreeArgs a) {
+  typedef typename Type<E>::frag frag;
+  typedef TreePlan<E, D, NT> Plan;
+  constexpr bool kF32 = sizeof(E) == 4;
+  constexpr int RB = 16 * NT, MT = D / 16, ES = sizeof(E);
+  constexpr int KC = D * ES / 64;  // 64-byte pieces of a key, 16 bytes a lane
+  constexpr int VC = ES / 2;       // 16-byte pieces of eight values
+  __shared__ int64_t before_s[kKvMaxRequests + 1];
+  __shared__ __attribute__((aligned(16))) float sum_s[4][16][D + 4];
+  __shared__ float m_s[4][RB], l_s[4][RB];
+  __shared__ uint32_t mask_s[kMaxNodes * kMaskRow];
+  __shared__ int jump_s[kMaxNodes];
+  __shared__ uint8_t dead_s[kMaxNodes];
+  __shared__ int64_t wave_s[4];
+
+  const int tid = threadIdx.x, lane = tid & 63, w = wave_id();
+  const int n16 = lane & 15, g = lane >> 4;
+  Split* const splits = reinterpret_cast<Split*>(a.ws + (size_t)Plan::kGroups * 2 * Plan::kPartFloats);
+  float* const parts = a.ws;
+
+  // Units before each request.
+  int64_t mine = 0;
+  for (int x = 0; x < 4; ++x) {
+    const int i = 4 * tid + x;
+    if (i < a.n) {
+      const Request r = request(a, i);
+      before_s[i] = mine;
+      mine += (int64_t)((r.T * a.G + RB - 1) / RB) * a.Hkv * ((r.total + kTile - 1) / kTile);
+    }
+  }
+  int64_t inc = mine;
+#pragma unroll
+  for (int d = 1; d < 64; d <<= 1) {
+    const int64_t y = __shfl_up(inc, d);
+    if (lane >= d) inc += y;
+  }
+  if (lane == 63) wave_s[w] = inc;
   __syncthreads();
-  bool ok = true;
-  if (lane == 0) {
-    int j = node;
-    for (;;) {
-      seen_s[j >> 5] |= 1u << (j & 31);
-      const int p = a.parent[first + j];
-      if (p == -1) break;
-      if (p < 0 || p >= j) { ok = false; break; }
-      j = p;
-    }
+  int64_t at = inc - mine, total = 0;
+#pragma unroll
+  for (int x = 0; x < 4; ++x) {
+    at += x < w ? wave_s[x] : 0;
+    total += wave_s[x];
   }
-  ok = __shfl(ok, 0);
+  for (int x = 0; x < 4; ++x)
+    if (4 * tid + x < a.n) before_s[4 * tid + x] += at;
+  if (tid == 0) before_s[a.n] = total;
   __syncthreads();
-  const int len = a.length[s], cap = a.max_pages << a.log_p;
-  int total = len + T;
-  total = total < cap ? total : cap;
-  if (!ok) total = 0;
-  const int g = h / a.G;
-  const int64_t page_elems = (int64_t)a.Hkv * a.P * D;
-  const int32_t* row = a.table + (int64_t)s * a.max_pages;
-  float m = -INFINITY, l = 0.f, acc[D / 64];
-  for (int i = 0; i < D / 64; ++i) acc[i] = 0.f;
-  for (int k0 = 0; k0 < total; k0 += 64) {
-    const int key = k0 + lane;
-    bool vis = key < total;
-    if (vis && key >= len) vis = (seen_s[(key - len) >> 5] >> ((key - len) & 31)) & 1;
-    float x = -INFINITY;
-    if (vis) {
-      int page = row[key >> a.log_p];
-      page = page < 0 ? 0 : (page >= a.n_pages ? a.n_pages - 1 : page);
-      const E* kp = reinterpret_cast<const E*>(a.k) + page * page_elems +
-                    ((int64_t)g * a.P + (key & (a.P - 1))) * D;
-      x = 0.f;
-      for (int d = 0; d < D; ++d) x = fmaf(q_s[d], load(kp + d), x);
-      x *= a.scale;
+  const int64_t share = (total + Plan::kGroups - 1) / Plan::kGroups;
+  int64_t u = blockIdx.x * share;
+  const int64_t u_end = min(u + share, total), u_first = u;
+  int split_parts = 0;  // of a row block that starts here and goes on elsewhere
+
+  int i = 0;
+  if (u < u_end) {
+    int hi = a.n;
+    while (hi - i > 1) {
+      const int mid = (i + hi) / 2;
+      if (before_s[mid] <= u) i = mid; else hi = mid;
     }
-    float top = x;
-    for (int o = 32; o > 0; o >>= 1) top = fmaxf(top, __shfl_xor(top, o));
-    const float m2 = fmaxf(m, top);
-    const float shift = m2 == -INFINITY ? 0.f : m2;
-    const float keep = expf(m - shift), p = vis ? expf(x - shift) : 0.f;
-    float sum = p;
-    for (int o = 32; o > 0; o >>= 1) sum += __shfl_xor(sum, o);
-    l = l * keep + sum;
-    m = m2;
-    for (int i = 0; i < D / 64; ++i) acc[i] *= keep;
-    p_s[lane] = p;
-    uint64_t mask = __ballot(vis);
-    __syncthreads();
-    for (; mask != 0; mask &= mask - 1) {
-      const int j = __ffsll((unsigned long long)mask) - 1, kk = k0 + j, slot = kk & (a.P - 1);
-      int page = row[kk >> a.log_p];
-      page = page < 0 ? 0 : (page >= a.n_pages ? a.n_pages - 1 : page);
-      const E* vp = reinterpret_cast<const E*>(a.v) + page * page_elems + (int64_t)g * a.P * D +
-                    (slot >> 3) * D * 8 + (slot & 7);
-      for (int i = 0; i < D / 64; ++i) acc[i] = fmaf(p_s[j], load(vp + (lane + 64 * i) * 8), acc[i]);
-    }
-    __syncthreads();
   }
-  E* o = reinterpret_cast<E*>(a.out) + t * a.ldo + h * D;
-  for (int i = 0; i < D / 64; ++i) store(o + lane + 64 * i, l == 0.f ? 0.f : acc[i] / l);
+  const float c = a.scale * 1.44269504088896340736f;
+  const int64_t head_bytes = (int64_t)a.P * D * ES, page_bytes = head_bytes * a.Hkv;
+  // This lane's place in a half step of 16 keys, of the x-th key tile.
+  const int k_lane = (8 * ((n16 >> 2) & 1) + (n16 & 3)) * D * ES + 16 * g;
+  const int v_lane = ((g & 1) * D + n16) * 8 * ES;
+
+  while (u < u_end) {
+    i = __builtin_amdgcn_readfirstlane(i);
+    while (before_s[i + 1] <= u) ++i;
+    const Request r = request(a, i);
+    const int tiles = (r.total + kTile - 1) / kTile, R = r.T * a.G, blocks = (R + RB - 1) / RB;
+    const int64_t in = u - before_s[i];
+    const int job = __builtin_amdgcn_readfirstlane((int)(in / tiles));
+    const int t0 = __builtin_amdgcn_readfirstlane((int)(in - (int64_t)job * tiles));
+    const int t1 = (int)min((int64_t)tiles, t0 + (u_end - u));
+    const int hk = job / blocks, row0 = (job % blocks) * RB;
+    const bool tail = t1 * kTile > r.len;
+    if (tail) ancestors(a.parent + r.first, r.T, mask_s, jump_s, dead_s);
+
+    int tok[NT];
+    frag q[KC][NT];
+#pragma unroll
+    for (int nt = 0; nt < NT; ++nt) {
+      const int row = min(row0 + 16 * nt + n16, R - 1);
+      tok[nt] = row / a.G;
+      const char* p = a.q + ((int64_t)(r.first + tok[nt]) * a.ldq + (hk * a.G + row % a.G) * D) * ES + 16 * g;
+#pragma unroll
+      for (int x = 0; x < KC; ++x) q[x][nt] = *reinterpret_cast<const frag*>(p + 64 * x);
+    }
+
+    f32x4 O[MT][NT];
+    float shift[NT], limit[NT], l[NT];
+#pragma unroll
+    for (int nt = 0; nt < NT; ++nt) {
+      shift[nt] = 0.f;
+      limit[nt] = -INFINITY;
+      l[nt] = 0.f;
+#pragma unroll
+      for (int mt = 0; mt < MT; ++mt) O[mt][nt] = f32x4{};
+    }
+    frag K[2][KC], V[MT][VC];
+    const char* const kb = a.k + hk * head_bytes + k_lane;
+    const char* const vb = a.v + hk * head_bytes + v_lane;
+    // Where the two half steps of 16 keys of tile t lie in the pools.
+    const auto place = [&](int t, int64_t(&at)[2]) {
+      const int key = t * kTile + 32 * w;
+#pragma unroll
+      for (int x = 0; x < 2; ++x) {
+        const int slot = key + 16 * x;
+        int page = constant(r.row, min(slot >> a.log_p, a.max_pages - 1));
+        page = min(max(page, 0), a.n_pages - 1);
+        at[x] = page * page_bytes + (int64_t)(slot & (a.P - 1)) * (D * ES);
+      }
+    };
+    const auto load_k = [&](const int64_t(&at)[2]) {
+      const char* p = kb + (n16 >> 3 ? at[1] : at[0]);
+#pragma unroll
+      for (int x = 0; x < 2; ++x)
+#pragma unroll
+        for (int y = 0; y < KC; ++y) K[x][y] = *reinterpret_cast<const frag*>(p + 4 * x * D * ES + 64 * y);
+    };
+    const auto load_v = [&](const int64_t(&at)[2]) {
+      const char* p = vb + (g >> 1 ? at[1] : at[0]);
+#pragma unroll
+      for (int mt = 0; mt < MT; ++mt)
+#pragma unroll
+        for (int y = 0; y < VC; ++y) V[mt][y] = *reinterpret_cast<const frag*>(p + (16 * mt * 8) * ES + 16 * y);
+    };
+
+    int64_t now[2];
+    place(t0, now);
+    load_k(now);
+    load_v(now);
+    for (int t = t0; t < t1; ++t) {
+      const int key0 = t * kTile + 32 * w;
+      const bool more = t + 1 < t1;
+      int64_t next[2];
+      if (more) place(t + 1, next);
+      f32x4 S[2][NT];
+#pragma unroll
+      for (int x = 0; x < 2; ++x)
+#pragma unroll
+        for (int nt = 0; nt < NT; ++nt) {
+          S[x][nt] = f32x4{};
+#pragma unroll
+          for (int y = 0; y < KC; ++y) S[x][nt] = mma(K[x][y], q[y][nt], S[x][nt]);
+        }
+      if (more) load_k(next);
+      const bool masked = key0 + 32 > r.len;
+      if (masked) {
+#pragma unroll
+        for (int nt = 0; nt < NT; ++nt) {
+          const uint32_t seen = seen8(mask_s + tok[nt] * kMaskRow, key0 + 8 * g - r.len);
+#pragma unroll
+          for (int x = 0; x < 2; ++x)
+#pragma unroll
+            for (int e = 0; e < 4; ++e)
+              if (!(seen >> (4 * x + e) & 1) || key0 + 8 * g + 4 * x + e >= r.total) S[x][nt][e] = -INFINITY;
+        }
+      }
+      float m[NT];
+      bool over = false;
+#pragma unroll
+      for (int nt = 0; nt < NT; ++nt) {
+        const f32x4 s = S[0][nt], y = S[1][nt];
+        m[nt] = fmaxf(max3(max3(s[0], s[1], s[2]), s[3], y[0]), max3(y[1], y[2], y[3])) * c;
+        over |= m[nt] > limit[nt];
+      }
+      if (__any(over)) {
+#pragma unroll
+        for (int nt = 0; nt < NT; ++nt) {
+          const float top = max_groups(m[nt]);
+          const bool moves = top > limit[nt], fresh = limit[nt] == -INFINITY;
+          const float f = moves && !fresh ? exp2_fast(shift[nt] - top) : 1.f;
+          shift[nt] = moves ? top : shift[nt];
+          limit[nt] = moves ? top + kLag : limit[nt];
+          l[nt] *= f;
+#pragma unroll
+          for (int mt = 0; mt < MT; ++mt) O[mt][nt] *= f;
+        }
+      }
+      float p[NT][8];
+      frag P[NT][VC];
+#pragma unroll
+      for (int nt = 0; nt < NT; ++nt) {
+#pragma unroll
+        for (int e = 0; e < 8; ++e) {
+          p[nt][e] = exp2_fast(fmaf(S[e >> 2][nt][e & 3], c, -shift[nt]));
+          l[nt] += p[nt][e];
+        }
+        if constexpr (kF32) {
+#pragma unroll
+          for (int y = 0; y < 2; ++y)
+#pragma unroll
+            for (int e = 0; e < 4; ++e) P[nt][y][e] = p[nt][4 * y + e];
+        } else {
+          P[nt][0] = pack8(p[nt]);
+        }
+      }
+      if (masked) {
+        // A weight of zero does not hide an infinity or NaN: such values count
+        // as zero, and where a weight meets one the row's sum becomes NaN.
+#pragma unroll
+        for (int mt = 0; mt < MT; ++mt) {
+          bool bad = false;
+#pragma unroll
+          for (int y = 0; y < VC; ++y) bad |= any_nonfinite(V[mt][y]);
+          if (__any(bad)) {
+#pragma unroll
+            for (int nt = 0; nt < NT; ++nt) {
+              f32x4 met = {};
+#pragma unroll
+              for (int y = 0; y < VC; ++y) met = mma(nonfinite_ones(V[mt][y]), P[nt][y], met);
+#pragma unroll
+              for (int e = 0; e < 4; ++e) O[mt][nt][e] = met[e] != 0.f ? NAN : O[mt][nt][e];
+            }
+#pragma unroll
+            for (int y = 0; y < VC; ++y) V[mt][y] = finite_only(V[mt][y]);
+          }
+        }
+      }
+#pragma unroll
+      for (int mt = 0; mt < MT; ++mt)
+#pragma unroll
+        for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+          for (int y = 0; y < VC; ++y) O[mt][nt] = mma(V[mt][y], P[nt][y], O[mt][nt]);
+      if (more) load_v(next);
+    }
+
+    // The four waves' sums, by the largest maximum.
+#pragma unroll
+    for (int nt = 0; nt < NT; ++nt) {
+      l[nt] = sum_groups(l[nt]);
+      if (g == 0) {
+        m_s[w][16 * nt + n16] = limit[nt] == -INFINITY ? -INFINITY : shift[nt];
+        l_s[w][16 * nt + n16] = l[nt];
+      }
+    }
+    __syncthreads();
+    const bool whole = t0 == 0 && t1 == tiles;
+    const int slot = u == u_first ? 0 : 1;
+    float* const part = parts + (2 * (size_t)blockIdx.x + slot) * Plan::kPartFloats;
+    const int orow = tid >> 4, od = (tid & 15) * (D / 16);
+#pragma unroll
+    for (int nt = 0; nt < NT; ++nt) {
+      if (row0 + 16 * nt >= R) break;
+      float top = -INFINITY;
+#pragma unroll
+      for (int x = 0; x < 4; ++x) top = fmaxf(top, m_s[x][16 * nt + n16]);
+      const float own = m_s[w][16 * nt + n16];
+      const float f = own == -INFINITY ? 0.f : exp2_fast(own - top);
+#pragma unroll
+      for (int mt = 0; mt < MT; ++mt)
+        *reinterpret_cast<f32x4*>(&sum_s[w][n16][16 * mt + 4 * g]) = O[mt][nt] * f;
+      __syncthreads();
+      const int row = row0 + 16 * nt + orow;
+      if (row < R) {
+        float om = -INFINITY, sum = 0.f;
+#pragma unroll
+        for (int x = 0; x < 4; ++x) om = fmaxf(om, m_s[x][16 * nt + orow]);
+#pragma unroll
+        for (int x = 0; x < 4; ++x) {
+          const float mx = m_s[x][16 * nt + orow];
+          sum += l_s[x][16 * nt + orow] * (mx == -INFINITY ? 0.f : exp2_fast(mx - om));
+        }
+        const bool dead = tail && dead_s[row / a.G];
+        float o[D / 16];
+#pragma unroll
+        for (int y = 0; y < D / 64; ++y) {
+          f32x4 v = *reinterpret_cast<const f32x4*>(&sum_s[0][orow][od + 4 * y]);
+#pragma unroll
+          for (int x = 1; x < 4; ++x) v += *reinterpret_cast<const f32x4*>(&sum_s[x][orow][od + 4 * y]);
+#pragma unroll
+          for (int e = 0; e < 4; ++e) o[4 * y + e] = v[e];
+        }
+        if (whole) {
+          write_row<E, D>(a, r.first, hk, row, od, o, dead || sum == 0.f ? 0.f : 1.f / sum);
+        } else {
+          float* to = part + (16 * nt + orow) * (D + 2);
+#pragma unroll
+          for (int y = 0; y < D / 16; y += 2) *reinterpret_cast<f32x2*>(to + od + y) = f32x2{o[y], o[y + 1]};
+          if ((tid & 15) == 0) *reinterpret_cast<f32x2*>(to + D) = f32x2{om, dead ? -1.f : sum};
+        }
+      }
+      __syncthreads();
+    }
+    if (t0 == 0 && !whole) {
+      const int64_t end = u + tiles;  // of the row block
+      split_parts = (int)((end - 1) / share) - (int)blockIdx.x + 1;
+      if (tid == 0)
+        splits[blockIdx.x] = Split{split_parts, slot, r.first, hk, row0, min(RB, R - row0)};
+    }
+    u += t1 - t0;
+  }
+  if (split_parts == 0 && tid == 0) splits[blockIdx.x].parts = 0;
+}
+
+// Adds the parts of the row block that starts in workgroup blockIdx.x's stretch
+// and ends in a later one's; blockIdx.y four rows, a wave every fourth part.
+template <typename E, int D, int NT>
+__global__ __launch_bounds__(256) void tree_join_kernel(TreeArgs a) {
+  typedef TreePlan<E, D, NT> Plan;
+  __shared__ float m_s[4][4], l_s[4][4], o_s[4][4][D];
+  const Split sp = reinterpret_cast<const Split*>(a.ws + (size_t)Plan::kGroups * 2 * Plan::kPartFloats)[blockIdx.x];
+  const int row4 = blockIdx.y * 4;
+  if (sp.parts == 0 || row4 >= sp.rows) return;
+  const int tid = threadIdx.x, w = wave_id(), lr = (tid & 63) >> 4, od = (tid & 15) * (D / 16);
+  const int row = min(row4 + lr, sp.rows - 1);
+  float m = -INFINITY, l = 0.f, o[D / 16];
+  bool dead = false;  // a sum of -1 marks a node that sees nothing
+#pragma unroll
+  for (int y = 0; y < D / 16; ++y) o[y] = 0.f;
+#pragma unroll 2
+  for (int p = w; p < sp.parts; p += 4) {
+    const size_t slot = 2 * (size_t)(blockIdx.x + p) + (p == 0 ? sp.slot : 0);
+    const float* from = a.ws + slot * Plan::kPartFloats + row * (D + 2);
+    const f32x2 ml = *reinterpret_cast<const f32x2*>(from + D);
+    dead |= ml[1] == -1.f;
+    const float top = fmaxf(m, ml[0]);
+    const float f = m == top ? 1.f : exp2_fast(m - top), h = ml[0] == top ? 1.f : exp2_fast(ml[0] - top);
+    m = top;
+    l = l * f + ml[1] * h;
+#pragma unroll
+    for (int y = 0; y < D / 16; y += 2) {
+      const f32x2 v = *reinterpret_cast<const f32x2*>(from + od + y);
+      o[y] = o[y] * f + v[0] * h;
+      o[y + 1] = o[y + 1] * f + v[1] * h;
+    }
+  }
+  if ((tid & 15) == 0) {
+    m_s[w][lr] = m;
+    l_s[w][lr] = dead ? -1.f : l;
+  }
+#pragma unroll
+  for (int y = 0; y < D / 16; ++y) o_s[w][lr][od + y] = o[y];
+  __syncthreads();
+  if (w != 0 || row4 + lr >= sp.rows) return;
+  float top = -INFINITY, sum = 0.f, f[4];
+#pragma unroll
+  for (int x = 0; x < 4; ++x) top = fmaxf(top, m_s[x][lr]);
+#pragma unroll
+  for (int x = 0; x < 4; ++x) {
+    f[x] = m_s[x][lr] == top ? 1.f : exp2_fast(m_s[x][lr] - top);
+    dead |= l_s[x][lr] == -1.f;
+    sum += l_s[x][lr] * f[x];
+  }
+#pragma unroll
+  for (int y = 0; y < D / 16; ++y) {
+    o[y] = 0.f;
+#pragma unroll
+    for (int x = 0; x < 4; ++x) o[y] += o_s[x][lr][od + y] * f[x];
+  }
+  write_row<E, D>(a, sp.first, sp.head, sp.row0 + row, od, o, dead || sum == 0.f ? 0.f : 1.f / sum);
+}
+
+template <typename E, int D, int NT>
+hipError_t launch(const TreeArgs& a, hipStream_t s) {
+  typedef TreePlan<E, D, NT> Plan;
+  tree_kernel<E, D, NT><<<Plan::kGroups, 256, 0, s>>>(a);
+  const hipError_t err = hipGetLastError();
+  if (err != hipSuccess) return err;
+  tree_join_kernel<E, D, NT><<<dim3(Plan::kGroups, Plan::kRows / 4), 256, 0, s>>>(a);
+  return hipGetLastError();
+}
+
+template <int X>
+struct Const {
+  static constexpr int value = X;
+};
+
+// The kernel by type, head size and rows: 16 rows a workgroup while the largest
+// tree has no more, then 32, then 64 (fp32: 32) in several row blocks.
+template <typename F>
+auto tree_choice(int G, int D, bool f32, int max_nodes, F f) {
+  const int64_t rows = (int64_t)G * max_nodes;
+  const auto by_rows = [&](auto e, auto d) {
+    if (rows <= 16) return f(e, d, Const<1>{});
+    if constexpr (sizeof(e) == 4) {
+      return f(e, d, Const<2>{});
+    } else {
+      return rows <= 32 ? f(e, d, Const<2>{}) : f(e, d, Const<4>{});
+    }
+  };
+  if (f32) return D == 64 ? by_rows(float{}, Const<64>{}) : by_rows(float{}, Const<128>{});
+  return D == 64 ? by_rows(uint16_t{}, Const<64>{}) : by_rows(uint16_t{}, Const<128>{});
 }
 
 }  // namespace
 
-size_t tree_attention_workspace(int, int, int, bool, int, int) { return 256; }
+size_t tree_attention_workspace(int Hq, int Hkv, int D, bool f32, int, int max_nodes) {
+  return tree_choice(Hq / Hkv, D, f32, max_nodes, [](auto e, auto d, auto nt) {
+    return TreePlan<decltype(e), decltype(d)::value, decltype(nt)::value>::kBytes;
+  });
+}
 
 hipError_t launch_tree_attention(const TreeArgs& a, hipStream_t s) {
-  const dim3 grid(a.n_tokens, a.Hq);
-  if (a.f32) {
-    if (a.D == 64) tree_kernel<float, 64><<<grid, 64, 0, s>>>(a);
-    else tree_kernel<float, 128><<<grid, 64, 0, s>>>(a);
-  } else {
-    if (a.D == 64) tree_kernel<uint16_t, 64><<<grid, 64, 0, s>>>(a);
-    else tree_kernel<uint16_t, 128><<<grid, 64, 0, s>>>(a);
-  }
-  return hipGetLastError();
+  return tree_choice(a.G, a.D, a.f32, a.max_nodes, [&](auto e, auto d, auto nt) {
+    return launch<decltype(e), decltype(d)::value, decltype(nt)::value>(a, s);
+  });
 }
 
 }  // namespace s2moe
