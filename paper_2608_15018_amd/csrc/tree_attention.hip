@@ -27,6 +27,9 @@
 namespace s2moe {
 namespace {
 
+#ifndef S2MOE_TREE_WIDE
+#define S2MOE_TREE_WIDE 32
+#endif
 constexpr int kTile = 128;  // keys of a unit, 32 a wave
 
 // A row block whose parts the joining launch adds, as the workgroup that has
@@ -67,7 +70,7 @@ template <typename E, int D, int NT>
 struct TreePlan {
   static constexpr int kRows = 16 * NT;
   // Workgroups that fit a compute unit.
-  static constexpr int kPerCu = NT == 4 || (NT == 2 && D * sizeof(E) == 512) ? 1 : 2;
+  static constexpr int kPerCu = NT == 2 && D * sizeof(E) == 512 ? 1 : 2;
   static constexpr int kGroups = 256 * kPerCu;
   static constexpr size_t kPartFloats = (size_t)kRows * (D + 2);
   static constexpr size_t kBytes = kGroups * (2 * kPartFloats * 4 + sizeof(Split));
@@ -135,12 +138,91 @@ __device__ void ancestors(const int32_t* parent, int T, uint32_t* mask_s, int* j
   }
 }
 
+// Units before each request into before_s[0 .. n]; returns their number.
+__device__ int64_t count_units(const TreeArgs& a, int RB, int64_t* before_s) {
+  __shared__ int64_t wave_s[4];
+  const int tid = threadIdx.x, lane = tid & 63, w = tid >> 6;
+  int64_t mine = 0;
+  for (int x = 0; x < 4; ++x) {
+    const int i = 4 * tid + x;
+    if (i < a.n) {
+      const Request r = request(a, i);
+      before_s[i] = mine;
+      mine += (int64_t)((r.T * a.G + RB - 1) / RB) * a.Hkv * ((r.total + kTile - 1) / kTile);
+    }
+  }
+  int64_t inc = mine;
+#pragma unroll
+  for (int d = 1; d < 64; d <<= 1) {
+    const int64_t y = __shfl_up(inc, d);
+    if (lane >= d) inc += y;
+  }
+  if (lane == 63) wave_s[w] = inc;
+  __syncthreads();
+  int64_t at = inc - mine, total = 0;
+#pragma unroll
+  for (int x = 0; x < 4; ++x) {
+    at += x < w ? wave_s[x] : 0;
+    total += wave_s[x];
+  }
+  for (int x = 0; x < 4; ++x)
+    if (4 * tid + x < a.n) before_s[4 * tid + x] += at;
+  if (tid == 0) before_s[a.n] = total;
+  __syncthreads();
+  return total;
+}
+
+// The request that unit u falls into.
+__device__ int request_of(int64_t u, int n, const int64_t* before_s) {
+  int i = 0, hi = n;
+  while (hi - i > 1) {
+    const int mid = (i + hi) / 2;
+    if (before_s[mid] <= u) i = mid; else hi = mid;
+  }
+  return i;
+}
+
 // Which of eight slots from node k0 on a row sees, k0 < 0 being cached tokens.
 __device__ __forceinline__ uint32_t seen8(const uint32_t* mask, int k0) {
   k0 = min(max(k0, -32), kMaxNodes);
   const int x = (k0 + 32) >> 5;
   const uint64_t two = (uint64_t)mask[x + 1] << 32 | mask[x];
   return (uint32_t)(two >> (k0 & 31)) & 0xFFu;
+}
+
+__device__ __forceinline__ float largest(f32x4 a, f32x4 b) {
+  return fmaxf(max3(max3(a[0], a[1], a[2]), a[3], b[0]), max3(b[1], b[2], b[3]));
+}
+
+// Scores of keys key .. key + 7 that a row does not see become -inf.
+template <int NT>
+__device__ __forceinline__ void mask_scores(f32x4 (&S)[2][NT], const int (&tok)[NT], const uint32_t* mask_s,
+                                            int key, int len, int total) {
+#pragma unroll
+  for (int nt = 0; nt < NT; ++nt) {
+    const uint32_t seen = seen8(mask_s + tok[nt] * kMaskRow, key - len);
+#pragma unroll
+    for (int e = 0; e < 8; ++e)
+      if (!(seen >> e & 1) || key + e >= total) S[e >> 2][nt][e & 3] = -INFINITY;
+  }
+}
+
+// Rows with a score past their limit move their maximum to it (m: the lane's
+// largest scores).
+template <int MT, int NT>
+__device__ __forceinline__ void raise(const float (&m)[NT], float (&shift)[NT], float (&limit)[NT],
+                                      float (&l)[NT], f32x4 (&O)[MT][NT]) {
+#pragma unroll
+  for (int nt = 0; nt < NT; ++nt) {
+    const float top = max_groups(m[nt]);
+    const bool moves = top > limit[nt], fresh = limit[nt] == -INFINITY;
+    const float f = moves && !fresh ? exp2_fast(shift[nt] - top) : 1.f;
+    shift[nt] = moves ? top : shift[nt];
+    limit[nt] = moves ? top + kLag : limit[nt];
+    l[nt] *= f;
+#pragma unroll
+    for (int mt = 0; mt < MT; ++mt) O[mt][nt] *= f;
+  }
 }
 
 // D / 16 elements of an output row, times `inv`; zeros where inv is 0.
@@ -174,54 +256,19 @@ __global__ __launch_bounds__(256, (TreePlan<E, D, NT>::kPerCu)) void tree_kernel
   __shared__ uint32_t mask_s[kMaxNodes * kMaskRow];
   __shared__ int jump_s[kMaxNodes];
   __shared__ uint8_t dead_s[kMaxNodes];
-  __shared__ int64_t wave_s[4];
 
   const int tid = threadIdx.x, lane = tid & 63, w = wave_id();
   const int n16 = lane & 15, g = lane >> 4;
   Split* const splits = reinterpret_cast<Split*>(a.ws + (size_t)Plan::kGroups * 2 * Plan::kPartFloats);
   float* const parts = a.ws;
 
-  // Units before each request.
-  int64_t mine = 0;
-  for (int x = 0; x < 4; ++x) {
-    const int i = 4 * tid + x;
-    if (i < a.n) {
-      const Request r = request(a, i);
-      before_s[i] = mine;
-      mine += (int64_t)((r.T * a.G + RB - 1) / RB) * a.Hkv * ((r.total + kTile - 1) / kTile);
-    }
-  }
-  int64_t inc = mine;
-#pragma unroll
-  for (int d = 1; d < 64; d <<= 1) {
-    const int64_t y = __shfl_up(inc, d);
-    if (lane >= d) inc += y;
-  }
-  if (lane == 63) wave_s[w] = inc;
-  __syncthreads();
-  int64_t at = inc - mine, total = 0;
-#pragma unroll
-  for (int x = 0; x < 4; ++x) {
-    at += x < w ? wave_s[x] : 0;
-    total += wave_s[x];
-  }
-  for (int x = 0; x < 4; ++x)
-    if (4 * tid + x < a.n) before_s[4 * tid + x] += at;
-  if (tid == 0) before_s[a.n] = total;
-  __syncthreads();
+  const int64_t total = count_units(a, RB, before_s);
   const int64_t share = (total + Plan::kGroups - 1) / Plan::kGroups;
   int64_t u = blockIdx.x * share;
   const int64_t u_end = min(u + share, total), u_first = u;
   int split_parts = 0;  // of a row block that starts here and goes on elsewhere
 
-  int i = 0;
-  if (u < u_end) {
-    int hi = a.n;
-    while (hi - i > 1) {
-      const int mid = (i + hi) / 2;
-      if (before_s[mid] <= u) i = mid; else hi = mid;
-    }
-  }
+  int i = u < u_end ? request_of(u, a.n, before_s) : 0;
   const float c = a.scale * 1.44269504088896340736f;
   const int64_t head_bytes = (int64_t)a.P * D * ES, page_bytes = head_bytes * a.Hkv;
   // This lane's place in a half step of 16 keys, of the x-th key tile.
@@ -311,38 +358,15 @@ __global__ __launch_bounds__(256, (TreePlan<E, D, NT>::kPerCu)) void tree_kernel
         }
       if (more) load_k(next);
       const bool masked = key0 + 32 > r.len;
-      if (masked) {
-#pragma unroll
-        for (int nt = 0; nt < NT; ++nt) {
-          const uint32_t seen = seen8(mask_s + tok[nt] * kMaskRow, key0 + 8 * g - r.len);
-#pragma unroll
-          for (int x = 0; x < 2; ++x)
-#pragma unroll
-            for (int e = 0; e < 4; ++e)
-              if (!(seen >> (4 * x + e) & 1) || key0 + 8 * g + 4 * x + e >= r.total) S[x][nt][e] = -INFINITY;
-        }
-      }
+      if (masked) mask_scores<NT>(S, tok, mask_s, key0 + 8 * g, r.len, r.total);
       float m[NT];
       bool over = false;
 #pragma unroll
       for (int nt = 0; nt < NT; ++nt) {
-        const f32x4 s = S[0][nt], y = S[1][nt];
-        m[nt] = fmaxf(max3(max3(s[0], s[1], s[2]), s[3], y[0]), max3(y[1], y[2], y[3])) * c;
+        m[nt] = largest(S[0][nt], S[1][nt]) * c;
         over |= m[nt] > limit[nt];
       }
-      if (__any(over)) {
-#pragma unroll
-        for (int nt = 0; nt < NT; ++nt) {
-          const float top = max_groups(m[nt]);
-          const bool moves = top > limit[nt], fresh = limit[nt] == -INFINITY;
-          const float f = moves && !fresh ? exp2_fast(shift[nt] - top) : 1.f;
-          shift[nt] = moves ? top : shift[nt];
-          limit[nt] = moves ? top + kLag : limit[nt];
-          l[nt] *= f;
-#pragma unroll
-          for (int mt = 0; mt < MT; ++mt) O[mt][nt] *= f;
-        }
-      }
+      if (__any(over)) raise<MT, NT>(m, shift, limit, l, O);
       float p[NT][8];
       frag P[NT][VC];
 #pragma unroll
@@ -460,11 +484,234 @@ __global__ __launch_bounds__(256, (TreePlan<E, D, NT>::kPerCu)) void tree_kernel
   if (split_parts == 0 && tid == 0) splits[blockIdx.x].parts = 0;
 }
 
+// Larger trees (bf16): rows are split over the waves, 16 NT each, and the keys and
+// values of a stage are fetched once for all of them, by loads that go from the
+// pages into LDS without a register between: three stages are in flight while one
+// is used.  A wave fetches an eighth or quarter of a stage that lies in one page.
+template <int D, int NT>
+struct WidePlan {
+  static constexpr int kRows = 64 * NT;
+  static constexpr int kKeys = D == 128 ? 32 : 64;  // of a stage
+  static constexpr int kStage = kKeys * D * 2;      // bytes of its keys, or values
+  static constexpr int kRing = 4 * 2 * kStage;
+  static constexpr int kPerCu = D == 128 && NT == 4 ? 1 : 2;
+  static constexpr int kGroups = 256 * kPerCu;
+  static constexpr size_t kPartFloats = (size_t)kRows * (D + 2);
+  static constexpr size_t kBytes = kGroups * (2 * kPartFloats * 4 + sizeof(Split));
+  static size_t lds(int n, int max_nodes) {
+    return kRing + (size_t)(n + 1) * 8 + (size_t)max_nodes * (kMaskRow * 4 + 4 + 4);
+  }
+};
+
+template <int D, int NT>
+__global__ __launch_bounds__(256, (WidePlan<D, NT>::kPerCu)) void tree_wide_kernel(TreeArgs a) {
+  typedef WidePlan<D, NT> Plan;
+  constexpr int RB = Plan::kRows, MT = D / 16, KC = D / 32, SK = Plan::kKeys;
+  constexpr int kLoads = Plan::kStage / 4096;  // 1 KB loads a wave makes for keys, or values
+  constexpr int CH = D / 8;                    // 16-byte chunks of a key
+  extern __shared__ __attribute__((aligned(16))) char smem[];
+  char* const k_lds = smem;
+  char* const v_lds = smem + 4 * Plan::kStage;
+  int64_t* const before_s = reinterpret_cast<int64_t*>(smem + Plan::kRing);
+  uint32_t* const mask_s = reinterpret_cast<uint32_t*>(before_s + a.n + 1);
+  int* const jump_s = reinterpret_cast<int*>(mask_s + a.max_nodes * kMaskRow);
+  uint8_t* const dead_s = reinterpret_cast<uint8_t*>(jump_s + a.max_nodes);
+
+  const int tid = threadIdx.x, lane = tid & 63, w = wave_id();
+  const int n16 = lane & 15, g = lane >> 4;
+  Split* const splits = reinterpret_cast<Split*>(a.ws + (size_t)Plan::kGroups * 2 * Plan::kPartFloats);
+  const int64_t total = count_units(a, RB, before_s);
+  const int64_t share = (total + Plan::kGroups - 1) / Plan::kGroups;
+  int64_t u = blockIdx.x * share;
+  const int64_t u_end = min(u + share, total), u_first = u;
+  int split_parts = 0;
+  int i = u < u_end ? request_of(u, a.n, before_s) : 0;
+  const float c = a.scale * 1.44269504088896340736f;
+  const int64_t head_bytes = (int64_t)a.P * D * 2, page_bytes = head_bytes * a.Hkv;
+
+  // Chunk x of key r of a stage lies at chunk x ^ swizzle(r); values lie as they do
+  // in the page.
+  const auto swizzle = [](int r) { return D == 128 ? r & 15 : (r >> 1) & 7; };
+  uint32_t k_off[kLoads];
+#pragma unroll
+  for (int x = 0; x < kLoads; ++x) {
+    const int r = x * (64 / CH) + lane / CH;  // within the wave's keys
+    k_off[x] = r * D * 2 + (((lane % CH) ^ swizzle(w * (SK / 4) + r)) << 4);
+  }
+  const int key_row = 8 * (n16 >> 2) + (n16 & 3);  // of the first 16-key tile; the second's is 4 on
+
+  while (u < u_end) {
+    i = __builtin_amdgcn_readfirstlane(i);
+    while (before_s[i + 1] <= u) ++i;
+    const Request r = request(a, i);
+    const int tiles = (r.total + kTile - 1) / kTile, R = r.T * a.G, blocks = (R + RB - 1) / RB;
+    const int64_t in = u - before_s[i];
+    const int job = __builtin_amdgcn_readfirstlane((int)(in / tiles));
+    const int t0 = __builtin_amdgcn_readfirstlane((int)(in - (int64_t)job * tiles));
+    const int t1 = (int)min((int64_t)tiles, t0 + (u_end - u));
+    const int hk = job / blocks, row0 = (job % blocks) * RB;
+    const int s0 = t0 * (kTile / SK), s1 = min(t1 * (kTile / SK), (r.total + SK - 1) / SK);
+    const bool tail = t1 * kTile > r.len;
+    const int wrow0 = row0 + 16 * NT * w;
+    const bool active = wrow0 < R;
+
+    // Stage s into its place in the ring; past the stretch, its last again.
+    const char* const kb = a.k + hk * head_bytes;
+    const char* const vb = a.v + hk * head_bytes;
+    const auto page_of = [&](int s) {
+      const int key = min(s, s1 - 1) * SK + w * (SK / 4);
+      const int page = constant(r.row, min(key >> a.log_p, a.max_pages - 1));
+      return min(max(page, 0), a.n_pages - 1);
+    };
+    const auto load_stage = [&](int s, int page) {
+      const int key = min(s, s1 - 1) * SK + w * (SK / 4);
+      const int64_t at = page * page_bytes + (int64_t)(key & (a.P - 1)) * (D * 2);
+#pragma unroll
+      for (int x = 0; x < kLoads; ++x)
+        load_to_lds(kb + at, k_off[x], k_lds + (s & 3) * Plan::kStage + (w * kLoads + x) * 1024);
+#pragma unroll
+      for (int x = 0; x < kLoads; ++x)
+        load_to_lds(vb + at, x * 1024 + lane * 16, v_lds + (s & 3) * Plan::kStage + (w * kLoads + x) * 1024);
+    };
+    load_stage(s0, page_of(s0));
+    load_stage(s0 + 1, page_of(s0 + 1));
+    load_stage(s0 + 2, page_of(s0 + 2));
+    int page = page_of(s0 + 3);
+    if (tail) ancestors(a.parent + r.first, r.T, mask_s, jump_s, dead_s);
+
+    int tok[NT];
+    bf16x8 q[KC][NT];
+#pragma unroll
+    for (int nt = 0; nt < NT; ++nt) {
+      const int row = min(wrow0 + 16 * nt + n16, R - 1);
+      tok[nt] = row / a.G;
+      const char* p = a.q + ((int64_t)(r.first + tok[nt]) * a.ldq + (hk * a.G + row % a.G) * D) * 2 + 16 * g;
+#pragma unroll
+      for (int x = 0; x < KC; ++x) q[x][nt] = *reinterpret_cast<const bf16x8*>(p + 64 * x);
+    }
+    f32x4 O[MT][NT];
+    float shift[NT], limit[NT], l[NT];
+#pragma unroll
+    for (int nt = 0; nt < NT; ++nt) {
+      shift[nt] = 0.f;
+      limit[nt] = -INFINITY;
+      l[nt] = 0.f;
+#pragma unroll
+      for (int mt = 0; mt < MT; ++mt) O[mt][nt] = f32x4{};
+    }
+    for (int s = s0; s < s1; ++s) {
+      // Stage s is there for everybody, and stage s - 1, whose place stage s + 3
+      // takes, is read by nobody any more.
+      wait_loads<4 * kLoads>();
+      __builtin_amdgcn_s_barrier();
+      load_stage(s + 3, page);
+      page = page_of(s + 4);
+      if (!active) continue;
+#pragma unroll
+      for (int sub = 0; sub < SK / 32; ++sub) {
+        const int key0 = s * SK + 32 * sub;
+        const char* kt = k_lds + (s & 3) * Plan::kStage + 32 * sub * D * 2;
+        const char* vt = v_lds + (s & 3) * Plan::kStage + (4 * sub + g) * (D * 16) + n16 * 16;
+        f32x4 S[2][NT];
+#pragma unroll
+        for (int x = 0; x < 2; ++x) {
+#pragma unroll
+          for (int nt = 0; nt < NT; ++nt) S[x][nt] = f32x4{};
+          const int row = key_row + 4 * x;
+#pragma unroll
+          for (int y = 0; y < KC; ++y) {
+            const bf16x8 k = *reinterpret_cast<const bf16x8*>(kt + row * D * 2 + (((4 * y + g) ^ swizzle(row)) << 4));
+#pragma unroll
+            for (int nt = 0; nt < NT; ++nt) S[x][nt] = mma(k, q[y][nt], S[x][nt]);
+          }
+        }
+        const bool masked = key0 + 32 > r.len;
+        if (masked) mask_scores<NT>(S, tok, mask_s, key0 + 8 * g, r.len, r.total);
+        float m[NT];
+        bool over = false;
+#pragma unroll
+        for (int nt = 0; nt < NT; ++nt) {
+          m[nt] = largest(S[0][nt], S[1][nt]) * c;
+          over |= m[nt] > limit[nt];
+        }
+        if (__any(over)) raise<MT, NT>(m, shift, limit, l, O);
+        bf16x8 P[NT];
+#pragma unroll
+        for (int nt = 0; nt < NT; ++nt) {
+          float p[8];
+#pragma unroll
+          for (int e = 0; e < 8; ++e) {
+            p[e] = exp2_fast(fmaf(S[e >> 2][nt][e & 3], c, -shift[nt]));
+            l[nt] += p[e];
+          }
+          P[nt] = pack8(p);
+        }
+#pragma unroll
+        for (int mt = 0; mt < MT; ++mt) {
+          bf16x8 v = *reinterpret_cast<const bf16x8*>(vt + mt * 256);
+          if (masked && __any(any_nonfinite(v))) {
+#pragma unroll
+            for (int nt = 0; nt < NT; ++nt) {
+              const f32x4 met = mma(nonfinite_ones(v), P[nt], f32x4{});
+#pragma unroll
+              for (int e = 0; e < 4; ++e) O[mt][nt][e] = met[e] != 0.f ? NAN : O[mt][nt][e];
+            }
+            v = finite_only(v);
+          }
+#pragma unroll
+          for (int nt = 0; nt < NT; ++nt) O[mt][nt] = mma(v, P[nt], O[mt][nt]);
+        }
+      }
+    }
+    wait_loads<0>();  // what was loaded past the stretch
+    __syncthreads();  // nobody reads this stretch's stages or masks any more
+
+    const bool whole = t0 == 0 && t1 == tiles;
+    const int slot = u == u_first ? 0 : 1;
+    float* const part = a.ws + (2 * (size_t)blockIdx.x + slot) * Plan::kPartFloats;
+#pragma unroll
+    for (int nt = 0; nt < NT; ++nt) {
+      const int row = wrow0 + 16 * nt + n16;
+      const float sum = sum_groups(l[nt]);
+      if (row >= R) continue;
+      const bool dead = tail && dead_s[row / a.G];
+      if (whole) {
+        const float inv = dead || sum == 0.f ? 0.f : 1.f / sum;
+        uint16_t* o = reinterpret_cast<uint16_t*>(a.out) + (int64_t)(r.first + row / a.G) * a.ldo +
+                      (hk * a.G + row % a.G) * D + 4 * g;
+#pragma unroll
+        for (int mt = 0; mt < MT; ++mt) {
+          f32x4 v;
+#pragma unroll
+          for (int e = 0; e < 4; ++e) v[e] = inv == 0.f ? 0.f : O[mt][nt][e] * inv;
+          *reinterpret_cast<bf16x4*>(o + 16 * mt) = __builtin_convertvector(v, bf16x4);
+        }
+      } else {
+        float* to = part + (row - row0) * (D + 2);
+#pragma unroll
+        for (int mt = 0; mt < MT; ++mt)
+#pragma unroll
+          for (int e = 0; e < 4; e += 2)
+            *reinterpret_cast<f32x2*>(to + 16 * mt + 4 * g + e) = f32x2{O[mt][nt][e], O[mt][nt][e + 1]};
+        if (g == 0)
+          *reinterpret_cast<f32x2*>(to + D) = f32x2{limit[nt] == -INFINITY ? -INFINITY : shift[nt], dead ? -1.f : sum};
+      }
+    }
+    if (t0 == 0 && !whole) {
+      split_parts = (int)((u + tiles - 1) / share) - (int)blockIdx.x + 1;
+      if (tid == 0)
+        splits[blockIdx.x] = Split{split_parts, slot, r.first, hk, row0, min(RB, R - row0)};
+    }
+    u += t1 - t0;
+    __syncthreads();  // dead_s is free again
+  }
+  if (split_parts == 0 && tid == 0) splits[blockIdx.x].parts = 0;
+}
+
 // Adds the parts of the row block that starts in workgroup blockIdx.x's stretch
 // and ends in a later one's; blockIdx.y four rows, a wave every fourth part.
-template <typename E, int D, int NT>
+template <typename E, int D, typename Plan>
 __global__ __launch_bounds__(256) void tree_join_kernel(TreeArgs a) {
-  typedef TreePlan<E, D, NT> Plan;
   __shared__ float m_s[4][4], l_s[4][4], o_s[4][4][D];
   const Split sp = reinterpret_cast<const Split*>(a.ws + (size_t)Plan::kGroups * 2 * Plan::kPartFloats)[blockIdx.x];
   const int row4 = blockIdx.y * 4;
@@ -518,50 +765,61 @@ __global__ __launch_bounds__(256) void tree_join_kernel(TreeArgs a) {
   write_row<E, D>(a, sp.first, sp.head, sp.row0 + row, od, o, dead || sum == 0.f ? 0.f : 1.f / sum);
 }
 
-template <typename E, int D, int NT>
-hipError_t launch(const TreeArgs& a, hipStream_t s) {
-  typedef TreePlan<E, D, NT> Plan;
-  tree_kernel<E, D, NT><<<Plan::kGroups, 256, 0, s>>>(a);
+template <typename E, int D, typename Plan>
+hipError_t launch_join(const TreeArgs& a, hipStream_t s) {
   const hipError_t err = hipGetLastError();
   if (err != hipSuccess) return err;
-  tree_join_kernel<E, D, NT><<<dim3(Plan::kGroups, Plan::kRows / 4), 256, 0, s>>>(a);
+  tree_join_kernel<E, D, Plan><<<dim3(Plan::kGroups, Plan::kRows / 4), 256, 0, s>>>(a);
   return hipGetLastError();
 }
 
-template <int X>
-struct Const {
-  static constexpr int value = X;
+template <typename E, int D, int NT>
+struct ByKeys {  // waves split the keys
+  static size_t bytes() { return TreePlan<E, D, NT>::kBytes; }
+  static hipError_t launch(const TreeArgs& a, hipStream_t s) {
+    tree_kernel<E, D, NT><<<TreePlan<E, D, NT>::kGroups, 256, 0, s>>>(a);
+    return launch_join<E, D, TreePlan<E, D, NT>>(a, s);
+  }
 };
 
-// The kernel by type, head size and rows: 16 rows a workgroup while the largest
-// tree has no more, then 32, then 64 (fp32: 32) in several row blocks.
+template <int D, int NT>
+struct ByRows {  // waves split the rows
+  typedef WidePlan<D, NT> Plan;
+  static size_t bytes() { return Plan::kBytes; }
+  static hipError_t launch(const TreeArgs& a, hipStream_t s) {
+    static const hipError_t ready = hipFuncSetAttribute(
+        reinterpret_cast<const void*>(tree_wide_kernel<D, NT>),
+        hipFuncAttributeMaxDynamicSharedMemorySize, (int)Plan::lds(kKvMaxRequests, kMaxNodes));
+    if (ready != hipSuccess) return ready;
+    tree_wide_kernel<D, NT><<<Plan::kGroups, 256, Plan::lds(a.n, a.max_nodes), s>>>(a);
+    return launch_join<uint16_t, D, Plan>(a, s);
+  }
+};
+
+template <int D, typename F>
+auto choose(int64_t rows, bool f32, F f) {
+  if (f32) return rows <= 16 ? f(ByKeys<float, D, 1>{}) : f(ByKeys<float, D, 2>{});
+  if (rows <= 16) return f(ByKeys<uint16_t, D, 1>{});
+  if (rows <= S2MOE_TREE_WIDE) return f(ByKeys<uint16_t, D, 2>{});
+  if (rows <= 64) return f(ByRows<D, 1>{});
+  if (rows <= 128 || D == 128) return f(ByRows<D, 2>{});
+  return f(ByRows<D, 4>{});
+}
+
 template <typename F>
-auto tree_choice(int G, int D, bool f32, int max_nodes, F f) {
+auto choose(int G, int D, bool f32, int max_nodes, F f) {
   const int64_t rows = (int64_t)G * max_nodes;
-  const auto by_rows = [&](auto e, auto d) {
-    if (rows <= 16) return f(e, d, Const<1>{});
-    if constexpr (sizeof(e) == 4) {
-      return f(e, d, Const<2>{});
-    } else {
-      return rows <= 32 ? f(e, d, Const<2>{}) : f(e, d, Const<4>{});
-    }
-  };
-  if (f32) return D == 64 ? by_rows(float{}, Const<64>{}) : by_rows(float{}, Const<128>{});
-  return D == 64 ? by_rows(uint16_t{}, Const<64>{}) : by_rows(uint16_t{}, Const<128>{});
+  return D == 64 ? choose<64>(rows, f32, f) : choose<128>(rows, f32, f);
 }
 
 }  // namespace
 
 size_t tree_attention_workspace(int Hq, int Hkv, int D, bool f32, int, int max_nodes) {
-  return tree_choice(Hq / Hkv, D, f32, max_nodes, [](auto e, auto d, auto nt) {
-    return TreePlan<decltype(e), decltype(d)::value, decltype(nt)::value>::kBytes;
-  });
+  return choose(Hq / Hkv, D, f32, max_nodes, [](auto k) { return decltype(k)::bytes(); });
 }
 
 hipError_t launch_tree_attention(const TreeArgs& a, hipStream_t s) {
-  return tree_choice(a.G, a.D, a.f32, a.max_nodes, [&](auto e, auto d, auto nt) {
-    return launch<decltype(e), decltype(d)::value, decltype(nt)::value>(a, s);
-  });
+  return choose(a.G, a.D, a.f32, a.max_nodes, [&](auto k) { return decltype(k)::launch(a, s); });
 }
 
 }  // namespace s2moe
