@@ -151,7 +151,24 @@ s2moe_status check_tree(const char* fn, const s2moe_kv_cache* cache, const s2moe
   if (max_nodes > S2MOE_MAX_TOKENS)
     return fail(S2MOE_EUNSUPPORTED, "%s: max_nodes = %d exceeds %d", fn, max_nodes,
                 S2MOE_MAX_TOKENS);
+  // Units of work of one sequence: a 32-bit number on the device.
+  const int64_t tiles = (int64_t)c->max_pages * c->P / 128 + 1;
+  const int64_t blocks = ((int64_t)attn->n_heads / c->Hkv * max_nodes + 15) / 16;
+  if (tiles * blocks * c->Hkv >= (int64_t)1 << 31)
+    return fail(S2MOE_EUNSUPPORTED, "%s: sequences of up to %d pages with %d heads and %d nodes", fn,
+                c->max_pages, attn->n_heads, max_nodes);
   return S2MOE_OK;
+}
+
+// The part of a tree attention call that its workspace depends on.
+void tree_sizes(const s2moe::KvCache& c, const s2moe_attn* attn, int32_t max_nodes,
+                s2moe::TreeArgs* a) {
+  a->Hq = attn->n_heads;
+  a->Hkv = c.Hkv;
+  a->G = attn->n_heads / c.Hkv;
+  a->D = c.D;
+  a->f32 = c.f32;
+  a->max_nodes = max_nodes;
 }
 
 }  // namespace
@@ -271,7 +288,9 @@ size_t s2moe_tree_attention_workspace_bytes(const s2moe_kv_cache* cache, const s
   if (check_tree("s2moe_tree_attention_workspace_bytes", cache, attn, n, max_nodes, &c) !=
       S2MOE_OK)
     return 0;
-  return s2moe::tree_attention_workspace(attn->n_heads, c.Hkv, c.D, c.f32, n, max_nodes);
+  s2moe::TreeArgs a{};
+  tree_sizes(c, attn, max_nodes, &a);
+  return s2moe::tree_attention_workspace(a);
 }
 
 s2moe_status s2moe_tree_attention(const s2moe_kv_cache* cache, int32_t layer,
@@ -297,7 +316,9 @@ s2moe_status s2moe_tree_attention(const s2moe_kv_cache* cache, int32_t layer,
   const int64_t w = (int64_t)Hq * c.D * elt;
   if (rows_meet(q, attn->ldq * elt, w, out, attn->ldo * elt, w, n_tokens))
     return fail(S2MOE_EINVAL, "%s: out overlaps q", fn);
-  const size_t need = s2moe::tree_attention_workspace(Hq, c.Hkv, c.D, c.f32, n, max_nodes);
+  s2moe::TreeArgs a{};
+  tree_sizes(c, attn, max_nodes, &a);
+  const size_t need = s2moe::tree_attention_workspace(a);
   if (workspace == nullptr)
     return fail(S2MOE_EWORKSPACE, "%s: workspace is NULL (%zu bytes needed)", fn, need);
   if (!aligned16(workspace))
@@ -305,7 +326,6 @@ s2moe_status s2moe_tree_attention(const s2moe_kv_cache* cache, int32_t layer,
   if (workspace_bytes < need)
     return fail(S2MOE_EWORKSPACE, "%s: workspace holds %zu bytes, %zu needed", fn,
                 workspace_bytes, need);
-  s2moe::TreeArgs a;
   a.k = c.k + layer * c.layer_bytes();
   a.v = c.v + layer * c.layer_bytes();
   a.table = c.table;
@@ -315,14 +335,8 @@ s2moe_status s2moe_tree_attention(const s2moe_kv_cache* cache, int32_t layer,
   a.log_p = c.log_p;
   a.max_seqs = c.max_seqs;
   a.max_pages = c.max_pages;
-  a.Hq = Hq;
-  a.Hkv = c.Hkv;
-  a.G = Hq / c.Hkv;
-  a.D = c.D;
-  a.f32 = c.f32;
   a.n = n;
   a.n_tokens = n_tokens;
-  a.max_nodes = max_nodes;
   a.seqs = seqs;
   a.tok_off = tok_off;
   a.parent = parent;

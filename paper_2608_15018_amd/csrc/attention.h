@@ -67,7 +67,8 @@ struct TreeArgs {
   float scale;
   float* ws;
 };
-size_t tree_attention_workspace(int Hq, int Hkv, int D, bool f32, int n, int max_nodes);
+// Of a's head counts, head size, type and max_nodes alone.
+size_t tree_attention_workspace(const TreeArgs& a);
 hipError_t launch_tree_attention(const TreeArgs& a, hipStream_t s);
 
 struct PromptArgs {

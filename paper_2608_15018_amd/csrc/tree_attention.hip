@@ -2,7 +2,7 @@
 //
 // Rows.  The query heads of one kv head read the same keys, so the G = Hq / Hkv
 // heads of a sequence's T nodes are T G rows of one product with the keys,
-// taken 16 NT at a time by a workgroup.
+// a block of them to a workgroup.
 //
 // Products.  S^T = K Q^T and O^T = V^T P^T, so that a lane holds scores of one
 // row: the maximum and the sum of a row need no exchange but over the four
@@ -11,15 +11,13 @@
 // 16-key tiles to be key 8 (m / 4) + 4 x + m % 4 of the step: lane group g then
 // holds keys 8 g .. 8 g + 7, and the cache keeps eight neighbouring tokens of one
 // coordinate of V together, so V is read in the order in which it is needed.
-// No operand passes through LDS.
 //
 // Softmax.  One pass with a running maximum per row; it may lag behind the true
 // one by 2^8, so that the accumulators are rescaled about once a row.
 //
 // Split.  The work is a list of units (sequence, kv head, row block, 128 keys),
 // cut into equal stretches, one for each of a fixed number of workgroups,
-// whatever the lengths are: the host does not know them.  Within a workgroup
-// the four waves take 32 keys each.  A row block that one workgroup does not
+// whatever the lengths are: the host does not know them.  A row block that one workgroup does not
 // finish goes to the workspace in parts, and a second launch joins them.
 #include "attention.h"
 #include "attn_common.h"
@@ -27,10 +25,7 @@
 namespace s2moe {
 namespace {
 
-#ifndef S2MOE_TREE_WIDE
-#define S2MOE_TREE_WIDE 32
-#endif
-constexpr int kTile = 128;  // keys of a unit, 32 a wave
+constexpr int kTile = 128;  // keys of a unit
 
 // A row block whose parts the joining launch adds, as the workgroup that has
 // its first keys leaves it.
@@ -43,17 +38,14 @@ struct Split {
   int rows;
 };
 
+// 16 bytes along k, as the matrix instructions take them.
 template <typename E>
-struct Type;
-template <>
-struct Type<uint16_t> {
-  typedef bf16x8 frag;          // 8 of k
-  static constexpr int kK = 8;  // elements of 16 bytes
+struct Fragment {
+  typedef bf16x8 type;
 };
 template <>
-struct Type<float> {
-  typedef f32x4 frag;
-  static constexpr int kK = 4;
+struct Fragment<float> {
+  typedef f32x4 type;
 };
 
 __device__ __forceinline__ f32x4 mma(bf16x8 a, bf16x8 b, f32x4 c) {
@@ -66,35 +58,43 @@ __device__ __forceinline__ f32x4 mma(f32x4 a, f32x4 b, f32x4 c) {
   return c;
 }
 
-template <typename E, int D, int NT>
-struct TreePlan {
-  static constexpr int kRows = 16 * NT;
-  // Workgroups that fit a compute unit.
-  static constexpr int kPerCu = NT == 2 && D * sizeof(E) == 512 ? 1 : 2;
-  static constexpr int kGroups = 256 * kPerCu;
-  static constexpr size_t kPartFloats = (size_t)kRows * (D + 2);
-  static constexpr size_t kBytes = kGroups * (2 * kPartFloats * 4 + sizeof(Split));
+// Where parts go: two for each workgroup, of as many rows as a row block can
+// have, D sums, the maximum and the sum of weights each; then the splits.
+struct Workspace {
+  float* parts;
+  Split* splits;
+  int rows;
+  __device__ __host__ Workspace(float* ws, int groups, int rows_, int D) : parts(ws), rows(rows_) {
+    splits = reinterpret_cast<Split*>(ws + (size_t)groups * 2 * rows * (D + 2));
+  }
+  static size_t bytes(int groups, int rows, int D) {
+    return groups * ((size_t)2 * rows * (D + 2) * 4 + sizeof(Split));
+  }
+  __device__ float* part(int group, int slot, int D) const {
+    return parts + (2 * (size_t)group + slot) * rows * (D + 2);
+  }
 };
-
-__device__ __forceinline__ bool sane(const TreeArgs& a, int first, int end) {
-  return first >= 0 && first < end && end <= a.n_tokens;
+inline __device__ __host__ int part_rows(const TreeArgs& a, int RB) {
+  const int64_t rows = (int64_t)a.G * a.max_nodes;
+  return rows < RB ? (int)rows : RB;
 }
 
-// Tree and context of request i: first token, nodes, cached tokens, table row.
+// One request's tree and context: first token, nodes, cached tokens, those and
+// the nodes' slots together, table row; and the units before it.
 struct Request {
-  int first, T, len, total;
-  const int32_t* row;
+  int64_t before;
+  int first, T, len, total, seq, pad;
 };
 __device__ __forceinline__ Request request(const TreeArgs& a, int i) {
   Request r{};
-  r.first = constant(a.tok_off, i);
-  const int end = constant(a.tok_off, i + 1), s = constant(a.seqs, i);
-  if (!sane(a, r.first, end) || s < 0 || s >= a.max_seqs) return r;
-  r.T = min(end - r.first, a.max_nodes);
+  r.first = a.tok_off[i];
+  const int end = a.tok_off[i + 1];
+  r.seq = a.seqs[i];
+  const bool good = r.first >= 0 && r.first < end && end <= a.n_tokens && r.seq >= 0 && r.seq < a.max_seqs;
+  r.T = good ? min(end - r.first, a.max_nodes) : 0;
   const int cap = a.max_pages << a.log_p;
-  r.len = min(max(constant(a.length, s), 0), cap);
+  r.len = good ? min(max(a.length[r.seq], 0), cap) : 0;
   r.total = r.len + min(r.T, cap - r.len);
-  r.row = a.table + (int64_t)s * a.max_pages;
   return r;
 }
 
@@ -138,18 +138,25 @@ __device__ void ancestors(const int32_t* parent, int T, uint32_t* mask_s, int* j
   }
 }
 
-// Units before each request into before_s[0 .. n]; returns their number.
-__device__ int64_t count_units(const TreeArgs& a, int RB, int64_t* before_s) {
+// All requests, with the units before each, into req_s[0 .. n - 1]; returns the
+// number of units.  256 threads, ceil(n / 256) consecutive requests each.
+__device__ int64_t list_requests(const TreeArgs& a, int RB, Request* req_s) {
   __shared__ int64_t wave_s[4];
   const int tid = threadIdx.x, lane = tid & 63, w = tid >> 6;
+  const int per = (a.n + 255) >> 8;
   int64_t mine = 0;
-  for (int x = 0; x < 4; ++x) {
-    const int i = 4 * tid + x;
-    if (i < a.n) {
-      const Request r = request(a, i);
-      before_s[i] = mine;
-      mine += (int64_t)((r.T * a.G + RB - 1) / RB) * a.Hkv * ((r.total + kTile - 1) / kTile);
-    }
+  for (int x = 0; x < per; ++x) {
+    const int i = per * tid + x;
+    if (i >= a.n) break;
+    Request r = request(a, i);
+    r.before = mine;
+    req_s[i] = r;
+    mine += (int64_t)((r.T * a.G + RB - 1) / RB) * a.Hkv * ((r.total + kTile - 1) / kTile);
+  }
+  if (a.n == 1) {  // one thread knows all
+    if (tid == 0) wave_s[0] = mine;
+    __syncthreads();
+    return wave_s[0];
   }
   int64_t inc = mine;
 #pragma unroll
@@ -165,21 +172,47 @@ __device__ int64_t count_units(const TreeArgs& a, int RB, int64_t* before_s) {
     at += x < w ? wave_s[x] : 0;
     total += wave_s[x];
   }
-  for (int x = 0; x < 4; ++x)
-    if (4 * tid + x < a.n) before_s[4 * tid + x] += at;
-  if (tid == 0) before_s[a.n] = total;
+  for (int x = 0; x < per; ++x)
+    if (per * tid + x < a.n) req_s[per * tid + x].before += at;
   __syncthreads();
   return total;
 }
 
-// The request that unit u falls into.
-__device__ int request_of(int64_t u, int n, const int64_t* before_s) {
+// The last request that has units and whose first is at or before u.
+__device__ int request_of(int64_t u, int n, const Request* req_s) {
   int i = 0, hi = n;
   while (hi - i > 1) {
     const int mid = (i + hi) / 2;
-    if (before_s[mid] <= u) i = mid; else hi = mid;
+    if (req_s[mid].before <= u) i = mid; else hi = mid;
   }
-  return i;
+  return __builtin_amdgcn_readfirstlane(i);
+}
+
+// The stretch of a row block that unit u starts: at most up to unit u_end.
+struct Stretch {
+  int first, T, len, total;      // as in Request
+  const int32_t* row;            // of the table
+  int R, hk, row0, t0, t1, tiles;
+};
+__device__ __forceinline__ Stretch stretch_of(const TreeArgs& a, const Request* req_s, int i, int RB,
+                                              int64_t u, int64_t u_end) {
+  const auto same = [](int x) { return __builtin_amdgcn_readfirstlane(x); };
+  const Request r = req_s[i];
+  Stretch z;
+  z.first = same(r.first);
+  z.T = same(r.T);
+  z.len = same(r.len);
+  z.total = same(r.total);
+  z.row = a.table + (int64_t)same(r.seq) * a.max_pages;
+  z.R = z.T * a.G;
+  z.tiles = (z.total + kTile - 1) / kTile;
+  const int in = same((int)(u - r.before)), blocks = (z.R + RB - 1) / RB;
+  const int job = in / z.tiles;
+  z.t0 = in - job * z.tiles;
+  z.t1 = same((int)min((int64_t)z.tiles, z.t0 + (u_end - u)));
+  z.hk = job / blocks;
+  z.row0 = (job % blocks) * RB;
+  return z;
 }
 
 // Which of eight slots from node k0 on a row sees, k0 < 0 being cached tokens.
@@ -242,15 +275,27 @@ __device__ __forceinline__ void write_row(const TreeArgs& a, int first, int hk, 
   }
 }
 
+// Small trees: the four waves take 32 keys of a unit each, all rows of the block,
+// and their sums are added at the end of a stretch.  No operand passes through
+// LDS; the loads of the next unit are issued as soon as this one's registers are
+// free, so that two workgroups a compute unit keep over 100 KB in flight.
 template <typename E, int D, int NT>
-__global__ __launch_bounds__(256, (TreePlan<E, D, NT>::kPerCu)) void tree_kernel(TreeArgs a) {
-  typedef typename Type<E>::frag frag;
-  typedef TreePlan<E, D, NT> Plan;
+struct KeysPlan {
+  static constexpr int kRows = 16 * NT;
+  // Workgroups that fit a compute unit.
+  static constexpr int kPerCu = NT == 2 && D * sizeof(E) == 512 ? 1 : 2;
+  static constexpr int kGroups = 256 * kPerCu;
+};
+
+template <typename E, int D, int NT>
+__global__ __launch_bounds__(256, (KeysPlan<E, D, NT>::kPerCu)) void tree_keys_kernel(TreeArgs a) {
+  typedef typename Fragment<E>::type frag;
+  typedef KeysPlan<E, D, NT> Plan;
   constexpr bool kF32 = sizeof(E) == 4;
   constexpr int RB = 16 * NT, MT = D / 16, ES = sizeof(E);
   constexpr int KC = D * ES / 64;  // 64-byte pieces of a key, 16 bytes a lane
   constexpr int VC = ES / 2;       // 16-byte pieces of eight values
-  __shared__ int64_t before_s[kKvMaxRequests + 1];
+  __shared__ Request req_s[kKvMaxRequests];
   __shared__ __attribute__((aligned(16))) float sum_s[4][16][D + 4];
   __shared__ float m_s[4][RB], l_s[4][RB];
   __shared__ uint32_t mask_s[kMaxNodes * kMaskRow];
@@ -259,16 +304,13 @@ __global__ __launch_bounds__(256, (TreePlan<E, D, NT>::kPerCu)) void tree_kernel
 
   const int tid = threadIdx.x, lane = tid & 63, w = wave_id();
   const int n16 = lane & 15, g = lane >> 4;
-  Split* const splits = reinterpret_cast<Split*>(a.ws + (size_t)Plan::kGroups * 2 * Plan::kPartFloats);
-  float* const parts = a.ws;
-
-  const int64_t total = count_units(a, RB, before_s);
+  const Workspace ws(a.ws, Plan::kGroups, part_rows(a, RB), D);
+  const int64_t total = list_requests(a, RB, req_s);
   const int64_t share = (total + Plan::kGroups - 1) / Plan::kGroups;
   int64_t u = blockIdx.x * share;
   const int64_t u_end = min(u + share, total), u_first = u;
   int split_parts = 0;  // of a row block that starts here and goes on elsewhere
 
-  int i = u < u_end ? request_of(u, a.n, before_s) : 0;
   const float c = a.scale * 1.44269504088896340736f;
   const int64_t head_bytes = (int64_t)a.P * D * ES, page_bytes = head_bytes * a.Hkv;
   // This lane's place in a half step of 16 keys, of the x-th key tile.
@@ -276,15 +318,8 @@ __global__ __launch_bounds__(256, (TreePlan<E, D, NT>::kPerCu)) void tree_kernel
   const int v_lane = ((g & 1) * D + n16) * 8 * ES;
 
   while (u < u_end) {
-    i = __builtin_amdgcn_readfirstlane(i);
-    while (before_s[i + 1] <= u) ++i;
-    const Request r = request(a, i);
-    const int tiles = (r.total + kTile - 1) / kTile, R = r.T * a.G, blocks = (R + RB - 1) / RB;
-    const int64_t in = u - before_s[i];
-    const int job = __builtin_amdgcn_readfirstlane((int)(in / tiles));
-    const int t0 = __builtin_amdgcn_readfirstlane((int)(in - (int64_t)job * tiles));
-    const int t1 = (int)min((int64_t)tiles, t0 + (u_end - u));
-    const int hk = job / blocks, row0 = (job % blocks) * RB;
+    const Stretch r = stretch_of(a, req_s, request_of(u, a.n, req_s), RB, u, u_end);
+    const int t0 = r.t0, t1 = r.t1, R = r.R, hk = r.hk, row0 = r.row0;
     const bool tail = t1 * kTile > r.len;
     if (tail) ancestors(a.parent + r.first, r.T, mask_s, jump_s, dead_s);
 
@@ -294,7 +329,7 @@ __global__ __launch_bounds__(256, (TreePlan<E, D, NT>::kPerCu)) void tree_kernel
     for (int nt = 0; nt < NT; ++nt) {
       const int row = min(row0 + 16 * nt + n16, R - 1);
       tok[nt] = row / a.G;
-      const char* p = a.q + ((int64_t)(r.first + tok[nt]) * a.ldq + (hk * a.G + row % a.G) * D) * ES + 16 * g;
+      const char* p = a.q + ((int64_t)(r.first + tok[nt]) * a.ldq + (hk * a.G + row - tok[nt] * a.G) * D) * ES + 16 * g;
 #pragma unroll
       for (int x = 0; x < KC; ++x) q[x][nt] = *reinterpret_cast<const frag*>(p + 64 * x);
     }
@@ -426,9 +461,9 @@ __global__ __launch_bounds__(256, (TreePlan<E, D, NT>::kPerCu)) void tree_kernel
       }
     }
     __syncthreads();
-    const bool whole = t0 == 0 && t1 == tiles;
+    const bool whole = t0 == 0 && t1 == r.tiles;
     const int slot = u == u_first ? 0 : 1;
-    float* const part = parts + (2 * (size_t)blockIdx.x + slot) * Plan::kPartFloats;
+    float* const part = ws.part(blockIdx.x, slot, D);
     const int orow = tid >> 4, od = (tid & 15) * (D / 16);
 #pragma unroll
     for (int nt = 0; nt < NT; ++nt) {
@@ -474,170 +509,134 @@ __global__ __launch_bounds__(256, (TreePlan<E, D, NT>::kPerCu)) void tree_kernel
       __syncthreads();
     }
     if (t0 == 0 && !whole) {
-      const int64_t end = u + tiles;  // of the row block
-      split_parts = (int)((end - 1) / share) - (int)blockIdx.x + 1;
+      split_parts = (int)((u + r.tiles - 1) / share) - (int)blockIdx.x + 1;
       if (tid == 0)
-        splits[blockIdx.x] = Split{split_parts, slot, r.first, hk, row0, min(RB, R - row0)};
+        ws.splits[blockIdx.x] = Split{split_parts, slot, r.first, hk, row0, min(RB, R - row0)};
     }
     u += t1 - t0;
   }
-  if (split_parts == 0 && tid == 0) splits[blockIdx.x].parts = 0;
+  if (split_parts == 0 && tid == 0) ws.splits[blockIdx.x].parts = 0;
 }
 
-// Larger trees (bf16): rows are split over the waves, 16 NT each, and the keys and
-// values of a stage are fetched once for all of them, by loads that go from the
+// Larger trees (bf16): the waves split the rows, 16 at a time in turn, and the keys
+// and values of a stage are fetched once for all of them, by loads that go from the
 // pages into LDS without a register between: three stages are in flight while one
-// is used.  A wave fetches an eighth or quarter of a stage that lies in one page.
+// is used.  A wave fetches a quarter of a stage, which lies in one page.
 template <int D, int NT>
-struct WidePlan {
+struct RowsPlan {
   static constexpr int kRows = 64 * NT;
   static constexpr int kKeys = D == 128 ? 32 : 64;  // of a stage
   static constexpr int kStage = kKeys * D * 2;      // bytes of its keys, or values
   static constexpr int kRing = 4 * 2 * kStage;
-  static constexpr int kPerCu = D == 128 && NT == 4 ? 1 : 2;
-  static constexpr int kGroups = 256 * kPerCu;
-  static constexpr size_t kPartFloats = (size_t)kRows * (D + 2);
-  static constexpr size_t kBytes = kGroups * (2 * kPartFloats * 4 + sizeof(Split));
+  static constexpr int kGroups = 512;               // two fit a compute unit
   static size_t lds(int n, int max_nodes) {
-    return kRing + (size_t)(n + 1) * 8 + (size_t)max_nodes * (kMaskRow * 4 + 4 + 4);
+    return kRing + (size_t)n * sizeof(Request) + (size_t)max_nodes * (kMaskRow * 4 + 4 + 4);
   }
 };
 
-template <int D, int NT>
-__global__ __launch_bounds__(256, (WidePlan<D, NT>::kPerCu)) void tree_wide_kernel(TreeArgs a) {
-  typedef WidePlan<D, NT> Plan;
-  constexpr int RB = Plan::kRows, MT = D / 16, KC = D / 32, SK = Plan::kKeys;
-  constexpr int kLoads = Plan::kStage / 4096;  // 1 KB loads a wave makes for keys, or values
-  constexpr int CH = D / 8;                    // 16-byte chunks of a key
-  extern __shared__ __attribute__((aligned(16))) char smem[];
-  char* const k_lds = smem;
-  char* const v_lds = smem + 4 * Plan::kStage;
-  int64_t* const before_s = reinterpret_cast<int64_t*>(smem + Plan::kRing);
-  uint32_t* const mask_s = reinterpret_cast<uint32_t*>(before_s + a.n + 1);
-  int* const jump_s = reinterpret_cast<int*>(mask_s + a.max_nodes * kMaskRow);
-  uint8_t* const dead_s = reinterpret_cast<uint8_t*>(jump_s + a.max_nodes);
+template <int D>
+struct RowsStage {  // what the waves of a workgroup share in a stretch
+  char *k_lds, *v_lds;
+  uint32_t* mask_s;
+  uint8_t* dead_s;
+  const char *kb, *vb;  // the head's keys and values in the first page
+  int64_t page_bytes;
+  uint32_t k_off[RowsPlan<D, 1>::kStage / 4096];
+  int s0, s1;
+};
 
-  const int tid = threadIdx.x, lane = tid & 63, w = wave_id();
-  const int n16 = lane & 15, g = lane >> 4;
-  Split* const splits = reinterpret_cast<Split*>(a.ws + (size_t)Plan::kGroups * 2 * Plan::kPartFloats);
-  const int64_t total = count_units(a, RB, before_s);
-  const int64_t share = (total + Plan::kGroups - 1) / Plan::kGroups;
-  int64_t u = blockIdx.x * share;
-  const int64_t u_end = min(u + share, total), u_first = u;
-  int split_parts = 0;
-  int i = u < u_end ? request_of(u, a.n, before_s) : 0;
-  const float c = a.scale * 1.44269504088896340736f;
-  const int64_t head_bytes = (int64_t)a.P * D * 2, page_bytes = head_bytes * a.Hkv;
-
-  // Chunk x of key r of a stage lies at chunk x ^ swizzle(r); values lie as they do
-  // in the page.
-  const auto swizzle = [](int r) { return D == 128 ? r & 15 : (r >> 1) & 7; };
-  uint32_t k_off[kLoads];
+// Stage s into its place in the ring; past the stretch, its last again.
+template <int D>
+__device__ __forceinline__ int rows_key(const RowsStage<D>& st, int s) {
+  return min(s, st.s1 - 1) * RowsPlan<D, 1>::kKeys + wave_id() * (RowsPlan<D, 1>::kKeys / 4);
+}
+template <int D>
+__device__ __forceinline__ int rows_page(const TreeArgs& a, const Stretch& r, const RowsStage<D>& st, int s) {
+  const int page = constant(r.row, min(rows_key(st, s) >> a.log_p, a.max_pages - 1));
+  return min(max(page, 0), a.n_pages - 1);
+}
+template <int D>
+__device__ __forceinline__ void load_rows_stage(const TreeArgs& a, const Stretch& r, const RowsStage<D>& st, int s,
+                                                int page) {
+  typedef RowsPlan<D, 1> Plan;
+  constexpr int kLoads = Plan::kStage / 4096;
+  const int64_t at = page * st.page_bytes + (int64_t)(rows_key(st, s) & (a.P - 1)) * (D * 2);
+  const int to = (s & 3) * Plan::kStage + wave_id() * kLoads * 1024;
 #pragma unroll
-  for (int x = 0; x < kLoads; ++x) {
-    const int r = x * (64 / CH) + lane / CH;  // within the wave's keys
-    k_off[x] = r * D * 2 + (((lane % CH) ^ swizzle(w * (SK / 4) + r)) << 4);
-  }
+  for (int x = 0; x < kLoads; ++x) load_to_lds(st.kb + at, st.k_off[x], st.k_lds + to + x * 1024);
+#pragma unroll
+  for (int x = 0; x < kLoads; ++x)
+    load_to_lds(st.vb + at, x * 1024 + (threadIdx.x & 63) * 16, st.v_lds + to + x * 1024);
+}
+
+// A stretch, for a wave with NA tiles of 16 rows in it; all waves come through
+// here with their own NA, and pass the same barriers.
+template <int D, int NA>
+__device__ __forceinline__ void rows_stretch(const TreeArgs& a, const Stretch& r, const RowsStage<D>& st, int page,
+                                             bool tail, int tile0, bool whole, float* part) {
+  typedef RowsPlan<D, 1> Plan;
+  constexpr int MT = D / 16, KC = D / 32, SK = Plan::kKeys, kLoads = Plan::kStage / 4096;
+  constexpr int N1 = NA > 0 ? NA : 1;
+  const int lane = threadIdx.x & 63, w = wave_id(), n16 = lane & 15, g = lane >> 4;
+  const auto swizzle = [](int x) { return D == 128 ? x & 15 : (x >> 1) & 7; };
   const int key_row = 8 * (n16 >> 2) + (n16 & 3);  // of the first 16-key tile; the second's is 4 on
-
-  while (u < u_end) {
-    i = __builtin_amdgcn_readfirstlane(i);
-    while (before_s[i + 1] <= u) ++i;
-    const Request r = request(a, i);
-    const int tiles = (r.total + kTile - 1) / kTile, R = r.T * a.G, blocks = (R + RB - 1) / RB;
-    const int64_t in = u - before_s[i];
-    const int job = __builtin_amdgcn_readfirstlane((int)(in / tiles));
-    const int t0 = __builtin_amdgcn_readfirstlane((int)(in - (int64_t)job * tiles));
-    const int t1 = (int)min((int64_t)tiles, t0 + (u_end - u));
-    const int hk = job / blocks, row0 = (job % blocks) * RB;
-    const int s0 = t0 * (kTile / SK), s1 = min(t1 * (kTile / SK), (r.total + SK - 1) / SK);
-    const bool tail = t1 * kTile > r.len;
-    const int wrow0 = row0 + 16 * NT * w;
-    const bool active = wrow0 < R;
-
-    // Stage s into its place in the ring; past the stretch, its last again.
-    const char* const kb = a.k + hk * head_bytes;
-    const char* const vb = a.v + hk * head_bytes;
-    const auto page_of = [&](int s) {
-      const int key = min(s, s1 - 1) * SK + w * (SK / 4);
-      const int page = constant(r.row, min(key >> a.log_p, a.max_pages - 1));
-      return min(max(page, 0), a.n_pages - 1);
-    };
-    const auto load_stage = [&](int s, int page) {
-      const int key = min(s, s1 - 1) * SK + w * (SK / 4);
-      const int64_t at = page * page_bytes + (int64_t)(key & (a.P - 1)) * (D * 2);
+  const float c = a.scale * 1.44269504088896340736f;
+  int tok[N1];
+  bf16x8 q[KC][N1];
+  f32x4 O[MT][N1];
+  float shift[N1], limit[N1], l[N1];
 #pragma unroll
-      for (int x = 0; x < kLoads; ++x)
-        load_to_lds(kb + at, k_off[x], k_lds + (s & 3) * Plan::kStage + (w * kLoads + x) * 1024);
+  for (int nt = 0; nt < NA; ++nt) {
+    const int row = min(tile0 + 64 * nt + n16, r.R - 1);
+    tok[nt] = row / a.G;
+    const char* p = a.q + ((int64_t)(r.first + tok[nt]) * a.ldq + (r.hk * a.G + row - tok[nt] * a.G) * D) * 2 + 16 * g;
 #pragma unroll
-      for (int x = 0; x < kLoads; ++x)
-        load_to_lds(vb + at, x * 1024 + lane * 16, v_lds + (s & 3) * Plan::kStage + (w * kLoads + x) * 1024);
-    };
-    load_stage(s0, page_of(s0));
-    load_stage(s0 + 1, page_of(s0 + 1));
-    load_stage(s0 + 2, page_of(s0 + 2));
-    int page = page_of(s0 + 3);
-    if (tail) ancestors(a.parent + r.first, r.T, mask_s, jump_s, dead_s);
-
-    int tok[NT];
-    bf16x8 q[KC][NT];
+    for (int x = 0; x < KC; ++x) q[x][nt] = *reinterpret_cast<const bf16x8*>(p + 64 * x);
+    shift[nt] = 0.f;
+    limit[nt] = -INFINITY;
+    l[nt] = 0.f;
 #pragma unroll
-    for (int nt = 0; nt < NT; ++nt) {
-      const int row = min(wrow0 + 16 * nt + n16, R - 1);
-      tok[nt] = row / a.G;
-      const char* p = a.q + ((int64_t)(r.first + tok[nt]) * a.ldq + (hk * a.G + row % a.G) * D) * 2 + 16 * g;
-#pragma unroll
-      for (int x = 0; x < KC; ++x) q[x][nt] = *reinterpret_cast<const bf16x8*>(p + 64 * x);
-    }
-    f32x4 O[MT][NT];
-    float shift[NT], limit[NT], l[NT];
-#pragma unroll
-    for (int nt = 0; nt < NT; ++nt) {
-      shift[nt] = 0.f;
-      limit[nt] = -INFINITY;
-      l[nt] = 0.f;
-#pragma unroll
-      for (int mt = 0; mt < MT; ++mt) O[mt][nt] = f32x4{};
-    }
-    for (int s = s0; s < s1; ++s) {
-      // Stage s is there for everybody, and stage s - 1, whose place stage s + 3
-      // takes, is read by nobody any more.
-      wait_loads<4 * kLoads>();
-      __builtin_amdgcn_s_barrier();
-      load_stage(s + 3, page);
-      page = page_of(s + 4);
-      if (!active) continue;
+    for (int mt = 0; mt < MT; ++mt) O[mt][nt] = f32x4{};
+  }
+  for (int s = st.s0; s < st.s1; ++s) {
+    // Stage s is there for everybody, and stage s - 1, whose place stage s + 3
+    // takes, is read by nobody any more.
+    wait_loads<4 * kLoads>();
+    __builtin_amdgcn_s_barrier();
+    load_rows_stage<D>(a, r, st, s + 3, page);
+    page = rows_page<D>(a, r, st, s + 4);
+    if constexpr (NA > 0) {
 #pragma unroll
       for (int sub = 0; sub < SK / 32; ++sub) {
         const int key0 = s * SK + 32 * sub;
-        const char* kt = k_lds + (s & 3) * Plan::kStage + 32 * sub * D * 2;
-        const char* vt = v_lds + (s & 3) * Plan::kStage + (4 * sub + g) * (D * 16) + n16 * 16;
-        f32x4 S[2][NT];
+        const char* kt = st.k_lds + (s & 3) * Plan::kStage + 32 * sub * D * 2;
+        const char* vt = st.v_lds + (s & 3) * Plan::kStage + (4 * sub + g) * (D * 16) + n16 * 16;
+        f32x4 S[2][NA];
 #pragma unroll
         for (int x = 0; x < 2; ++x) {
 #pragma unroll
-          for (int nt = 0; nt < NT; ++nt) S[x][nt] = f32x4{};
+          for (int nt = 0; nt < NA; ++nt) S[x][nt] = f32x4{};
           const int row = key_row + 4 * x;
 #pragma unroll
           for (int y = 0; y < KC; ++y) {
             const bf16x8 k = *reinterpret_cast<const bf16x8*>(kt + row * D * 2 + (((4 * y + g) ^ swizzle(row)) << 4));
 #pragma unroll
-            for (int nt = 0; nt < NT; ++nt) S[x][nt] = mma(k, q[y][nt], S[x][nt]);
+            for (int nt = 0; nt < NA; ++nt) S[x][nt] = mma(k, q[y][nt], S[x][nt]);
           }
         }
         const bool masked = key0 + 32 > r.len;
-        if (masked) mask_scores<NT>(S, tok, mask_s, key0 + 8 * g, r.len, r.total);
-        float m[NT];
+        if (masked) mask_scores<NA>(S, tok, st.mask_s, key0 + 8 * g, r.len, r.total);
+        float m[NA];
         bool over = false;
 #pragma unroll
-        for (int nt = 0; nt < NT; ++nt) {
+        for (int nt = 0; nt < NA; ++nt) {
           m[nt] = largest(S[0][nt], S[1][nt]) * c;
           over |= m[nt] > limit[nt];
         }
-        if (__any(over)) raise<MT, NT>(m, shift, limit, l, O);
-        bf16x8 P[NT];
+        if (__any(over)) raise<MT, NA>(m, shift, limit, l, O);
+        bf16x8 P[NA];
 #pragma unroll
-        for (int nt = 0; nt < NT; ++nt) {
+        for (int nt = 0; nt < NA; ++nt) {
           float p[8];
 #pragma unroll
           for (int e = 0; e < 8; ++e) {
@@ -651,7 +650,7 @@ __global__ __launch_bounds__(256, (WidePlan<D, NT>::kPerCu)) void tree_wide_kern
           bf16x8 v = *reinterpret_cast<const bf16x8*>(vt + mt * 256);
           if (masked && __any(any_nonfinite(v))) {
 #pragma unroll
-            for (int nt = 0; nt < NT; ++nt) {
+            for (int nt = 0; nt < NA; ++nt) {
               const f32x4 met = mma(nonfinite_ones(v), P[nt], f32x4{});
 #pragma unroll
               for (int e = 0; e < 4; ++e) O[mt][nt][e] = met[e] != 0.f ? NAN : O[mt][nt][e];
@@ -659,61 +658,109 @@ __global__ __launch_bounds__(256, (WidePlan<D, NT>::kPerCu)) void tree_wide_kern
             v = finite_only(v);
           }
 #pragma unroll
-          for (int nt = 0; nt < NT; ++nt) O[mt][nt] = mma(v, P[nt], O[mt][nt]);
+          for (int nt = 0; nt < NA; ++nt) O[mt][nt] = mma(v, P[nt], O[mt][nt]);
         }
       }
     }
-    wait_loads<0>();  // what was loaded past the stretch
-    __syncthreads();  // nobody reads this stretch's stages or masks any more
+  }
+  wait_loads<0>();  // what was loaded past the stretch
+  __syncthreads();  // nobody reads this stretch's stages any more
+#pragma unroll
+  for (int nt = 0; nt < NA; ++nt) {
+    const int row = tile0 + 64 * nt + n16;
+    const float sum = sum_groups(l[nt]);
+    if (row >= r.R) continue;
+    const bool dead = tail && st.dead_s[tok[nt]];
+    if (whole) {
+      const float inv = dead || sum == 0.f ? 0.f : 1.f / sum;
+      uint16_t* o = reinterpret_cast<uint16_t*>(a.out) + (int64_t)(r.first + tok[nt]) * a.ldo +
+                    (r.hk * a.G + row - tok[nt] * a.G) * D + 4 * g;
+#pragma unroll
+      for (int mt = 0; mt < MT; ++mt) {
+        f32x4 v;
+#pragma unroll
+        for (int e = 0; e < 4; ++e) v[e] = inv == 0.f ? 0.f : O[mt][nt][e] * inv;
+        *reinterpret_cast<bf16x4*>(o + 16 * mt) = __builtin_convertvector(v, bf16x4);
+      }
+    } else {
+      float* to = part + (row - r.row0) * (D + 2);
+#pragma unroll
+      for (int mt = 0; mt < MT; ++mt)
+#pragma unroll
+        for (int e = 0; e < 4; e += 2)
+          *reinterpret_cast<f32x2*>(to + 16 * mt + 4 * g + e) = f32x2{O[mt][nt][e], O[mt][nt][e + 1]};
+      if (g == 0)
+        *reinterpret_cast<f32x2*>(to + D) = f32x2{limit[nt] == -INFINITY ? -INFINITY : shift[nt], dead ? -1.f : sum};
+    }
+  }
+}
 
-    const bool whole = t0 == 0 && t1 == tiles;
+template <int D, int NT>
+__global__ __launch_bounds__(256, 2) void tree_rows_kernel(TreeArgs a) {
+  typedef RowsPlan<D, NT> Plan;
+  constexpr int RB = Plan::kRows, SK = Plan::kKeys, kLoads = Plan::kStage / 4096, CH = D / 8;
+  extern __shared__ __attribute__((aligned(16))) char smem[];
+  Request* const req_s = reinterpret_cast<Request*>(smem + Plan::kRing);
+  RowsStage<D> st;
+  st.k_lds = smem;
+  st.v_lds = smem + 4 * Plan::kStage;
+  st.mask_s = reinterpret_cast<uint32_t*>(req_s + a.n);
+  int* const jump_s = reinterpret_cast<int*>(st.mask_s + a.max_nodes * kMaskRow);
+  st.dead_s = reinterpret_cast<uint8_t*>(jump_s + a.max_nodes);
+
+  const int tid = threadIdx.x, lane = tid & 63, w = wave_id();
+  const Workspace ws(a.ws, Plan::kGroups, part_rows(a, RB), D);
+  const int64_t total = list_requests(a, RB, req_s);
+  const int64_t share = (total + Plan::kGroups - 1) / Plan::kGroups;
+  int64_t u = blockIdx.x * share;
+  const int64_t u_end = min(u + share, total), u_first = u;
+  int split_parts = 0;
+  const int64_t head_bytes = (int64_t)a.P * D * 2;
+  st.page_bytes = head_bytes * a.Hkv;
+  // Chunk x of key i of a stage lies at chunk x ^ swizzle(i), so that reads spread
+  // over all banks; values lie as they do in the page.
+#pragma unroll
+  for (int x = 0; x < kLoads; ++x) {
+    const int i = x * (64 / CH) + lane / CH, at = w * (SK / 4) + i;  // within the wave's keys, the stage's
+    st.k_off[x] = i * D * 2 + (((lane % CH) ^ (D == 128 ? at & 15 : (at >> 1) & 7)) << 4);
+  }
+  while (u < u_end) {
+    const Stretch r = stretch_of(a, req_s, request_of(u, a.n, req_s), RB, u, u_end);
+    st.kb = a.k + r.hk * head_bytes;
+    st.vb = a.v + r.hk * head_bytes;
+    st.s0 = r.t0 * (kTile / SK);
+    st.s1 = min(r.t1 * (kTile / SK), (r.total + SK - 1) / SK);
+#pragma unroll
+    for (int x = 0; x < 3; ++x) load_rows_stage<D>(a, r, st, st.s0 + x, rows_page<D>(a, r, st, st.s0 + x));
+    const int page = rows_page<D>(a, r, st, st.s0 + 3);
+    const bool tail = r.t1 * kTile > r.len, whole = r.t0 == 0 && r.t1 == r.tiles;
+    if (tail) ancestors(a.parent + r.first, r.T, st.mask_s, jump_s, st.dead_s);
     const int slot = u == u_first ? 0 : 1;
-    float* const part = a.ws + (2 * (size_t)blockIdx.x + slot) * Plan::kPartFloats;
-#pragma unroll
-    for (int nt = 0; nt < NT; ++nt) {
-      const int row = wrow0 + 16 * nt + n16;
-      const float sum = sum_groups(l[nt]);
-      if (row >= R) continue;
-      const bool dead = tail && dead_s[row / a.G];
-      if (whole) {
-        const float inv = dead || sum == 0.f ? 0.f : 1.f / sum;
-        uint16_t* o = reinterpret_cast<uint16_t*>(a.out) + (int64_t)(r.first + row / a.G) * a.ldo +
-                      (hk * a.G + row % a.G) * D + 4 * g;
-#pragma unroll
-        for (int mt = 0; mt < MT; ++mt) {
-          f32x4 v;
-#pragma unroll
-          for (int e = 0; e < 4; ++e) v[e] = inv == 0.f ? 0.f : O[mt][nt][e] * inv;
-          *reinterpret_cast<bf16x4*>(o + 16 * mt) = __builtin_convertvector(v, bf16x4);
-        }
-      } else {
-        float* to = part + (row - row0) * (D + 2);
-#pragma unroll
-        for (int mt = 0; mt < MT; ++mt)
-#pragma unroll
-          for (int e = 0; e < 4; e += 2)
-            *reinterpret_cast<f32x2*>(to + 16 * mt + 4 * g + e) = f32x2{O[mt][nt][e], O[mt][nt][e + 1]};
-        if (g == 0)
-          *reinterpret_cast<f32x2*>(to + D) = f32x2{limit[nt] == -INFINITY ? -INFINITY : shift[nt], dead ? -1.f : sum};
-      }
-    }
-    if (t0 == 0 && !whole) {
-      split_parts = (int)((u + tiles - 1) / share) - (int)blockIdx.x + 1;
+    float* const part = ws.part(blockIdx.x, slot, D);
+    const int tile0 = r.row0 + 16 * w;
+    const int na = tile0 >= r.R ? 0 : min(NT, (r.R - tile0 + 63) / 64);
+    if (na == 0) rows_stretch<D, 0>(a, r, st, page, tail, tile0, whole, part);
+    else if (na == 1) rows_stretch<D, 1>(a, r, st, page, tail, tile0, whole, part);
+    else if (NT == 2 || na == 2) rows_stretch<D, 2>(a, r, st, page, tail, tile0, whole, part);
+    else rows_stretch<D, NT == 4 ? 4 : 0>(a, r, st, page, tail, tile0, whole, part);
+    if (r.t0 == 0 && !whole) {
+      split_parts = (int)((u + r.tiles - 1) / share) - (int)blockIdx.x + 1;
       if (tid == 0)
-        splits[blockIdx.x] = Split{split_parts, slot, r.first, hk, row0, min(RB, R - row0)};
+        ws.splits[blockIdx.x] = Split{split_parts, slot, r.first, r.hk, r.row0, min(RB, r.R - r.row0)};
     }
-    u += t1 - t0;
+    u += r.t1 - r.t0;
     __syncthreads();  // dead_s is free again
   }
-  if (split_parts == 0 && tid == 0) splits[blockIdx.x].parts = 0;
+  if (split_parts == 0 && tid == 0) ws.splits[blockIdx.x].parts = 0;
 }
 
 // Adds the parts of the row block that starts in workgroup blockIdx.x's stretch
 // and ends in a later one's; blockIdx.y four rows, a wave every fourth part.
-template <typename E, int D, typename Plan>
-__global__ __launch_bounds__(256) void tree_join_kernel(TreeArgs a) {
+template <typename E, int D>
+__global__ __launch_bounds__(256) void tree_join_kernel(TreeArgs a, int groups, int RB) {
   __shared__ float m_s[4][4], l_s[4][4], o_s[4][4][D];
-  const Split sp = reinterpret_cast<const Split*>(a.ws + (size_t)Plan::kGroups * 2 * Plan::kPartFloats)[blockIdx.x];
+  const Workspace ws(a.ws, groups, part_rows(a, RB), D);
+  const Split sp = ws.splits[blockIdx.x];
   const int row4 = blockIdx.y * 4;
   if (sp.parts == 0 || row4 >= sp.rows) return;
   const int tid = threadIdx.x, w = wave_id(), lr = (tid & 63) >> 4, od = (tid & 15) * (D / 16);
@@ -722,10 +769,9 @@ __global__ __launch_bounds__(256) void tree_join_kernel(TreeArgs a) {
   bool dead = false;  // a sum of -1 marks a node that sees nothing
 #pragma unroll
   for (int y = 0; y < D / 16; ++y) o[y] = 0.f;
-#pragma unroll 2
+#pragma unroll 4
   for (int p = w; p < sp.parts; p += 4) {
-    const size_t slot = 2 * (size_t)(blockIdx.x + p) + (p == 0 ? sp.slot : 0);
-    const float* from = a.ws + slot * Plan::kPartFloats + row * (D + 2);
+    const float* from = ws.part(blockIdx.x + p, p == 0 ? sp.slot : 0, D) + row * (D + 2);
     const f32x2 ml = *reinterpret_cast<const f32x2*>(from + D);
     dead |= ml[1] == -1.f;
     const float top = fmaxf(m, ml[0]);
@@ -769,57 +815,59 @@ template <typename E, int D, typename Plan>
 hipError_t launch_join(const TreeArgs& a, hipStream_t s) {
   const hipError_t err = hipGetLastError();
   if (err != hipSuccess) return err;
-  tree_join_kernel<E, D, Plan><<<dim3(Plan::kGroups, Plan::kRows / 4), 256, 0, s>>>(a);
+  const dim3 grid(Plan::kGroups, (part_rows(a, Plan::kRows) + 3) / 4);
+  tree_join_kernel<E, D><<<grid, 256, 0, s>>>(a, Plan::kGroups, Plan::kRows);
   return hipGetLastError();
 }
 
-template <typename E, int D, int NT>
-struct ByKeys {  // waves split the keys
-  static size_t bytes() { return TreePlan<E, D, NT>::kBytes; }
+template <typename E, int D_, int NT>
+struct ByKeys {
+  typedef KeysPlan<E, D_, NT> Plan;
+  static constexpr int D = D_;
   static hipError_t launch(const TreeArgs& a, hipStream_t s) {
-    tree_kernel<E, D, NT><<<TreePlan<E, D, NT>::kGroups, 256, 0, s>>>(a);
-    return launch_join<E, D, TreePlan<E, D, NT>>(a, s);
+    tree_keys_kernel<E, D, NT><<<Plan::kGroups, 256, 0, s>>>(a);
+    return launch_join<E, D, Plan>(a, s);
   }
 };
 
-template <int D, int NT>
-struct ByRows {  // waves split the rows
-  typedef WidePlan<D, NT> Plan;
-  static size_t bytes() { return Plan::kBytes; }
+template <int D_, int NT>
+struct ByRows {
+  typedef RowsPlan<D_, NT> Plan;
+  static constexpr int D = D_;
   static hipError_t launch(const TreeArgs& a, hipStream_t s) {
     static const hipError_t ready = hipFuncSetAttribute(
-        reinterpret_cast<const void*>(tree_wide_kernel<D, NT>),
+        reinterpret_cast<const void*>(tree_rows_kernel<D, NT>),
         hipFuncAttributeMaxDynamicSharedMemorySize, (int)Plan::lds(kKvMaxRequests, kMaxNodes));
     if (ready != hipSuccess) return ready;
-    tree_wide_kernel<D, NT><<<Plan::kGroups, 256, Plan::lds(a.n, a.max_nodes), s>>>(a);
+    tree_rows_kernel<D, NT><<<Plan::kGroups, 256, Plan::lds(a.n, a.max_nodes), s>>>(a);
     return launch_join<uint16_t, D, Plan>(a, s);
   }
 };
 
+// The kernel by type, head size and the rows that the largest tree can have.
 template <int D, typename F>
 auto choose(int64_t rows, bool f32, F f) {
   if (f32) return rows <= 16 ? f(ByKeys<float, D, 1>{}) : f(ByKeys<float, D, 2>{});
-  if (rows <= 16) return f(ByKeys<uint16_t, D, 1>{});
-  if (rows <= S2MOE_TREE_WIDE) return f(ByKeys<uint16_t, D, 2>{});
-  if (rows <= 64) return f(ByRows<D, 1>{});
-  if (rows <= 128 || D == 128) return f(ByRows<D, 2>{});
-  return f(ByRows<D, 4>{});
+  return rows <= 16 ? f(ByKeys<uint16_t, D, 1>{}) : f(ByRows<D, D == 64 ? 4 : 2>{});
 }
 
 template <typename F>
-auto choose(int G, int D, bool f32, int max_nodes, F f) {
-  const int64_t rows = (int64_t)G * max_nodes;
-  return D == 64 ? choose<64>(rows, f32, f) : choose<128>(rows, f32, f);
+auto choose(const TreeArgs& a, F f) {
+  const int64_t rows = (int64_t)a.G * a.max_nodes;
+  return a.D == 64 ? choose<64>(rows, a.f32, f) : choose<128>(rows, a.f32, f);
 }
 
 }  // namespace
 
-size_t tree_attention_workspace(int Hq, int Hkv, int D, bool f32, int, int max_nodes) {
-  return choose(Hq / Hkv, D, f32, max_nodes, [](auto k) { return decltype(k)::bytes(); });
+size_t tree_attention_workspace(const TreeArgs& a) {
+  return choose(a, [&](auto k) {
+    typedef decltype(k) K;
+    return Workspace::bytes(K::Plan::kGroups, part_rows(a, K::Plan::kRows), K::D);
+  });
 }
 
 hipError_t launch_tree_attention(const TreeArgs& a, hipStream_t s) {
-  return choose(a.G, a.D, a.f32, a.max_nodes, [&](auto k) { return decltype(k)::launch(a, s); });
+  return choose(a, [&](auto k) { return decltype(k)::launch(a, s); });
 }
 
 }  // namespace s2moe
