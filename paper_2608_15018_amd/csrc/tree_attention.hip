@@ -258,6 +258,32 @@ __device__ __forceinline__ void raise(const float (&m)[NT], float (&shift)[NT], 
   }
 }
 
+// Where some rows do not see some keys: a weight of zero does not hide an infinity
+// or NaN, so those values count as zero, and where a weight meets one the row's sum
+// becomes NaN.
+template <int MT, int NT, int VC, typename frag>
+__device__ __forceinline__ void hide_nonfinite(frag (&V)[MT][VC], const frag (&P)[NT][VC], f32x4 (&O)[MT][NT]) {
+  bool bad = false;
+#pragma unroll
+  for (int mt = 0; mt < MT; ++mt)
+#pragma unroll
+    for (int y = 0; y < VC; ++y) bad |= any_nonfinite(V[mt][y]);
+  if (!__any(bad)) return;
+#pragma unroll
+  for (int mt = 0; mt < MT; ++mt) {
+#pragma unroll
+    for (int nt = 0; nt < NT; ++nt) {
+      f32x4 met = {};
+#pragma unroll
+      for (int y = 0; y < VC; ++y) met = mma(nonfinite_ones(V[mt][y]), P[nt][y], met);
+#pragma unroll
+      for (int e = 0; e < 4; ++e) O[mt][nt][e] = met[e] != 0.f ? NAN : O[mt][nt][e];
+    }
+#pragma unroll
+    for (int y = 0; y < VC; ++y) V[mt][y] = finite_only(V[mt][y]);
+  }
+}
+
 // D / 16 elements of an output row, times `inv`; zeros where inv is 0.
 template <typename E, int D>
 __device__ __forceinline__ void write_row(const TreeArgs& a, int first, int hk, int row, int od,
@@ -420,28 +446,7 @@ __global__ __launch_bounds__(256, (KeysPlan<E, D, NT>::kPerCu)) void tree_keys_k
           P[nt][0] = pack8(p[nt]);
         }
       }
-      if (masked) {
-        // A weight of zero does not hide an infinity or NaN: such values count
-        // as zero, and where a weight meets one the row's sum becomes NaN.
-#pragma unroll
-        for (int mt = 0; mt < MT; ++mt) {
-          bool bad = false;
-#pragma unroll
-          for (int y = 0; y < VC; ++y) bad |= any_nonfinite(V[mt][y]);
-          if (__any(bad)) {
-#pragma unroll
-            for (int nt = 0; nt < NT; ++nt) {
-              f32x4 met = {};
-#pragma unroll
-              for (int y = 0; y < VC; ++y) met = mma(nonfinite_ones(V[mt][y]), P[nt][y], met);
-#pragma unroll
-              for (int e = 0; e < 4; ++e) O[mt][nt][e] = met[e] != 0.f ? NAN : O[mt][nt][e];
-            }
-#pragma unroll
-            for (int y = 0; y < VC; ++y) V[mt][y] = finite_only(V[mt][y]);
-          }
-        }
-      }
+      if (masked) hide_nonfinite<MT, NT, VC>(V, P, O);
 #pragma unroll
       for (int mt = 0; mt < MT; ++mt)
 #pragma unroll
@@ -577,7 +582,7 @@ __device__ __forceinline__ void rows_stretch(const TreeArgs& a, const Stretch& r
   typedef RowsPlan<D, 1> Plan;
   constexpr int MT = D / 16, KC = D / 32, SK = Plan::kKeys, kLoads = Plan::kStage / 4096;
   constexpr int N1 = NA > 0 ? NA : 1;
-  const int lane = threadIdx.x & 63, w = wave_id(), n16 = lane & 15, g = lane >> 4;
+  const int lane = threadIdx.x & 63, n16 = lane & 15, g = lane >> 4;
   const auto swizzle = [](int x) { return D == 128 ? x & 15 : (x >> 1) & 7; };
   const int key_row = 8 * (n16 >> 2) + (n16 & 3);  // of the first 16-key tile; the second's is 4 on
   const float c = a.scale * 1.44269504088896340736f;
@@ -624,6 +629,9 @@ __device__ __forceinline__ void rows_stretch(const TreeArgs& a, const Stretch& r
             for (int nt = 0; nt < NA; ++nt) S[x][nt] = mma(k, q[y][nt], S[x][nt]);
           }
         }
+        bf16x8 V[MT][1];
+#pragma unroll
+        for (int mt = 0; mt < MT; ++mt) V[mt][0] = *reinterpret_cast<const bf16x8*>(vt + mt * 256);
         const bool masked = key0 + 32 > r.len;
         if (masked) mask_scores<NA>(S, tok, st.mask_s, key0 + 8 * g, r.len, r.total);
         float m[NA];
@@ -634,7 +642,7 @@ __device__ __forceinline__ void rows_stretch(const TreeArgs& a, const Stretch& r
           over |= m[nt] > limit[nt];
         }
         if (__any(over)) raise<MT, NA>(m, shift, limit, l, O);
-        bf16x8 P[NA];
+        bf16x8 P[NA][1];
 #pragma unroll
         for (int nt = 0; nt < NA; ++nt) {
           float p[8];
@@ -643,23 +651,13 @@ __device__ __forceinline__ void rows_stretch(const TreeArgs& a, const Stretch& r
             p[e] = exp2_fast(fmaf(S[e >> 2][nt][e & 3], c, -shift[nt]));
             l[nt] += p[e];
           }
-          P[nt] = pack8(p);
+          P[nt][0] = pack8(p);
         }
+        if (masked) hide_nonfinite<MT, NA, 1>(V, P, O);
 #pragma unroll
-        for (int mt = 0; mt < MT; ++mt) {
-          bf16x8 v = *reinterpret_cast<const bf16x8*>(vt + mt * 256);
-          if (masked && __any(any_nonfinite(v))) {
+        for (int mt = 0; mt < MT; ++mt)
 #pragma unroll
-            for (int nt = 0; nt < NA; ++nt) {
-              const f32x4 met = mma(nonfinite_ones(v), P[nt], f32x4{});
-#pragma unroll
-              for (int e = 0; e < 4; ++e) O[mt][nt][e] = met[e] != 0.f ? NAN : O[mt][nt][e];
-            }
-            v = finite_only(v);
-          }
-#pragma unroll
-          for (int nt = 0; nt < NA; ++nt) O[mt][nt] = mma(v, P[nt], O[mt][nt]);
-        }
+          for (int nt = 0; nt < NA; ++nt) O[mt][nt] = mma(V[mt][0], P[nt][0], O[mt][nt]);
       }
     }
   }
