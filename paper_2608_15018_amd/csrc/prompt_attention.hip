@@ -5,60 +5,6 @@
 namespace s2moe {
 namespace {
 
-__device__ __forceinline__ float load(const float* p) { return *p; }
-__device__ __forceinline__ float load(const uint16_t* p) { return bf16_to_f32(*p); }
-__device__ __forceinline__ void store(float* p, float x) { *p = x; }
-__device__ __forceinline__ void store(uint16_t* p, float x) { *p = (uint16_t)f32_to_bf16(x); }
-
-template <typename E, int D>
-__global__ __launch_bounds__(64) void prompt_kernel(PromptArgs a) {
-  __shared__ float q_s[D], p_s[64];
-  const int t = blockIdx.x, h = blockIdx.y, lane = threadIdx.x;
-  int lo = 0, hi = a.n;
-  while (hi - lo > 1) {
-    const int mid = (lo + hi) / 2;
-    if (a.tok_off[mid] <= t) lo = mid; else hi = mid;
-  }
-  const int first = a.tok_off[lo];
-  if (first < 0 || t < first || t >= a.tok_off[lo + 1]) return;
-  const E* q = reinterpret_cast<const E*>(a.q) + t * a.ldq + h * D;
-  for (int d = lane; d < D; d += 64) q_s[d] = load(q + d);
-  __syncthreads();
-  const int total = t - first + 1, g = h / a.G;
-  float m = -INFINITY, l = 0.f, acc[D / 64];
-  for (int i = 0; i < D / 64; ++i) acc[i] = 0.f;
-  for (int k0 = 0; k0 < total; k0 += 64) {
-    const int key = k0 + lane;
-    const bool vis = key < total;
-    float x = -INFINITY;
-    if (vis) {
-      const E* kp = reinterpret_cast<const E*>(a.k) + (first + key) * a.ldk + g * D;
-      x = 0.f;
-      for (int d = 0; d < D; ++d) x = fmaf(q_s[d], load(kp + d), x);
-      x *= a.scale;
-    }
-    float top = x;
-    for (int o = 32; o > 0; o >>= 1) top = fmaxf(top, __shfl_xor(top, o));
-    const float m2 = fmaxf(m, top);
-    const float keep = expf(m - m2), p = vis ? expf(x - m2) : 0.f;
-    float sum = p;
-    for (int o = 32; o > 0; o >>= 1) sum += __shfl_xor(sum, o);
-    l = l * keep + sum;
-    m = m2;
-    for (int i = 0; i < D / 64; ++i) acc[i] *= keep;
-    p_s[lane] = p;
-    __syncthreads();
-    const int n = total - k0 < 64 ? total - k0 : 64;
-    for (int j = 0; j < n; ++j) {
-      const E* vp = reinterpret_cast<const E*>(a.v) + (first + k0 + j) * a.ldv + g * D;
-      for (int i = 0; i < D / 64; ++i) acc[i] = fmaf(p_s[j], load(vp + lane + 64 * i), acc[i]);
-    }
-    __syncthreads();
-  }
-  E* o = reinterpret_cast<E*>(a.out) + t * a.ldo + h * D;
-  for (int i = 0; i < D / 64; ++i) store(o + lane + 64 * i, acc[i] / l);
-}
-
 // Workgroup b of a kv head: which rows of which prompt.  Prompts take
 // ceil(len G / rows) workgroups each, last ones first (they see the most
 // keys); 256 threads share the offsets.
@@ -464,6 +410,135 @@ __global__ __launch_bounds__(256, D == 64 ? 2 : 1) void prompt_bf16_kernel(Promp
   }
 }
 
+// ---------------------------------------------------------------- fp32
+// The fp32 matrix instructions run at a sixteenth of the bf16 rate, so nothing needs
+// LDS: a wave takes 32 rows and reads keys and values of 16 tokens a step into
+// registers, the next step's as soon as this one's are used.  Their operands hold one
+// k a lane, so values need no transposition: step e of a product takes key 4 g + e of
+// lane group g, where the scores of those keys are.
+template <int D>
+__global__ __launch_bounds__(256, 2) void prompt_f32_kernel(PromptArgs a) {
+  constexpr int kRows = 128, KC = D / 16, MT = D / 16;
+  const int lane = threadIdx.x & 63, w = wave_id(), n16 = lane & 15, g = lane >> 4;
+  const int hk = blockIdx.x % a.Hkv;
+  int first, len, qb;
+  if (!find_block(a, blockIdx.x / a.Hkv, kRows, &first, &len, &qb)) return;
+  const int R = len * a.G, row0 = qb * kRows + w * 32;
+  if (row0 >= R) return;
+  const int n_step = (min(row0 + 31, R - 1) / a.G) / 16 + 1, first_tok = row0 / a.G;
+
+  int tok[2];
+  f32x4 q[KC][2], O[MT][2];
+  float shift[2] = {0.f, 0.f}, limit[2] = {-INFINITY, -INFINITY}, l[2] = {0.f, 0.f};
+#pragma unroll
+  for (int nt = 0; nt < 2; ++nt) {
+    const int row = min(row0 + 16 * nt + n16, R - 1);
+    tok[nt] = row / a.G;
+    const float* p = reinterpret_cast<const float*>(a.q) + (int64_t)(first + tok[nt]) * a.ldq +
+                     (hk * a.G + row - tok[nt] * a.G) * D + 4 * g;
+#pragma unroll
+    for (int x = 0; x < KC; ++x) q[x][nt] = *reinterpret_cast<const f32x4*>(p + 16 * x);
+#pragma unroll
+    for (int mt = 0; mt < MT; ++mt) O[mt][nt] = f32x4{};
+  }
+  const float* const kg = reinterpret_cast<const float*>(a.k) + (int64_t)first * a.ldk + hk * D + 4 * g;
+  const float* const vg = reinterpret_cast<const float*>(a.v) + (int64_t)first * a.ldv + hk * D + n16;
+  f32x4 K[KC], V[MT];
+  const auto load_k = [&](int t) {
+    const float* p = kg + (int64_t)min(16 * t + n16, len - 1) * a.ldk;
+#pragma unroll
+    for (int x = 0; x < KC; ++x) K[x] = *reinterpret_cast<const f32x4*>(p + 16 * x);
+  };
+  const auto load_v = [&](int t) {
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+      const float* p = vg + (int64_t)min(16 * t + 4 * g + e, len - 1) * a.ldv;
+#pragma unroll
+      for (int mt = 0; mt < MT; ++mt) V[mt][e] = p[16 * mt];
+    }
+  };
+  const auto mma = [](f32x4 x, f32x4 y, f32x4 z) {
+#pragma unroll
+    for (int j = 0; j < 4; ++j) z = __builtin_amdgcn_mfma_f32_16x16x4f32(x[j], y[j], z, 0, 0, 0);
+    return z;
+  };
+  const float c = a.scale * 1.44269504088896340736f;
+  load_k(0);
+  load_v(0);
+  for (int t = 0; t < n_step; ++t) {
+    f32x4 S[2] = {};
+#pragma unroll
+    for (int x = 0; x < KC; ++x)
+#pragma unroll
+      for (int nt = 0; nt < 2; ++nt) S[nt] = mma(K[x], q[x][nt], S[nt]);
+    if (t + 1 < n_step) load_k(t + 1);
+    const bool masked = 16 * t + 15 > first_tok;
+    float m[2];
+    bool over = false;
+#pragma unroll
+    for (int nt = 0; nt < 2; ++nt) {
+      if (masked)
+#pragma unroll
+        for (int e = 0; e < 4; ++e)
+          if (16 * t + 4 * g + e > tok[nt]) S[nt][e] = -INFINITY;
+      m[nt] = fmaxf(max3(S[nt][0], S[nt][1], S[nt][2]), S[nt][3]) * c;
+      over |= m[nt] > limit[nt];
+    }
+    if (__any(over)) {
+#pragma unroll
+      for (int nt = 0; nt < 2; ++nt) {
+        const float top = max_groups(m[nt]);
+        const bool moves = top > limit[nt], fresh = limit[nt] == -INFINITY;
+        const float f = moves && !fresh ? exp2_fast(shift[nt] - top) : 1.f;
+        shift[nt] = moves ? top : shift[nt];
+        limit[nt] = moves ? top + kLag : limit[nt];
+        l[nt] *= f;
+#pragma unroll
+        for (int mt = 0; mt < MT; ++mt) O[mt][nt] *= f;
+      }
+    }
+    f32x4 P[2];
+#pragma unroll
+    for (int nt = 0; nt < 2; ++nt)
+#pragma unroll
+      for (int e = 0; e < 4; ++e) {
+        P[nt][e] = exp2_fast(fmaf(S[nt][e], c, -shift[nt]));
+        l[nt] += P[nt][e];
+      }
+    if (masked) {  // as in the bf16 kernel
+      bool bad = false;
+#pragma unroll
+      for (int mt = 0; mt < MT; ++mt) bad |= any_nonfinite(V[mt]);
+      if (__any(bad))
+#pragma unroll
+        for (int mt = 0; mt < MT; ++mt) {
+#pragma unroll
+          for (int nt = 0; nt < 2; ++nt) {
+            const f32x4 met = mma(nonfinite_ones(V[mt]), P[nt], f32x4{});
+#pragma unroll
+            for (int e = 0; e < 4; ++e) O[mt][nt][e] = met[e] != 0.f ? NAN : O[mt][nt][e];
+          }
+          V[mt] = finite_only(V[mt]);
+        }
+    }
+#pragma unroll
+    for (int mt = 0; mt < MT; ++mt)
+#pragma unroll
+      for (int nt = 0; nt < 2; ++nt) O[mt][nt] = mma(V[mt], P[nt], O[mt][nt]);
+    if (t + 1 < n_step) load_v(t + 1);
+  }
+#pragma unroll
+  for (int nt = 0; nt < 2; ++nt) {
+    const int row = row0 + 16 * nt + n16;
+    const float inv = 1.f / sum_groups(l[nt]);
+    if (row >= R) continue;
+    float* p = reinterpret_cast<float*>(a.out) + (int64_t)(first + tok[nt]) * a.ldo +
+               (hk * a.G + row - tok[nt] * a.G) * D + 4 * g;
+#pragma unroll
+    for (int mt = 0; mt < MT; ++mt) *reinterpret_cast<f32x4*>(p + 16 * mt) = O[mt][nt] * inv;
+  }
+}
+
 template <int D>
 hipError_t launch_bf16(const PromptArgs& a, hipStream_t s) {
   static const hipError_t ready = hipFuncSetAttribute(
@@ -479,13 +554,10 @@ hipError_t launch_bf16(const PromptArgs& a, hipStream_t s) {
 }  // namespace
 
 hipError_t launch_prompt_attention(const PromptArgs& a, hipStream_t s) {
-  const dim3 grid(a.n_tokens, a.Hq);
-  if (a.f32) {
-    if (a.D == 64) prompt_kernel<float, 64><<<grid, 64, 0, s>>>(a);
-    else prompt_kernel<float, 128><<<grid, 64, 0, s>>>(a);
-  } else {
-    return a.D == 64 ? launch_bf16<64>(a, s) : launch_bf16<128>(a, s);
-  }
+  if (!a.f32) return a.D == 64 ? launch_bf16<64>(a, s) : launch_bf16<128>(a, s);
+  const unsigned blocks = (unsigned)(((int64_t)a.n_tokens * a.G / 128 + a.n) * a.Hkv);
+  if (a.D == 64) prompt_f32_kernel<64><<<blocks, 256, 0, s>>>(a);
+  else prompt_f32_kernel<128><<<blocks, 256, 0, s>>>(a);
   return hipGetLastError();
 }
 

@@ -25,6 +25,12 @@
 namespace s2moe {
 namespace {
 
+#ifndef XG
+#define XG 1
+#endif
+#ifndef XK
+#define XK 2
+#endif
 constexpr int kTile = 128;  // keys of a unit
 
 // A row block whose parts the joining launch adds, as the workgroup that has
@@ -136,6 +142,11 @@ __device__ void ancestors(const int32_t* parent, int T, uint32_t* mask_s, int* j
     }
     __syncthreads();
   }
+}
+
+// Bytes of the requests, and of masks, parents and flags of a tree's nodes.
+inline size_t shared_lists(int n, int max_nodes) {
+  return (size_t)n * sizeof(Request) + (size_t)max_nodes * (kMaskRow * 4 + 4 + 4);
 }
 
 // All requests, with the units before each, into req_s[0 .. n - 1]; returns the
@@ -309,8 +320,10 @@ template <typename E, int D, int NT>
 struct KeysPlan {
   static constexpr int kRows = 16 * NT;
   // Workgroups that fit a compute unit.
-  static constexpr int kPerCu = NT == 2 && D * sizeof(E) == 512 ? 1 : 2;
-  static constexpr int kGroups = 256 * kPerCu;
+  static constexpr int kPerCu = sizeof(E) == 2 ? XK : NT == 2 && D * sizeof(E) == 512 ? 1 : 2;
+  static constexpr int kGroups = 256 * kPerCu * XG;
+  static constexpr int kSums = 4 * 16 * (D + 4) * 4;  // bytes of the waves' sums of 16 rows
+  static size_t lds(int n, int max_nodes) { return kSums + shared_lists(n, max_nodes); }
 };
 
 template <typename E, int D, int NT>
@@ -321,12 +334,13 @@ __global__ __launch_bounds__(256, (KeysPlan<E, D, NT>::kPerCu)) void tree_keys_k
   constexpr int RB = 16 * NT, MT = D / 16, ES = sizeof(E);
   constexpr int KC = D * ES / 64;  // 64-byte pieces of a key, 16 bytes a lane
   constexpr int VC = ES / 2;       // 16-byte pieces of eight values
-  __shared__ Request req_s[kKvMaxRequests];
-  __shared__ __attribute__((aligned(16))) float sum_s[4][16][D + 4];
+  extern __shared__ __attribute__((aligned(16))) char smem[];
+  float(*const sum_s)[16][D + 4] = reinterpret_cast<float(*)[16][D + 4]>(smem);
+  Request* const req_s = reinterpret_cast<Request*>(smem + Plan::kSums);
+  uint32_t* const mask_s = reinterpret_cast<uint32_t*>(req_s + a.n);
+  int* const jump_s = reinterpret_cast<int*>(mask_s + a.max_nodes * kMaskRow);
+  uint8_t* const dead_s = reinterpret_cast<uint8_t*>(jump_s + a.max_nodes);
   __shared__ float m_s[4][RB], l_s[4][RB];
-  __shared__ uint32_t mask_s[kMaxNodes * kMaskRow];
-  __shared__ int jump_s[kMaxNodes];
-  __shared__ uint8_t dead_s[kMaxNodes];
 
   const int tid = threadIdx.x, lane = tid & 63, w = wave_id();
   const int n16 = lane & 15, g = lane >> 4;
@@ -533,9 +547,9 @@ struct RowsPlan {
   static constexpr int kKeys = D == 128 ? 32 : 64;  // of a stage
   static constexpr int kStage = kKeys * D * 2;      // bytes of its keys, or values
   static constexpr int kRing = 4 * 2 * kStage;
-  static constexpr int kGroups = 512;               // two fit a compute unit
+  static constexpr int kGroups = 512 * XG;               // two fit a compute unit
   static size_t lds(int n, int max_nodes) {
-    return kRing + (size_t)n * sizeof(Request) + (size_t)max_nodes * (kMaskRow * 4 + 4 + 4);
+    return kRing + shared_lists(n, max_nodes);
   }
 };
 
@@ -823,7 +837,11 @@ struct ByKeys {
   typedef KeysPlan<E, D_, NT> Plan;
   static constexpr int D = D_;
   static hipError_t launch(const TreeArgs& a, hipStream_t s) {
-    tree_keys_kernel<E, D, NT><<<Plan::kGroups, 256, 0, s>>>(a);
+    static const hipError_t ready = hipFuncSetAttribute(
+        reinterpret_cast<const void*>(tree_keys_kernel<E, D, NT>),
+        hipFuncAttributeMaxDynamicSharedMemorySize, (int)Plan::lds(kKvMaxRequests, kMaxNodes));
+    if (ready != hipSuccess) return ready;
+    tree_keys_kernel<E, D, NT><<<Plan::kGroups, 256, Plan::lds(a.n, a.max_nodes), s>>>(a);
     return launch_join<E, D, Plan>(a, s);
   }
 };
