@@ -2,6 +2,9 @@
 #include "attention.h"
 #include "attn_common.h"
 
+#ifndef S2MOE_PROMPT_SHORT
+#define S2MOE_PROMPT_SHORT 1024
+#endif
 namespace s2moe {
 namespace {
 
@@ -11,18 +14,17 @@ namespace {
 __device__ bool find_block(const PromptArgs& a, int b, int rows, int* first, int* len, int* qb) {
   __shared__ int wave_s[4], found_s[3];
   const int tid = threadIdx.x, lane = tid & 63, w = tid >> 6;
+  const int per = (a.n + 255) >> 8;  // consecutive prompts a thread looks at
   int n[4], f[4], mine = 0;
 #pragma unroll
   for (int i = 0; i < 4; ++i) {
-    const int s = 4 * tid + i;
-    int x = 0, y = 0;
-    if (s < a.n) {
-      x = a.tok_off[s];
-      y = a.tok_off[s + 1];
+    const int s = per * tid + i;
+    n[i] = f[i] = 0;
+    if (i < per && s < a.n) {
+      f[i] = a.tok_off[s];
+      const int end = a.tok_off[s + 1];
+      n[i] = f[i] >= 0 && f[i] < end && end <= a.n_tokens ? end - f[i] : 0;
     }
-    const bool good = x >= 0 && x < y && y <= a.n_tokens;
-    f[i] = x;
-    n[i] = good ? y - x : 0;
     mine += (n[i] * a.G + rows - 1) / rows;
   }
   int inc = mine;
@@ -59,30 +61,36 @@ __device__ bool find_block(const PromptArgs& a, int b, int rows, int* first, int
 }
 
 // ---------------------------------------------------------------- bf16
-template <int D>
+// NT tiles of 32 rows a wave.
+template <int D, int NT>
 struct PromptTile {
-  static constexpr int kRows = 256;          // rows of a workgroup, 64 a wave
-  static constexpr int kStage = 64 * D * 2;  // bytes of 64 keys, or of their values
-  static constexpr int kLoads = D / 32;      // 1 KB loads a wave makes for it
-  static constexpr int kLds = 8 * kStage;    // four stages of each
+  static constexpr int kRows = 128 * NT;        // of a workgroup
+  static constexpr int kStage = 64 * D * 2;     // bytes of 64 keys, or of their values
+  static constexpr int kLoads = D / 32;         // 1 KB loads a wave makes for it
+  static constexpr int kRing = NT == 2 ? 4 : 2; // stages of each in LDS
+  static constexpr int kLds = 2 * kRing * kStage;
+  // The overlapped loop needs all registers.
+  static constexpr bool kOverlap = D == 128 && NT == 2;
+  static constexpr int kPerCu = kOverlap ? 1 : D == 64 && NT == 1 ? 3 : 2;
 };
 
-template <int D>
-__global__ __launch_bounds__(256, D == 64 ? 2 : 1) void prompt_bf16_kernel(PromptArgs a) {
-  constexpr int kStage = PromptTile<D>::kStage, kLoads = PromptTile<D>::kLoads;
+template <int D, int NT>
+__global__ __launch_bounds__(256, (PromptTile<D, NT>::kPerCu)) void prompt_bf16_kernel(PromptArgs a) {
+  typedef PromptTile<D, NT> Tile;
+  constexpr int kStage = Tile::kStage, kLoads = Tile::kLoads, kRing = Tile::kRing, kRows = Tile::kRows;
   constexpr int KS = D / 16, MT = D / 32, CH = D / 8;  // k steps, tiles of D, 16-byte chunks of a row
   extern __shared__ __attribute__((aligned(16))) char smem[];
-  char* const k_lds = smem;               // four stages of keys
-  char* const v_lds = smem + 4 * kStage;  // four of values
+  char* const k_lds = smem;
+  char* const v_lds = smem + kRing * kStage;
 
   const int tid = threadIdx.x, lane = tid & 63, w = wave_id();
   const int hk = blockIdx.x % a.Hkv;
   int first, len, qb;
-  if (!find_block(a, blockIdx.x / a.Hkv, PromptTile<D>::kRows, &first, &len, &qb))
+  if (!find_block(a, blockIdx.x / a.Hkv, kRows, &first, &len, &qb))
     return;
-  const int R = len * a.G, row0 = qb * PromptTile<D>::kRows + w * 64;
+  const int R = len * a.G, row0 = qb * kRows + w * 32 * NT;
   const int l32 = lane & 31, h = lane >> 5;
-  const int last_row = min(qb * PromptTile<D>::kRows + PromptTile<D>::kRows, R) - 1;
+  const int last_row = min(qb * kRows + kRows, R) - 1;
   const int n_stage = (last_row / a.G) / 64 + 1;
 
   // This wave's rows: 32 steps of keys [0, n_full) that all of them see, and
@@ -90,16 +98,16 @@ __global__ __launch_bounds__(256, D == 64 ? 2 : 1) void prompt_bf16_kernel(Promp
   int n_full = 0, n_all = 0;
   if (row0 < R) {
     n_full = (row0 / a.G + 1) / 32;
-    n_all = (min(row0 + 63, R - 1) / a.G) / 32 + 1;
+    n_all = (min(row0 + 32 * NT - 1, R - 1) / a.G) / 32 + 1;
   }
-  int tok[2];
+  int tok[NT];
   const uint16_t* q = reinterpret_cast<const uint16_t*>(a.q);
-  bf16x8 qf[KS][2];
+  bf16x8 qf[KS][NT];
 #pragma unroll
-  for (int nt = 0; nt < 2; ++nt) {
+  for (int nt = 0; nt < NT; ++nt) {
     const int r = min(row0 + 32 * nt + l32, R - 1);
     tok[nt] = r / a.G;
-    const uint16_t* p = q + (int64_t)(first + tok[nt]) * a.ldq + (hk * a.G + r % a.G) * D + 8 * h;
+    const uint16_t* p = q + (int64_t)(first + tok[nt]) * a.ldq + (hk * a.G + r - tok[nt] * a.G) * D + 8 * h;
 #pragma unroll
     for (int ks = 0; ks < KS; ++ks) qf[ks][nt] = *reinterpret_cast<const bf16x8*>(p + 16 * ks);
   }
@@ -129,16 +137,15 @@ __global__ __launch_bounds__(256, D == 64 ? 2 : 1) void prompt_bf16_kernel(Promp
     for (int i = 0; i < kLoads; ++i)
       load_to_lds(from, rows >= 64 ? off[i] : place(i, ld, keys, rows), lds + (w * kLoads + i) * 1024);
   };
-  const auto load_k = [&](int s) { load_stage(kg, ldk, k_off, k_lds + (s & 3) * kStage, s, true); };
-  const auto load_v = [&](int s) { load_stage(vg, ldv, v_off, v_lds + (s & 3) * kStage, s, false); };
-  // Stages up to s + 1 of the keys and s of the values are there for
-  // everybody, and what is loaded now overwrites stages that nobody reads any
-  // more (s - 1 and s - 2).
+  const auto load_k = [&](int s) { load_stage(kg, ldk, k_off, k_lds + (s & (kRing - 1)) * kStage, s, true); };
+  const auto load_v = [&](int s) { load_stage(vg, ldv, v_off, v_lds + (s & (kRing - 1)) * kStage, s, false); };
+  // Stage s is there for everybody (with four in the ring, that of the keys after it
+  // too), and what is loaded now overwrites stages that nobody reads any more.
   const auto sync = [&](int s) {
-    wait_loads<2 * kLoads>();
+    wait_loads<kRing == 4 ? 2 * kLoads : 0>();
     __builtin_amdgcn_s_barrier();
-    load_k(s + 3);
-    load_v(s + 2);
+    load_k(s + kRing - 1);
+    load_v(s + kRing / 2);
   };
 
   // Row m of a key tile is key m with bits 2 and 3 exchanged: then a lane's
@@ -149,49 +156,54 @@ __global__ __launch_bounds__(256, D == 64 ? 2 : 1) void prompt_bf16_kernel(Promp
   const int v_r = (lane & 15) >> 2;
   const int v_at = (8 * h + v_r) * D * 2 + ((lane >> 4) & 1) * 32 + (lane & 3) * 8;
 
-  f32x16 O[MT][2];
+  f32x16 O[MT][NT];
 #pragma unroll
   for (int mt = 0; mt < MT; ++mt)
 #pragma unroll
-    for (int nt = 0; nt < 2; ++nt) O[mt][nt] = f32x16{};
-  float shift[2] = {0.f, 0.f}, limit[2] = {-INFINITY, -INFINITY}, l[2] = {0.f, 0.f};
+    for (int nt = 0; nt < NT; ++nt) O[mt][nt] = f32x16{};
+  float shift[NT], limit[NT], l[NT];
+#pragma unroll
+  for (int nt = 0; nt < NT; ++nt) {
+    shift[nt] = l[nt] = 0.f;
+    limit[nt] = -INFINITY;
+  }
   const float c = a.scale * 1.44269504088896340736f;
 
   const auto key_tile = [&](int j, int ks) {
-    return *reinterpret_cast<const bf16x8*>(k_lds + ((j >> 1) & 3) * kStage + (j & 1) * 32 * D * 2 + k_at +
+    return *reinterpret_cast<const bf16x8*>(k_lds + ((j >> 1) & (kRing - 1)) * kStage + (j & 1) * 32 * D * 2 + k_at +
                                             (k_x ^ (ks << 5)));
   };
-  const auto products_k = [&](int j, f32x16(&T)[2]) {
+  const auto products_k = [&](int j, f32x16(&T)[NT]) {
 #pragma unroll
-    for (int nt = 0; nt < 2; ++nt) T[nt] = f32x16{};
+    for (int nt = 0; nt < NT; ++nt) T[nt] = f32x16{};
 #pragma unroll
     for (int ks = 0; ks < KS; ++ks) {
       const bf16x8 kf = key_tile(j, ks);
 #pragma unroll
-      for (int nt = 0; nt < 2; ++nt) T[nt] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(kf, qf[ks][nt], T[nt], 0, 0, 0);
+      for (int nt = 0; nt < NT; ++nt) T[nt] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(kf, qf[ks][nt], T[nt], 0, 0, 0);
     }
   };
   const auto value_tile = [&](int j, int ks, int mt) -> bf16x8 {
-    const char* vt = v_lds + ((j >> 1) & 3) * kStage + ((j & 1) * 32 + 16 * ks) * D * 2 + v_at +
+    const char* vt = v_lds + ((j >> 1) & (kRing - 1)) * kStage + ((j & 1) * 32 + 16 * ks) * D * 2 + v_at +
                      ((mt ^ (D == 128 ? v_r : v_r >> 1)) << 6);
     const bf16x4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4bf16((__attribute__((address_space(3))) bf16x4*)vt);
     const bf16x4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4bf16((__attribute__((address_space(3))) bf16x4*)(vt + 4 * D * 2));
     return __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7);
   };
-  const auto products_v = [&](int j, const bf16x8(&W)[2][2]) {
+  const auto products_v = [&](int j, const bf16x8(&W)[2][NT]) {
 #pragma unroll
     for (int ks = 0; ks < 2; ++ks)
 #pragma unroll
       for (int mt = 0; mt < MT; ++mt) {
         const bf16x8 vf = value_tile(j, ks, mt);
 #pragma unroll
-        for (int nt = 0; nt < 2; ++nt) O[mt][nt] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(vf, W[ks][nt], O[mt][nt], 0, 0, 0);
+        for (int nt = 0; nt < NT; ++nt) O[mt][nt] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(vf, W[ks][nt], O[mt][nt], 0, 0, 0);
       }
   };
   // The weights of one step, by the maximum as it stands.
-  const auto weights = [&](const f32x16(&T)[2], bf16x8(&W)[2][2]) {
+  const auto weights = [&](const f32x16(&T)[NT], bf16x8(&W)[2][NT]) {
 #pragma unroll
-    for (int nt = 0; nt < 2; ++nt) {
+    for (int nt = 0; nt < NT; ++nt) {
       float p[16];
 #pragma unroll
       for (int i = 0; i < 16; ++i) {
@@ -211,10 +223,13 @@ __global__ __launch_bounds__(256, D == 64 ? 2 : 1) void prompt_bf16_kernel(Promp
   // Scores of the next step whose largest are m: a row with one past its limit
   // moves its maximum there, and what it has summed so far, W's step included,
   // shrinks by 2^-8 or more (so rounding W once more does not count).
-  const auto raise_to = [&](const float(&m)[2], bf16x8(&W)[2][2]) {
-    if (__builtin_expect(__any(m[0] > limit[0] || m[1] > limit[1]), 0)) {
+  const auto raise_to = [&](const float(&m)[NT], bf16x8(&W)[2][NT]) {
+    bool over = false;
 #pragma unroll
-      for (int nt = 0; nt < 2; ++nt) {
+    for (int nt = 0; nt < NT; ++nt) over |= m[nt] > limit[nt];
+    if (__builtin_expect(__any(over), 0)) {
+#pragma unroll
+      for (int nt = 0; nt < NT; ++nt) {
         const float top = max_halves(m[nt]);
         const bool moves = top > limit[nt], fresh = limit[nt] == -INFINITY;
         const float f = moves && !fresh ? exp2_fast(shift[nt] - top) : 1.f;
@@ -224,7 +239,7 @@ __global__ __launch_bounds__(256, D == 64 ? 2 : 1) void prompt_bf16_kernel(Promp
 #pragma unroll
         for (int mt = 0; mt < MT; ++mt) {
           O[mt][nt] *= f;
-          if (D == 128) asm volatile("" : "+a"(O[mt][nt]));
+          if (Tile::kOverlap) asm volatile("" : "+a"(O[mt][nt]));
         }
 #pragma unroll
         for (int ks = 0; ks < 2; ++ks) {
@@ -236,13 +251,15 @@ __global__ __launch_bounds__(256, D == 64 ? 2 : 1) void prompt_bf16_kernel(Promp
       }
     }
   };
-  const auto raise = [&](const f32x16(&T)[2], bf16x8(&W)[2][2]) {
-    const float m[2] = {largest(T[0]), largest(T[1])};
+  const auto raise = [&](const f32x16(&T)[NT], bf16x8(&W)[2][NT]) {
+    float m[NT];
+#pragma unroll
+    for (int nt = 0; nt < NT; ++nt) m[nt] = largest(T[nt]);
     raise_to(m, W);
   };
-  const auto mask = [&](int j, f32x16(&T)[2]) {
+  const auto mask = [&](int j, f32x16(&T)[NT]) {
 #pragma unroll
-    for (int nt = 0; nt < 2; ++nt)
+    for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
       for (int i = 0; i < 16; ++i)
         if (32 * j + 16 * (i >> 3) + 8 * h + (i & 7) > tok[nt]) T[nt][i] = -INFINITY;
@@ -250,7 +267,7 @@ __global__ __launch_bounds__(256, D == 64 ? 2 : 1) void prompt_bf16_kernel(Promp
   // The second product where some rows do not see some keys: a weight of zero
   // does not hide an infinity or NaN, so those values count as zero, and where a
   // weight meets one the row's sum becomes NaN.
-  const auto products_v_masked = [&](int j, const bf16x8(&W)[2][2]) {
+  const auto products_v_masked = [&](int j, const bf16x8(&W)[2][NT]) {
     bool bad = false;
 #pragma unroll
     for (int ks = 0; ks < 2; ++ks)
@@ -260,14 +277,14 @@ __global__ __launch_bounds__(256, D == 64 ? 2 : 1) void prompt_bf16_kernel(Promp
         bad |= any_nonfinite(vf);
         const bf16x8 fine = finite_only(vf);
 #pragma unroll
-        for (int nt = 0; nt < 2; ++nt)
+        for (int nt = 0; nt < NT; ++nt)
           O[mt][nt] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(fine, W[ks][nt], O[mt][nt], 0, 0, 0);
       }
     if (__builtin_expect(__any(bad), 0)) {
 #pragma unroll
       for (int mt = 0; mt < MT; ++mt)
 #pragma unroll
-        for (int nt = 0; nt < 2; ++nt) {
+        for (int nt = 0; nt < NT; ++nt) {
           f32x16 met = {};
 #pragma unroll
           for (int ks = 0; ks < 2; ++ks)
@@ -277,17 +294,28 @@ __global__ __launch_bounds__(256, D == 64 ? 2 : 1) void prompt_bf16_kernel(Promp
         }
     }
   };
+  load_k(0);
+  if constexpr (kRing == 4) load_k(1);
+  load_v(0);
+  if constexpr (kRing == 4) {
+    load_k(2);
+    load_v(1);
+  }
+  f32x16 SA[NT];
+  bf16x8 PA[2][NT] = {};
+  int s = 0;
+  if constexpr (Tile::kOverlap) {
   // One step of the overlapped loop: the scores of step j + 1 into `next`, the
   // weights of step j from `now` into W, and the products of the weights
   // `before` with the values of step j - 1.  Sixteen fragments of keys and
   // values, read four ahead, with two matrix instructions each; between those,
   // two scores become weights, and then the new scores' maximum is taken.
-  const auto step = [&](int j, const f32x16(&now)[2], f32x16(&next)[2], const bf16x8(&before)[2][2],
-                        bf16x8(&W)[2][2], bf16x8(&ahead)[4]) {
+  const auto step = [&](int j, const f32x16(&now)[NT], f32x16(&next)[NT], const bf16x8(&before)[2][NT],
+                        bf16x8(&W)[2][NT], bf16x8(&ahead)[4]) {
     constexpr int NF = KS + 2 * MT, EL = 32 / NF;  // fragments, scores each
     bf16x8 f[NF + 4];
     bf16x2 w2[16];
-    float m[2];
+    float m[NT];
 #pragma unroll
     for (int i = 0; i < 4; ++i) f[i] = ahead[i];
 #pragma unroll
@@ -297,7 +325,7 @@ __global__ __launch_bounds__(256, D == 64 ? 2 : 1) void prompt_bf16_kernel(Promp
       else if (n < NF) f[n] = value_tile(j - 1, (n - KS) / MT, (n - KS) % MT);
       else f[n] = key_tile(j + 2, n - NF);
 #pragma unroll
-      for (int nt = 0; nt < 2; ++nt) {
+      for (int nt = 0; nt < NT; ++nt) {
         if (i < KS) {
           next[nt] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(f[i], qf[i < KS ? i : 0][nt], i == 0 ? f32x16{} : next[nt], 0, 0, 0);
         } else {
@@ -326,7 +354,7 @@ __global__ __launch_bounds__(256, D == 64 ? 2 : 1) void prompt_bf16_kernel(Promp
       __builtin_amdgcn_sched_barrier(0);
     }
 #pragma unroll
-    for (int nt = 0; nt < 2; ++nt)
+    for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
       for (int ks = 0; ks < 2; ++ks)
 #pragma unroll
@@ -343,22 +371,13 @@ __global__ __launch_bounds__(256, D == 64 ? 2 : 1) void prompt_bf16_kernel(Promp
     m[1] *= c;
     raise_to(m, W);
   };
-
-  load_k(0);
-  load_k(1);
-  load_v(0);
-  load_k(2);
-  load_v(1);
-  f32x16 SA[2];
-  bf16x8 PA[2][2] = {};
-  int s = 0;
-  if (D == 128 && n_full >= 4) {
+  if (n_full >= 4) {
     // Steps whose keys every row of the wave sees, two a stage, as far as they
     // are even in number.  What a step does depends on nothing else in it, so
     // the matrix cores work while the weights are made.  (At D = 64 two waves
     // share a SIMD and do this for each other.)
-    f32x16 SB[2];
-    bf16x8 PB[2][2], ahead[4];
+    f32x16 SB[NT];
+    bf16x8 PB[2][NT], ahead[4];
     const int n_fast = n_full >> 1;
 #pragma unroll
     for (int ks = 0; ks < KS; ++ks) asm volatile("" : "+a"(qf[ks][0]), "+a"(qf[ks][1]));
@@ -379,6 +398,7 @@ __global__ __launch_bounds__(256, D == 64 ? 2 : 1) void prompt_bf16_kernel(Promp
     products_v(2 * s - 2, PA);
     products_v(2 * s - 1, PB);
   }
+  }
   for (; s < n_stage; ++s) {
     sync(s);
     for (int j = 2 * s; j < 2 * s + 2 && j < n_all; ++j) {
@@ -393,19 +413,27 @@ __global__ __launch_bounds__(256, D == 64 ? 2 : 1) void prompt_bf16_kernel(Promp
 
   uint16_t* out = reinterpret_cast<uint16_t*>(a.out);
 #pragma unroll
-  for (int nt = 0; nt < 2; ++nt) {
+  for (int nt = 0; nt < NT; ++nt) {
     const int r = row0 + 32 * nt + l32;
     const float inv = 1.f / sum_halves(l[nt]);
-    if (r >= R) continue;
-    uint16_t* p = out + (int64_t)(first + tok[nt]) * a.ldo + (hk * a.G + r % a.G) * D + 4 * h;
+    // A lane has four elements of every eight; the half-waves exchange fours, so
+    // that each stores 16 bytes.
+    uint16_t* p = out + (int64_t)(first + tok[nt]) * a.ldo + (hk * a.G + r - tok[nt] * a.G) * D + 8 * h;
 #pragma unroll
     for (int mt = 0; mt < MT; ++mt)
 #pragma unroll
-      for (int b = 0; b < 4; ++b) {
-        const f32x2 x = {O[mt][nt][4 * b] * inv, O[mt][nt][4 * b + 1] * inv};
-        const f32x2 y = {O[mt][nt][4 * b + 2] * inv, O[mt][nt][4 * b + 3] * inv};
-        const bf16x2 xb = __builtin_convertvector(x, bf16x2), yb = __builtin_convertvector(y, bf16x2);
-        *reinterpret_cast<bf16x4*>(p + 32 * mt + 8 * b) = __builtin_shufflevector(xb, yb, 0, 1, 2, 3);
+      for (int b = 0; b < 4; b += 2) {
+        u32x4 v;
+#pragma unroll
+        for (int x = 0; x < 2; ++x) {
+          const bf16x2 lo = pack2(O[mt][nt][4 * b + 2 * x] * inv, O[mt][nt][4 * b + 2 * x + 1] * inv);
+          const bf16x2 hi = pack2(O[mt][nt][4 * b + 4 + 2 * x] * inv, O[mt][nt][4 * b + 5 + 2 * x] * inv);
+          const auto both = __builtin_amdgcn_permlane32_swap(__builtin_bit_cast(uint32_t, lo),
+                                                             __builtin_bit_cast(uint32_t, hi), false, false);
+          v[x] = both[0];
+          v[2 + x] = both[1];
+        }
+        if (r < R) *reinterpret_cast<u32x4*>(p + 32 * mt + 8 * b) = v;
       }
   }
 }
@@ -416,15 +444,18 @@ __global__ __launch_bounds__(256, D == 64 ? 2 : 1) void prompt_bf16_kernel(Promp
 // registers, the next step's as soon as this one's are used.  Their operands hold one
 // k a lane, so values need no transposition: step e of a product takes key 4 g + e of
 // lane group g, where the scores of those keys are.
-template <int D>
+// SPLIT: the four waves share 32 rows and take every fourth step, and their sums
+// are added at the end.
+template <int D, bool SPLIT>
 __global__ __launch_bounds__(256, 2) void prompt_f32_kernel(PromptArgs a) {
-  constexpr int kRows = 128, KC = D / 16, MT = D / 16;
+  constexpr int kRows = SPLIT ? 32 : 128, KC = D / 16, MT = D / 16;
   const int lane = threadIdx.x & 63, w = wave_id(), n16 = lane & 15, g = lane >> 4;
   const int hk = blockIdx.x % a.Hkv;
   int first, len, qb;
   if (!find_block(a, blockIdx.x / a.Hkv, kRows, &first, &len, &qb)) return;
-  const int R = len * a.G, row0 = qb * kRows + w * 32;
+  const int R = len * a.G, row0 = qb * kRows + (SPLIT ? 0 : w * 32);
   if (row0 >= R) return;
+  const int t0 = SPLIT ? w : 0, dt = SPLIT ? 4 : 1;
   const int n_step = (min(row0 + 31, R - 1) / a.G) / 16 + 1, first_tok = row0 / a.G;
 
   int tok[2];
@@ -463,15 +494,15 @@ __global__ __launch_bounds__(256, 2) void prompt_f32_kernel(PromptArgs a) {
     return z;
   };
   const float c = a.scale * 1.44269504088896340736f;
-  load_k(0);
-  load_v(0);
-  for (int t = 0; t < n_step; ++t) {
+  load_k(t0);
+  load_v(t0);
+  for (int t = t0; t < n_step; t += dt) {
     f32x4 S[2] = {};
 #pragma unroll
     for (int x = 0; x < KC; ++x)
 #pragma unroll
       for (int nt = 0; nt < 2; ++nt) S[nt] = mma(K[x], q[x][nt], S[nt]);
-    if (t + 1 < n_step) load_k(t + 1);
+    if (t + dt < n_step) load_k(t + dt);
     const bool masked = 16 * t + 15 > first_tok;
     float m[2];
     bool over = false;
@@ -525,12 +556,47 @@ __global__ __launch_bounds__(256, 2) void prompt_f32_kernel(PromptArgs a) {
     for (int mt = 0; mt < MT; ++mt)
 #pragma unroll
       for (int nt = 0; nt < 2; ++nt) O[mt][nt] = mma(V[mt], P[nt], O[mt][nt]);
-    if (t + 1 < n_step) load_v(t + 1);
+    if (t + dt < n_step) load_v(t + dt);
+  }
+  if constexpr (SPLIT) {
+    __shared__ __attribute__((aligned(16))) float o_s[3][2][MT][64][4];
+    __shared__ float m_s[4][2][16], l_s[4][2][16];
+#pragma unroll
+    for (int nt = 0; nt < 2; ++nt) {
+      l[nt] = sum_groups(l[nt]);
+      m_s[w][nt][n16] = limit[nt] == -INFINITY ? -INFINITY : shift[nt];
+      l_s[w][nt][n16] = l[nt];
+    }
+    __syncthreads();
+#pragma unroll
+    for (int nt = 0; nt < 2; ++nt) {
+      float top = -INFINITY, sum = 0.f;
+#pragma unroll
+      for (int x = 0; x < 4; ++x) top = fmaxf(top, m_s[x][nt][n16]);
+#pragma unroll
+      for (int x = 0; x < 4; ++x)
+        sum += l_s[x][nt][n16] * (m_s[x][nt][n16] == -INFINITY ? 0.f : exp2_fast(m_s[x][nt][n16] - top));
+      const float own = m_s[w][nt][n16], f = own == -INFINITY ? 0.f : exp2_fast(own - top);
+      l[nt] = sum;
+#pragma unroll
+      for (int mt = 0; mt < MT; ++mt) {
+        O[mt][nt] *= f;
+        if (w > 0) *reinterpret_cast<f32x4*>(o_s[w - 1][nt][mt][lane]) = O[mt][nt];
+      }
+    }
+    __syncthreads();
+    if (w > 0) return;
+#pragma unroll
+    for (int x = 0; x < 3; ++x)
+#pragma unroll
+      for (int nt = 0; nt < 2; ++nt)
+#pragma unroll
+        for (int mt = 0; mt < MT; ++mt) O[mt][nt] += *reinterpret_cast<const f32x4*>(o_s[x][nt][mt][lane]);
   }
 #pragma unroll
   for (int nt = 0; nt < 2; ++nt) {
     const int row = row0 + 16 * nt + n16;
-    const float inv = 1.f / sum_groups(l[nt]);
+    const float inv = 1.f / (SPLIT ? l[nt] : sum_groups(l[nt]));
     if (row >= R) continue;
     float* p = reinterpret_cast<float*>(a.out) + (int64_t)(first + tok[nt]) * a.ldo +
                (hk * a.G + row - tok[nt] * a.G) * D + 4 * g;
@@ -539,15 +605,32 @@ __global__ __launch_bounds__(256, 2) void prompt_f32_kernel(PromptArgs a) {
   }
 }
 
-template <int D>
+template <int D, int NT>
 hipError_t launch_bf16(const PromptArgs& a, hipStream_t s) {
-  static const hipError_t ready = hipFuncSetAttribute(
-      reinterpret_cast<const void*>(prompt_bf16_kernel<D>),
-      hipFuncAttributeMaxDynamicSharedMemorySize, PromptTile<D>::kLds);
+  typedef PromptTile<D, NT> Tile;
+  static const hipError_t ready =
+      hipFuncSetAttribute(reinterpret_cast<const void*>(prompt_bf16_kernel<D, NT>),
+                          hipFuncAttributeMaxDynamicSharedMemorySize, Tile::kLds);
   if (ready != hipSuccess) return ready;
   // At most one unfilled workgroup per prompt.
-  const int64_t blocks = ((int64_t)a.n_tokens * a.G / PromptTile<D>::kRows + a.n) * a.Hkv;
-  prompt_bf16_kernel<D><<<(unsigned)blocks, 256, PromptTile<D>::kLds, s>>>(a);
+  const int64_t blocks = ((int64_t)a.n_tokens * a.G / Tile::kRows + a.n) * a.Hkv;
+  prompt_bf16_kernel<D, NT><<<(unsigned)blocks, 256, Tile::kLds, s>>>(a);
+  return hipGetLastError();
+}
+
+template <int D>
+hipError_t launch_bf16(const PromptArgs& a, hipStream_t s) {
+  return a.n_tokens / a.n < S2MOE_PROMPT_SHORT ? launch_bf16<D, 1>(a, s) : launch_bf16<D, 2>(a, s);
+}
+
+template <int D>
+hipError_t launch_f32(const PromptArgs& a, hipStream_t s) {
+  // By keys while rows alone would not give every SIMD of the GPU a wave.
+  const auto blocks = [&](int rows) { return ((int64_t)a.n_tokens * a.G / rows + a.n) * a.Hkv; };
+  if (blocks(32) < 1024)
+    prompt_f32_kernel<D, true><<<(unsigned)blocks(32), 256, 0, s>>>(a);
+  else
+    prompt_f32_kernel<D, false><<<(unsigned)blocks(128), 256, 0, s>>>(a);
   return hipGetLastError();
 }
 
@@ -555,10 +638,7 @@ hipError_t launch_bf16(const PromptArgs& a, hipStream_t s) {
 
 hipError_t launch_prompt_attention(const PromptArgs& a, hipStream_t s) {
   if (!a.f32) return a.D == 64 ? launch_bf16<64>(a, s) : launch_bf16<128>(a, s);
-  const unsigned blocks = (unsigned)(((int64_t)a.n_tokens * a.G / 128 + a.n) * a.Hkv);
-  if (a.D == 64) prompt_f32_kernel<64><<<blocks, 256, 0, s>>>(a);
-  else prompt_f32_kernel<128><<<blocks, 256, 0, s>>>(a);
-  return hipGetLastError();
+  return a.D == 64 ? launch_f32<64>(a, s) : launch_f32<128>(a, s);
 }
 
 }  // namespace s2moe
