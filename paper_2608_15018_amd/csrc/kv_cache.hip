@@ -6,6 +6,8 @@
 // workgroup for all of them (reserve, whose grants depend on each other);
 // what they decide does not depend on timing: a free page is one that nobody
 // holds, and the lowest ids are taken first, in the order of the requests.
+#include <type_traits>
+
 #include "attention.h"
 #include "common.h"
 
@@ -95,10 +97,11 @@ __global__ __launch_bounds__(256) void kv_free_kernel(KvCache c, const int32_t* 
   if (threadIdx.x == 0) c.length[s] = 0;
 }
 
-// Sum of x over the threads before this one; *total over all.  1024 threads.
-__device__ int scan_1024(int x, int* total, int* waves) {
-  const int lane = threadIdx.x & 63, w = threadIdx.x >> 6;
+// Sum of x over the threads before this one; *total over all.
+__device__ int scan_block(int x, int* total, int* waves) {
+  const int lane = threadIdx.x & 63, w = threadIdx.x >> 6, nw = blockDim.x >> 6;
   int inc = x;
+#pragma unroll
   for (int d = 1; d < 64; d <<= 1) {
     const int y = __shfl_up(inc, d);
     if (lane >= d) inc += y;
@@ -107,7 +110,7 @@ __device__ int scan_1024(int x, int* total, int* waves) {
   if (lane == 63) waves[w] = inc;
   __syncthreads();
   int before = 0, all = 0;
-  for (int j = 0; j < 16; ++j) {
+  for (int j = 0; j < nw; ++j) {
     const int y = waves[j];
     before += j < w ? y : 0;
     all += y;
@@ -116,96 +119,125 @@ __device__ int scan_1024(int x, int* total, int* waves) {
   return before + inc - x;
 }
 
-// Grants of one reserve call, one thread per request.
+// How many of ids[0 .. i - 1] (LDS, 16-byte aligned) equal x.
+__device__ int count_before(const int* ids, int i, int x) {
+  int n = 0;
+  for (int j = 0; j < i; j += 4) {
+    const int4 v = *reinterpret_cast<const int4*>(ids + j);
+    n += (v.x == x) + (j + 1 < i && v.y == x) + (j + 2 < i && v.z == x) + (j + 3 < i && v.w == x);
+  }
+  return n;
+}
+
+// Grants of one reserve call: one workgroup, one thread per request.  A wave looks
+// at 1024 pages a sweep, 64 at a time, so that the free ones come in order from
+// ballots.
 __global__ __launch_bounds__(1024) void kv_reserve_kernel(KvCache c, int n,
                                                           const int32_t* __restrict__ seqs,
                                                           const int32_t* __restrict__ extra,
                                                           int32_t* __restrict__ copied,
                                                           int32_t* __restrict__ status) {
-  __shared__ int seq_s[1024], shared_s[1024], first_s[1024], held_s[1024], copy_s[1024], to_s[1024],
-      waves[16];
-  const int i = threadIdx.x;
+  __shared__ __attribute__((aligned(16))) int seq_s[1024], shared_s[1024];
+  __shared__ int first_s[1024], held_s[1024], copy_s[1024], to_s[1024], waves[16];
+  const int i = threadIdx.x, lane = i & 63, w = i >> 6, nw = blockDim.x >> 6;
   const bool live = i < n;
   const int s = live ? seqs[i] : -1;
+  const int more = live ? extra[i] : 0;
   seq_s[i] = s;
-  __syncthreads();
-  int st = 0, need = 0, held = 0, page = -1;
+  to_s[i] = -1;
+  int st = 0, need = 0, held = 0, page = -1, refs = 0;
   int64_t last = 0;
   int32_t* row = nullptr;
-  if (live) {
-    if (!in_range(s, c.max_seqs)) st = kKvBadSeq;
-    for (int j = 0; j < i && !st; ++j) st = seq_s[j] == s ? kKvBadSeq : 0;
-  }
+  if (live && !in_range(s, c.max_seqs)) st = kKvBadSeq;
   if (live && !st) {
     row = c.table + (int64_t)s * c.max_pages;
-    const int64_t len = c.length[s], want = len + extra[i];
-    if (extra[i] < 0 || len < 0 || want > ((int64_t)c.max_pages << c.log_p)) {
+    const int64_t len = c.length[s], want = len + more;
+    if (more < 0 || len < 0 || want > ((int64_t)c.max_pages << c.log_p)) {
       st = kKvTooLong;
     } else {
       const int target = pages_of(c, want);
       held = pages_of(c, len);
+      last = len >> c.log_p;
+      if (more > 0 && (len & (c.P - 1)) != 0) {
+        const int p = row[last];
+        if (in_range(p, c.n_pages)) {
+          refs = c.refs[p];
+          if (refs > 1) page = p;
+        }
+      }
       while (held < target && row[held] >= 0) ++held;
       need = target - held > 0 ? target - held : 0;
-      last = len >> c.log_p;
-      if (extra[i] > 0 && (len & (c.P - 1)) != 0) {
-        const int p = row[last];
-        if (in_range(p, c.n_pages) && c.refs[p] > 1) page = p;
-      }
     }
+  }
+  __syncthreads();
+  if (live && st != kKvBadSeq && count_before(seq_s, i, s) > 0) {
+    st = kKvBadSeq;
+    need = 0;
+    page = -1;
   }
   shared_s[i] = page;
   __syncthreads();
   // Of the sequences that share a page the last keeps it.
-  int copy = 0;
-  if (page >= 0) {
-    int rank = 0;
-    for (int j = 0; j < i; ++j) rank += shared_s[j] == page;
-    copy = c.refs[page] - rank > 1;
-  }
+  const int copy = page >= 0 && refs - count_before(shared_s, i, page) > 1;
   const int take = need + copy;
   int total;
-  const int first = scan_1024(take, &total, waves);
+  const int first = scan_block(take, &total, waves);
   first_s[i] = first;
   held_s[i] = held;
   copy_s[i] = copy;
-  to_s[i] = -1;
   // How many free pages there are, up to `total`; then who gets which.
   int free_pages = 0;
   for (int pass = 0; pass < 2; ++pass) {
     int seen = 0;
     const int stop = pass == 0 ? total : (total < free_pages ? total : free_pages);
-    for (int64_t p0 = 0; p0 < c.n_pages && seen < stop; p0 += 1024 * 16) {
-      const int64_t mine = p0 + threadIdx.x * 16;
-      uint32_t free_mask = 0;
-      for (int b = 0; b < 16; ++b)
-        if (mine + b < c.n_pages && c.refs[mine + b] == 0) free_mask |= 1u << b;
-      int here;
-      int f = seen + scan_1024(__popc(free_mask), &here, waves);
-      if (pass == 1) {
-        for (; free_mask != 0 && f < stop; free_mask &= free_mask - 1, ++f) {
-          const int p = (int)(mine + __ffs(free_mask) - 1);
-          int lo = 0, hi = n;  // the last request whose first page is at or before f
-          while (hi - lo > 1) {
-            const int mid = (lo + hi) / 2;
-            if (first_s[mid] <= f) lo = mid; else hi = mid;
-          }
-          const int end = lo + 1 < n ? first_s[lo + 1] : total;
-          if (end > free_pages) continue;  // its request is not granted
-          int32_t* r = c.table + (int64_t)seq_s[lo] * c.max_pages;
-          const int k = f - first_s[lo];
-          if (k < copy_s[lo]) {
-            to_s[lo] = p;
-          } else {
-            r[held_s[lo] + k - copy_s[lo]] = p;
-          }
-          c.refs[p] = 1;
-        }
+    for (int64_t p0 = 0; p0 < c.n_pages && seen < stop; p0 += nw * 1024) {
+      const int64_t mine = p0 + w * 1024 + lane;
+      int r[16];
+#pragma unroll
+      for (int b = 0; b < 16; ++b) r[b] = mine + 64 * b < c.n_pages ? c.refs[mine + 64 * b] : 1;
+      uint64_t free_mask[16];
+      int here = 0;
+#pragma unroll
+      for (int b = 0; b < 16; ++b) {
+        free_mask[b] = __ballot(r[b] == 0);
+        here += __popcll(free_mask[b]);
       }
-      seen += here;
+      __syncthreads();  // `waves` is free again
+      if (lane == 0) waves[w] = here;
+      __syncthreads();
+      int f0 = seen;
+      for (int j = 0; j < nw; ++j) {
+        f0 += j < w ? waves[j] : 0;
+        seen += waves[j];
+      }
+      if (pass == 0) continue;
+#pragma unroll
+      for (int b = 0; b < 16; ++b) {
+        const int f = f0 + __popcll(free_mask[b] & ((1ull << lane) - 1));
+        f0 += __popcll(free_mask[b]);
+        if (r[b] != 0 || f >= stop) continue;
+        const int p = (int)(mine + 64 * b);
+        int lo = 0, hi = n;  // the last request whose first page is at or before f
+        while (hi - lo > 1) {
+          const int mid = (lo + hi) / 2;
+          if (first_s[mid] <= f) lo = mid; else hi = mid;
+        }
+        const int end = lo + 1 < n ? first_s[lo + 1] : total;
+        if (end > free_pages) continue;  // its request is not granted
+        const int k = f - first_s[lo];
+        if (k < copy_s[lo])
+          to_s[lo] = p;
+        else
+          c.table[(int64_t)seq_s[lo] * c.max_pages + held_s[lo] + k - copy_s[lo]] = p;
+        c.refs[p] = 1;
+      }
     }
-    if (pass == 0) free_pages = seen;
+    if (pass == 0) {
+      free_pages = seen;
+      __syncthreads();  // first_s and its like are complete
+    }
   }
-  __syncthreads();  // to_s[] is complete
+  __syncthreads();  // to_s is complete
   if (live) {
     if (take > 0 && first + take > free_pages) st = kKvNoPages;
     const int to = st ? -1 : to_s[i];
@@ -239,83 +271,123 @@ __global__ __launch_bounds__(256) void kv_copy_kernel(KvCache c, const int32_t* 
   }
 }
 
-// Status of a commit request, the same in both launches.  Block-wide.
+// Status of a commit request, the same in both launches.  Block-wide.  note(j, p,
+// from, to): the accepted node of rank j is p, its slots' pages are from and to.
+template <typename F>
 __device__ int check_commit(const KvCache& c, int i, int max_path,
                             const int32_t* __restrict__ seqs, const int32_t* __restrict__ path,
-                            int acc) {
+                            int acc, F note) {
   const int s = seqs[i];
-  if (repeated(seqs, i) || !in_range(s, c.max_seqs)) return kKvBadSeq;
-  const int64_t len = c.length[s];
-  if (len < 0 || acc < 0 || (path != nullptr && acc > max_path)) return kKvBadPath;
   int bad = 0;
-  const int32_t* row = c.table + (int64_t)s * c.max_pages;
-  // Every slot that is kept lies in a page that the sequence holds alone.
-  const auto alone = [&](int64_t pos) {
-    const int64_t at = pos >> c.log_p;
-    if (at >= c.max_pages) return false;
-    const int page = row[at];
-    return in_range(page, c.n_pages) && c.refs[page] == 1;
-  };
-  if (path != nullptr) {
-    for (int j = threadIdx.x; j < acc; j += blockDim.x) {
-      const int p = path[(int64_t)i * max_path + j];
-      const int before = j > 0 ? path[(int64_t)i * max_path + j - 1] : -1;
-      bad |= p <= before || !alone(len + p) || !alone(len + j);
+  if (in_range(s, c.max_seqs) && acc >= 0 && (path == nullptr || acc <= max_path)) {
+    const int64_t len = c.length[s];
+    const int32_t* row = c.table + (int64_t)s * c.max_pages;
+    // The page of a slot that the sequence holds alone; -1 where it does not.
+    const auto alone = [&](int64_t pos) {
+      const int64_t at = pos >> c.log_p;
+      if (pos < 0 || at >= c.max_pages) return -1;
+      const int page = row[at];
+      return in_range(page, c.n_pages) && c.refs[page] == 1 ? page : -1;
+    };
+    if (path != nullptr) {
+      for (int j = threadIdx.x; j < acc; j += blockDim.x) {
+        const int p = path[(int64_t)i * max_path + j];
+        const int before = j > 0 ? path[(int64_t)i * max_path + j - 1] : -1;
+        const int from = alone(len + p), to = alone(len + j);
+        bad |= p <= before || from < 0 || to < 0;
+        note(j, p, from, to);
+      }
+    } else {
+      for (int64_t j = threadIdx.x * (int64_t)c.P; j < acc; j += blockDim.x * (int64_t)c.P)
+        bad |= alone(len + j) < 0;
+      bad |= acc > 0 && alone(len + acc - 1) < 0;
     }
+    bad |= len < 0;
   } else {
-    for (int64_t j = threadIdx.x * (int64_t)c.P; j < acc; j += blockDim.x * (int64_t)c.P)
-      bad |= !alone(len + j);
-    bad |= acc > 0 && !alone(len + acc - 1);
+    bad = 1;
   }
+  if (repeated(seqs, i) || !in_range(s, c.max_seqs)) return kKvBadSeq;
   return __syncthreads_or(bad) ? kKvBadPath : 0;
 }
 
-// Moves one request's accepted tokens, blockIdx.y the request.  A thread
-// keeps to one 16-byte piece of a key, or one coordinate of the values, of
-// one (layer, head), and moves it for the path's nodes in ascending order:
-// path[j] >= j, so what it overwrites it has read before.
-template <typename E>
+// Moves one request's accepted tokens, blockIdx.y the request, a wave one (layer,
+// head).  path[j] >= j, so in ascending order nothing is overwritten that has yet to
+// be read: a later token's source is at or after its own target, past what is written
+// before.  Keys move 16 bytes a lane, 1 KB a load; of the values a lane has D / 64
+// coordinates and puts together whole groups of eight tokens.
+template <typename E, int D>
 __global__ __launch_bounds__(256) void kv_move_kernel(KvCache c, int max_path,
                                                       const int32_t* __restrict__ seqs,
                                                       const int32_t* __restrict__ path,
                                                       const int32_t* __restrict__ n_accept) {
-  __shared__ int from_s[kMaxNodes], to_s[kMaxNodes], from_p[kMaxNodes], to_p[kMaxNodes];
+  constexpr int kPieces = D * (int)sizeof(E) / 16, kAtOnce = 64 / kPieces;  // of a key; keys a load
+  constexpr int VD = D / 64;
+  typedef E E8 __attribute__((ext_vector_type(8)));
+  __shared__ int node_s[kMaxNodes], from_p[kMaxNodes], to_p[kMaxNodes];
   const int i = blockIdx.y, acc = n_accept[i];
-  if (check_commit(c, i, max_path, seqs, path, acc)) return;
-  const int s = seqs[i], len = c.length[s];
-  const int32_t* row = c.table + (int64_t)s * c.max_pages;
-  int moved = 0;
-  for (int j = threadIdx.x; j < acc; j += blockDim.x) {
-    const int p = path[(int64_t)i * max_path + j];
-    const int a = len + p, b = len + j;
-    from_s[j] = a & (c.P - 1);
-    to_s[j] = b & (c.P - 1);
-    from_p[j] = row[a >> c.log_p];
-    to_p[j] = row[b >> c.log_p];
-    moved += p == j;
-  }
-  // path[j] == j for the first j0 nodes: they stay.
-  const int j0 = __syncthreads_count(moved);
+  int stays = 0;
+  if (check_commit(c, i, max_path, seqs, path, acc, [&](int j, int p, int from, int to) {
+        node_s[j] = p;
+        from_p[j] = from;
+        to_p[j] = to;
+        stays = p == j;
+      }))
+    return;
+  const int j0 = __syncthreads_count(stays);  // path[j] == j for j < j0
   if (j0 == acc) return;
-  const int kp = c.D * (int)sizeof(E) / 16;        // pieces of a key
-  const int units = c.L * c.Hkv * (c.D + kp);
-  const int u = blockIdx.x * blockDim.x + threadIdx.x;
-  if (u >= units) return;
-  const int nv = c.L * c.Hkv * c.D;
-  const bool is_v = u < nv;
-  const int lh = is_v ? u / c.D : (u - nv) / kp, x = is_v ? u % c.D : (u - nv) % kp;
-  const int64_t base = (lh / c.Hkv) * c.layer_bytes() + (lh % c.Hkv) * c.head_bytes();
-  for (int j = j0; j < acc; ++j) {
-    const int64_t a = base + from_p[j] * c.page_bytes(), b = base + to_p[j] * c.page_bytes();
-    if (is_v) {
-      const int sa = from_s[j], sb = to_s[j];
-      const E* pa = reinterpret_cast<const E*>(c.v + a) + (sa >> 3) * c.D * 8 + x * 8 + (sa & 7);
-      E* pb = reinterpret_cast<E*>(c.v + b) + (sb >> 3) * c.D * 8 + x * 8 + (sb & 7);
-      *pb = *pa;
-    } else {
-      const int64_t r = (int64_t)c.D * sizeof(E);
-      *reinterpret_cast<u32x4*>(c.k + b + to_s[j] * r + 16 * x) =
-          *reinterpret_cast<const u32x4*>(c.k + a + from_s[j] * r + 16 * x);
+  const int len = c.length[seqs[i]], lane = threadIdx.x & 63;
+  const int64_t page_bytes = c.page_bytes();
+  const int piece = lane % kPieces, mine = lane / kPieces;
+  const auto slot = [&](int node) { return (len + node) & (c.P - 1); };
+  for (int lh = blockIdx.x * 4 + wave_id(); lh < c.L * c.Hkv; lh += gridDim.x * 4) {
+    const int64_t base = (lh / c.Hkv) * c.layer_bytes() + (lh % c.Hkv) * c.head_bytes();
+    int jb = j0, g0 = (len + j0) & ~7;
+    while (jb < acc || g0 < len + acc) {  // up to 4 kAtOnce keys, and a group of values
+      u32x4 x[4];
+#pragma unroll
+      for (int y = 0; y < 4; ++y) {
+        const int j = jb + y * kAtOnce + mine;
+        if (j < acc)
+          x[y] = *reinterpret_cast<const u32x4*>(c.k + base + from_p[j] * page_bytes +
+                                                 (slot(node_s[j]) * kPieces + piece) * 16);
+      }
+      const int j1 = g0 - len;  // the group's first slot as a node, below 0 for older tokens
+      const bool group = g0 < len + acc;
+      char* to = nullptr;
+      E8 v[VD];
+      E y8[VD][8];
+      if (group) {
+        to = c.v + base + to_p[max(j1, j0)] * page_bytes + (int64_t)(g0 & (c.P - 1)) * D * sizeof(E);
+#pragma unroll
+        for (int z = 0; z < VD; ++z) v[z] = *reinterpret_cast<const E8*>(to + (lane + 64 * z) * sizeof(E8));
+#pragma unroll
+        for (int e = 0; e < 8; ++e) {
+          const int j = j1 + e;
+          if (j >= j0 && j < acc) {
+            const int from = slot(node_s[j]);
+            const E* p = reinterpret_cast<const E*>(c.v + base + from_p[j] * page_bytes) + (from >> 3) * D * 8 + (from & 7);
+#pragma unroll
+            for (int z = 0; z < VD; ++z) y8[z][e] = p[(lane + 64 * z) * 8];
+          }
+        }
+      }
+#pragma unroll
+      for (int y = 0; y < 4; ++y) {
+        const int j = jb + y * kAtOnce + mine;
+        if (j < acc)
+          *reinterpret_cast<u32x4*>(c.k + base + to_p[j] * page_bytes + (slot(j) * kPieces + piece) * 16) = x[y];
+      }
+      if (group) {
+#pragma unroll
+        for (int z = 0; z < VD; ++z) {
+#pragma unroll
+          for (int e = 0; e < 8; ++e)
+            if (j1 + e >= j0 && j1 + e < acc) v[z][e] = y8[z][e];
+          *reinterpret_cast<E8*>(to + (lane + 64 * z) * sizeof(E8)) = v[z];
+        }
+      }
+      jb += 4 * kAtOnce;
+      g0 += 8;
     }
   }
 }
@@ -326,7 +398,7 @@ __global__ __launch_bounds__(256) void kv_commit_kernel(KvCache c, int max_path,
                                                         const int32_t* __restrict__ n_accept,
                                                         int32_t* __restrict__ status) {
   const int i = blockIdx.x, acc = n_accept[i];
-  const int st = check_commit(c, i, max_path, seqs, path, acc);
+  const int st = check_commit(c, i, max_path, seqs, path, acc, [](int, int, int, int) {});
   if (threadIdx.x == 0) status[i] = st;
   if (st) return;
   const int s = seqs[i];
@@ -335,32 +407,90 @@ __global__ __launch_bounds__(256) void kv_commit_kernel(KvCache c, int max_path,
   if (threadIdx.x == 0) c.length[s] = (int)len;
 }
 
-// One workgroup per token.
-template <typename E>
+// New tokens of one layer: blockIdx.x 4 TW packed tokens, TW a wave, blockIdx.y a kv
+// head.  The first token of a request and every token whose slot begins a group of
+// eight write their group's tokens; the others have nothing to do.  The lanes look up
+// the tokens' pages together; then one has D / 64 coordinates of the values, and a
+// group that is whole goes out 16 bytes or more a coordinate.
+template <typename E, int D, int TW>
 __global__ __launch_bounds__(256) void kv_append_kernel(KvCache c, AppendArgs a) {
-  const int t = blockIdx.x;
-  int lo = 0, hi = a.n;
-  while (hi - lo > 1) {
-    const int mid = (lo + hi) / 2;
-    if (a.tok_off[mid] <= t) lo = mid; else hi = mid;
+  constexpr int kPieces = D * (int)sizeof(E) / 16, VD = D / 64;
+  typedef E E8 __attribute__((ext_vector_type(8)));
+  typedef E EV __attribute__((ext_vector_type(VD)));
+  const int lane = threadIdx.x & 63, t0 = (blockIdx.x * 4 + wave_id()) * TW, h = blockIdx.y;
+  // Requests that begin at or before each token; lane x goes on with token t0 + x.
+  int began[TW] = {}, i = -1;
+  for (int i0 = 0; i0 < a.n; i0 += 64) {
+    const int off = i0 + lane < a.n ? a.tok_off[i0 + lane] : 0x7FFFFFFF;
+#pragma unroll
+    for (int x = 0; x < TW; ++x) began[x] += __popcll(__ballot(off <= t0 + x));
   }
-  if (t < a.tok_off[lo] || t >= a.tok_off[lo + 1]) return;
-  const int s = a.seqs[lo];
-  if (!in_range(s, c.max_seqs)) return;
-  const int64_t pos = (int64_t)c.length[s] + t - a.tok_off[lo];
-  const int64_t at = pos >> c.log_p;
-  if (pos < 0 || at >= c.max_pages) return;
-  const int page = c.table[(int64_t)s * c.max_pages + at];
-  if (!in_range(page, c.n_pages) || c.refs[page] != 1) return;
-  const int slot = (int)(pos & (c.P - 1));
-  const int64_t base = a.layer * c.layer_bytes() + page * c.page_bytes();
-  const E* k = reinterpret_cast<const E*>(a.k) + t * a.ldk;
-  const E* v = reinterpret_cast<const E*>(a.v) + t * a.ldv;
-  for (int x = threadIdx.x; x < c.Hkv * c.D; x += blockDim.x) {
-    const int h = x / c.D, d = x % c.D;
-    const int64_t head = base + h * c.head_bytes();
-    reinterpret_cast<E*>(c.k + head)[slot * c.D + d] = k[x];
-    reinterpret_cast<E*>(c.v + head)[(slot >> 3) * c.D * 8 + d * 8 + (slot & 7)] = v[x];
+#pragma unroll
+  for (int x = 0; x < TW; ++x) i = lane == x ? began[x] - 1 : i;
+  const int mine = t0 + lane;
+  int page = -1, slot = 0, count = 0;
+  if (i >= 0 && mine < a.n_tokens) {
+    const int begin = a.tok_off[i], end = min(a.tok_off[i + 1], a.n_tokens), s = a.seqs[i];
+    if (mine >= begin && mine < end && in_range(s, c.max_seqs)) {
+      const int64_t pos = (int64_t)c.length[s] + mine - begin, at = pos >> c.log_p;
+      if (pos >= 0 && at < c.max_pages && (mine == begin || (pos & 7) == 0)) {
+        const int p = c.table[(int64_t)s * c.max_pages + at];
+        if (in_range(p, c.n_pages) && c.refs[p] == 1) page = p;
+        slot = (int)(pos & (c.P - 1));
+        count = min(8 - (slot & 7), end - mine);
+      }
+    }
+  }
+#pragma unroll
+  for (int x = 0; x < TW; ++x) {
+    const int to = __builtin_amdgcn_readlane(page, x), at = __builtin_amdgcn_readlane(slot, x);
+    const int n = __builtin_amdgcn_readlane(count, x), t = t0 + x;
+    if (to < 0) continue;
+    const int64_t head = a.layer * c.layer_bytes() + to * c.page_bytes() + h * c.head_bytes();
+    const E* k = reinterpret_cast<const E*>(a.k) + t * a.ldk + h * D;
+    const E* v = reinterpret_cast<const E*>(a.v) + t * a.ldv + h * D + VD * lane;
+    u32x4* const kt = reinterpret_cast<u32x4*>(c.k + head) + at * kPieces;
+    E* const vt = reinterpret_cast<E*>(c.v + head) + (at >> 3) * D * 8 + VD * lane * 8;
+    if (n == 8) {
+      EV z[8];
+#pragma unroll
+      for (int e = 0; e < 8; ++e) z[e] = *reinterpret_cast<const EV*>(v + e * a.ldv);
+      u32x4 y[8 * kPieces / 64];
+#pragma unroll
+      for (int b = 0; b < 8 * kPieces / 64; ++b) {
+        const int q = lane + 64 * b;
+        y[b] = reinterpret_cast<const u32x4*>(k + (q / kPieces) * a.ldk)[q % kPieces];
+      }
+#pragma unroll
+      for (int b = 0; b < 8 * kPieces / 64; ++b) kt[lane + 64 * b] = y[b];
+#pragma unroll
+      for (int d = 0; d < VD; ++d) {
+        E8 o;
+#pragma unroll
+        for (int e = 0; e < 8; ++e) o[e] = z[e][d];
+        *reinterpret_cast<E8*>(vt + d * 8) = o;
+      }
+    } else {
+      for (int q = lane; q < n * kPieces; q += 64)
+        kt[q] = reinterpret_cast<const u32x4*>(k + (q / kPieces) * a.ldk)[q % kPieces];
+      for (int e = 0; e < n; ++e) {
+        const EV z = *reinterpret_cast<const EV*>(v + e * a.ldv);
+#pragma unroll
+        for (int d = 0; d < VD; ++d) vt[d * 8 + (at & 7) + e] = z[d];
+      }
+    }
+  }
+}
+
+// f(element, head size) for the cache's type.
+template <typename F>
+void by_type(const KvCache& c, F f) {
+  if (c.f32) {
+    if (c.D == 64) f(uint32_t{}, std::integral_constant<int, 64>{});
+    else f(uint32_t{}, std::integral_constant<int, 128>{});
+  } else {
+    if (c.D == 64) f(uint16_t{}, std::integral_constant<int, 64>{});
+    else f(uint16_t{}, std::integral_constant<int, 128>{});
   }
 }
 
@@ -379,7 +509,7 @@ hipError_t launch_kv_fork(const KvCache& c, int n, const int32_t* src, const int
 
 hipError_t launch_kv_reserve(const KvCache& c, int n, const int32_t* seqs, const int32_t* extra,
                              int32_t* copied, int32_t* status, hipStream_t s) {
-  kv_reserve_kernel<<<1, 1024, 0, s>>>(c, n, seqs, extra, copied, status);
+  kv_reserve_kernel<<<1, n <= 256 ? 256 : 1024, 0, s>>>(c, n, seqs, extra, copied, status);
   hipError_t err = hipGetLastError();
   if (err != hipSuccess) return err;
   kv_copy_kernel<<<dim3(c.L * c.Hkv, n), 256, 0, s>>>(c, seqs, copied);
@@ -390,12 +520,12 @@ hipError_t launch_kv_commit(const KvCache& c, int n, int max_path, const int32_t
                             const int32_t* path, const int32_t* n_accept, int32_t* status,
                             hipStream_t s) {
   if (path != nullptr && max_path > 0) {
-    const int units = c.L * c.Hkv * (c.D + c.D * c.elt() / 16);
-    const dim3 grid((units + 255) / 256, n);
-    if (c.f32)
-      kv_move_kernel<uint32_t><<<grid, 256, 0, s>>>(c, max_path, seqs, path, n_accept);
-    else
-      kv_move_kernel<uint16_t><<<grid, 256, 0, s>>>(c, max_path, seqs, path, n_accept);
+    // Four (layer, head) a workgroup, or more where that makes over 2048 workgroups.
+    const int most = 2048 / n > 0 ? 2048 / n : 1, want = (c.L * c.Hkv + 3) / 4;
+    const dim3 grid(want < most ? want : most, n);
+    by_type(c, [&](auto e, auto d) {
+      kv_move_kernel<decltype(e), decltype(d)::value><<<grid, 256, 0, s>>>(c, max_path, seqs, path, n_accept);
+    });
     const hipError_t err = hipGetLastError();
     if (err != hipSuccess) return err;
   }
@@ -410,10 +540,19 @@ hipError_t launch_kv_free(const KvCache& c, int n, const int32_t* seqs, int32_t*
 }
 
 hipError_t launch_kv_append(const KvCache& c, const AppendArgs& a, hipStream_t s) {
-  if (c.f32)
-    kv_append_kernel<uint32_t><<<a.n_tokens, 256, 0, s>>>(c, a);
-  else
-    kv_append_kernel<uint16_t><<<a.n_tokens, 256, 0, s>>>(c, a);
+  // A wave takes a token where requests bring few, else eight, of which about one
+  // begins a group.
+  const bool few = a.n_tokens / a.n < 8;
+  const int per = few ? 4 : 32;
+  const dim3 grid((a.n_tokens + per - 1) / per, c.Hkv);
+  by_type(c, [&](auto e, auto d) {
+    typedef decltype(e) E;
+    constexpr int D = decltype(d)::value;
+    if (few)
+      kv_append_kernel<E, D, 1><<<grid, 256, 0, s>>>(c, a);
+    else
+      kv_append_kernel<E, D, 8><<<grid, 256, 0, s>>>(c, a);
+  });
   return hipGetLastError();
 }
 
