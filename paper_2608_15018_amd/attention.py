@@ -33,22 +33,30 @@ def _code(dtype) -> int:
     return _CODES[dtype]
 
 
-def _ints(t, name, shape):
-    if t.dtype != torch.int32 or t.shape != shape:
-        raise ValueError(f"{name}: expected int32 {tuple(shape)}, got {t.dtype} {tuple(t.shape)}")
-    return _lib._ptr(t)
+_I32 = torch.int32
+
+
+# The checks are on every call's path to the GPU, which at the smallest sizes waits
+# for them: each property is read once.
+def _ints(t, name, n):
+    """Pointer of int32 [n]."""
+    if t.dtype is not _I32 or t.dim() != 1 or t.size(0) != n or not t.is_contiguous():
+        raise ValueError(f"{name}: expected contiguous int32 [{n}], got {t.dtype} {tuple(t.shape)}")
+    return t.data_ptr()
 
 
 def _rows(t, name, heads, head_dim, dtype):
-    """(pointer, elements from one token to the next) of [n, heads, head_dim]
-    whose heads lie together."""
-    if t.dtype != dtype or t.dim() != 3 or t.shape[1] != heads or t.shape[2] != head_dim:
+    """(pointer, elements from one token to the next, tokens) of [n, heads,
+    head_dim] whose heads lie together."""
+    shape = t.shape
+    if t.dtype is not dtype or len(shape) != 3 or shape[1] != heads or shape[2] != head_dim:
         raise ValueError(f"{name}: expected {dtype} [n, {heads}, {head_dim}], got {t.dtype} "
-                         f"{tuple(t.shape)}")
-    n, s0, s1, s2 = t.shape[0], *t.stride()
+                         f"{tuple(shape)}")
+    s0, s1, s2 = t.stride()
     if s2 != 1 or (s1 != head_dim and heads > 1):
         raise ValueError(f"{name}: the heads of a token must lie together (strides {t.stride()})")
-    return t.data_ptr(), s0 if n > 1 else heads * head_dim
+    n = shape[0]
+    return t.data_ptr(), s0 if n > 1 else heads * head_dim, n
 
 
 class KVCache:
@@ -102,28 +110,28 @@ class KVCache:
     def fork(self, src, dst, stream=None):
         """Sequence dst[i] becomes a copy of src[i] on the same pages."""
         n = src.shape[0]
-        _lib._check(self._lib.s2moe_kv_fork(self._ref, n, _ints(src, "src", (n,)),
-                                            _ints(dst, "dst", (n,)), self._status,
+        _lib._check(self._lib.s2moe_kv_fork(self._ref, n, _ints(src, "src", n),
+                                            _ints(dst, "dst", n), self._status,
                                             _lib._stream(stream)))
 
     def reserve(self, seqs, extra, stream=None):
         """Pages for extra[i] more tokens of seqs[i]; a shared page that they
         would be written to is copied."""
         n = seqs.shape[0]
-        _lib._check(self._lib.s2moe_kv_reserve(self._ref, n, _ints(seqs, "seqs", (n,)),
-                                               _ints(extra, "extra", (n,)), self._copied,
+        _lib._check(self._lib.s2moe_kv_reserve(self._ref, n, _ints(seqs, "seqs", n),
+                                               _ints(extra, "extra", n), self._copied,
                                                self._status, _lib._stream(stream)))
 
     def append(self, layer: int, k, v, seqs, tok_off, stream=None):
         """New tokens' keys and values [n_tokens, n_kv_heads, head_dim] into
         the slots after the lengths."""
-        n, t = seqs.shape[0], k.shape[0]
-        kp, ldk = _rows(k, "k", self.n_kv_heads, self.head_dim, self.dtype)
-        vp, ldv = _rows(v, "v", self.n_kv_heads, self.head_dim, self.dtype)
-        if v.shape[0] != t:
-            raise ValueError(f"v holds {v.shape[0]} tokens, k {t}")
-        _lib._check(self._lib.s2moe_kv_append(self._ref, layer, n, t, _ints(seqs, "seqs", (n,)),
-                                              _ints(tok_off, "tok_off", (n + 1,)), kp, ldk, vp,
+        n = seqs.shape[0]
+        kp, ldk, t = _rows(k, "k", self.n_kv_heads, self.head_dim, self.dtype)
+        vp, ldv, tv = _rows(v, "v", self.n_kv_heads, self.head_dim, self.dtype)
+        if tv != t:
+            raise ValueError(f"v holds {tv} tokens, k {t}")
+        _lib._check(self._lib.s2moe_kv_append(self._ref, layer, n, t, _ints(seqs, "seqs", n),
+                                              _ints(tok_off, "tok_off", n + 1), kp, ldk, vp,
                                               ldv, _lib._stream(stream)))
 
     def commit(self, seqs, path, n_accept, stream=None):
@@ -131,15 +139,18 @@ class KVCache:
         path None: the first n_accept[i] tokens as they lie."""
         n = seqs.shape[0]
         most = 0 if path is None else path.shape[1]
-        pp = None if path is None else _ints(path, "path", (n, most))
-        _lib._check(self._lib.s2moe_kv_commit(self._ref, n, most, _ints(seqs, "seqs", (n,)), pp,
-                                              _ints(n_accept, "n_accept", (n,)), self._status,
+        pp = None
+        if path is not None:
+            _lib._expect(path, "path", _I32, (n, most))
+            pp = _lib._ptr(path)
+        _lib._check(self._lib.s2moe_kv_commit(self._ref, n, most, _ints(seqs, "seqs", n), pp,
+                                              _ints(n_accept, "n_accept", n), self._status,
                                               _lib._stream(stream)))
 
     def free(self, seqs, stream=None):
         """Empties the sequences."""
         n = seqs.shape[0]
-        _lib._check(self._lib.s2moe_kv_free(self._ref, n, _ints(seqs, "seqs", (n,)),
+        _lib._check(self._lib.s2moe_kv_free(self._ref, n, _ints(seqs, "seqs", n),
                                             self._status, _lib._stream(stream)))
 
 
@@ -165,19 +176,22 @@ class TreeAttention:
 
     def __call__(self, layer: int, q, seqs, tok_off, parent, out=None, stream=None):
         """q [n_tokens, n_heads, head_dim] -> out of the same shape."""
-        c, n, t = self.cache, seqs.shape[0], q.shape[0]
+        c, n = self.cache, seqs.shape[0]
         if n > self.max_seqs:
             raise ValueError(f"{n} sequences, the workspace is for {self.max_seqs}")
-        qp, ldq = _rows(q, "q", self.n_heads, c.head_dim, c.dtype)
+        D, Hq = c.head_dim, self.n_heads
+        qp, ldq, t = _rows(q, "q", Hq, D, c.dtype)
         if out is None:
-            out = torch.empty((t, self.n_heads, c.head_dim), dtype=c.dtype, device=q.device)
-        op, ldo = _rows(out, "out", self.n_heads, c.head_dim, c.dtype)
-        if out.shape[0] != t:
-            raise ValueError(f"out holds {out.shape[0]} tokens, q {t}")
+            out = q.new_empty((t, Hq, D))
+            op, ldo = out.data_ptr(), Hq * D
+        else:
+            op, ldo, to = _rows(out, "out", Hq, D, c.dtype)
+            if to != t:
+                raise ValueError(f"out holds {to} tokens, q {t}")
         self.attn.ldq, self.attn.ldo = ldq, ldo
         _lib._check(self._lib.s2moe_tree_attention(
-            c._ref, layer, self._ref, n, t, self.max_nodes, qp, _ints(seqs, "seqs", (n,)),
-            _ints(tok_off, "tok_off", (n + 1,)), _ints(parent, "parent", (t,)),
+            c._ref, layer, self._ref, n, t, self.max_nodes, qp, _ints(seqs, "seqs", n),
+            _ints(tok_off, "tok_off", n + 1), _ints(parent, "parent", t),
             self.workspace.data_ptr(), self.bytes, op, _lib._stream(stream)))
         return out
 
@@ -187,22 +201,23 @@ def prompt_attention(q, k, v, tok_off, out=None, scale: float | None = None, str
     k and v [n_tokens, n_kv_heads, head_dim], tok_off [n + 1] int32."""
     if q.dim() != 3 or k.dim() != 3:
         raise ValueError("q, k, v: expected [n_tokens, heads, head_dim]")
-    t, Hq, D = q.shape
-    Hkv = k.shape[1]
-    qp, ldq = _rows(q, "q", Hq, D, q.dtype)
-    kp, ldk = _rows(k, "k", Hkv, D, q.dtype)
-    vp, ldv = _rows(v, "v", Hkv, D, q.dtype)
+    Hq, D, Hkv, dt = q.shape[1], q.shape[2], k.shape[1], q.dtype
+    qp, ldq, t = _rows(q, "q", Hq, D, dt)
+    kp, ldk, tk = _rows(k, "k", Hkv, D, dt)
+    vp, ldv, tv = _rows(v, "v", Hkv, D, dt)
     if out is None:
-        out = torch.empty((t, Hq, D), dtype=q.dtype, device=q.device)
-    op, ldo = _rows(out, "out", Hq, D, q.dtype)
-    if not (k.shape[0] == v.shape[0] == out.shape[0] == t):
-        raise ValueError(f"q, k, v, out hold {t}, {k.shape[0]}, {v.shape[0]}, {out.shape[0]} tokens")
+        out = q.new_empty((t, Hq, D))
+        op, ldo, to = out.data_ptr(), Hq * D, t
+    else:
+        op, ldo, to = _rows(out, "out", Hq, D, dt)
+    if not (tk == tv == to == t):
+        raise ValueError(f"q, k, v, out hold {t}, {tk}, {tv}, {to} tokens")
     if tok_off.dim() != 1 or tok_off.shape[0] < 1:
         raise ValueError("tok_off: expected int32 [n + 1]")
-    a = _lib.Attn(Hq, Hkv, D, _code(q.dtype), D ** -0.5 if scale is None else scale, ldq, ldk, ldv,
+    a = _lib.Attn(Hq, Hkv, D, _code(dt), D ** -0.5 if scale is None else scale, ldq, ldk, ldv,
                   ldo)
     n = tok_off.shape[0] - 1
     _lib._check(_lib.load().s2moe_prompt_attention(
-        ctypes.byref(a), n, t, qp, kp, vp, _ints(tok_off, "tok_off", (n + 1,)), op,
+        ctypes.byref(a), n, t, qp, kp, vp, _ints(tok_off, "tok_off", n + 1), op,
         _lib._stream(stream)))
     return out

@@ -25,12 +25,6 @@
 namespace s2moe {
 namespace {
 
-#ifndef XG
-#define XG 1
-#endif
-#ifndef XK
-#define XK 2
-#endif
 constexpr int kTile = 128;  // keys of a unit
 
 // A row block whose parts the joining launch adds, as the workgroup that has
@@ -320,8 +314,8 @@ template <typename E, int D, int NT>
 struct KeysPlan {
   static constexpr int kRows = 16 * NT;
   // Workgroups that fit a compute unit.
-  static constexpr int kPerCu = sizeof(E) == 2 ? XK : NT == 2 && D * sizeof(E) == 512 ? 1 : 2;
-  static constexpr int kGroups = 256 * kPerCu * XG;
+  static constexpr int kPerCu = D * sizeof(E) == 512 ? 1 : 2;
+  static constexpr int kGroups = 256 * kPerCu;
   static constexpr int kSums = 4 * 16 * (D + 4) * 4;  // bytes of the waves' sums of 16 rows
   static size_t lds(int n, int max_nodes) { return kSums + shared_lists(n, max_nodes); }
 };
@@ -547,7 +541,7 @@ struct RowsPlan {
   static constexpr int kKeys = D == 128 ? 32 : 64;  // of a stage
   static constexpr int kStage = kKeys * D * 2;      // bytes of its keys, or values
   static constexpr int kRing = 4 * 2 * kStage;
-  static constexpr int kGroups = 512 * XG;               // two fit a compute unit
+  static constexpr int kGroups = 512;               // two fit a compute unit
   static size_t lds(int n, int max_nodes) {
     return kRing + shared_lists(n, max_nodes);
   }
