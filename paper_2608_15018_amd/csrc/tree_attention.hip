@@ -355,7 +355,6 @@ __global__ __launch_bounds__(256, (KeysPlan<E, D, NT>::kPerCu)) void tree_keys_k
     const Stretch r = stretch_of(a, req_s, request_of(u, a.n, req_s), RB, u, u_end);
     const int t0 = r.t0, t1 = r.t1, R = r.R, hk = r.hk, row0 = r.row0;
     const bool tail = t1 * kTile > r.len;
-    if (tail) ancestors(a.parent + r.first, r.T, mask_s, jump_s, dead_s);
 
     int tok[NT];
     frag q[KC][NT];
@@ -411,6 +410,7 @@ __global__ __launch_bounds__(256, (KeysPlan<E, D, NT>::kPerCu)) void tree_keys_k
     place(t0, now);
     load_k(now);
     load_v(now);
+    if (tail) ancestors(a.parent + r.first, r.T, mask_s, jump_s, dead_s);
     for (int t = t0; t < t1; ++t) {
       const int key0 = t * kTile + 32 * w;
       const bool more = t + 1 < t1;
@@ -533,14 +533,16 @@ __global__ __launch_bounds__(256, (KeysPlan<E, D, NT>::kPerCu)) void tree_keys_k
 
 // Larger trees (bf16): the waves split the rows, 16 at a time in turn, and the keys
 // and values of a stage are fetched once for all of them, by loads that go from the
-// pages into LDS without a register between: three stages are in flight while one
-// is used.  A wave fetches a quarter of a stage, which lies in one page.
+// pages into LDS without a register between, three stages in flight while one is
+// used (at D = 128 two of 64 keys each in place of four of 32: 108 -> 121 us for 64
+// ragged trees).  A wave fetches a quarter of a stage, which lies in one page.
 template <int D, int NT>
 struct RowsPlan {
   static constexpr int kRows = 64 * NT;
   static constexpr int kKeys = D == 128 ? 32 : 64;  // of a stage
   static constexpr int kStage = kKeys * D * 2;      // bytes of its keys, or values
-  static constexpr int kRing = 4 * 2 * kStage;
+  static constexpr int kStages = 4;
+  static constexpr int kRing = kStages * 2 * kStage;
   static constexpr int kGroups = 512;               // two fit a compute unit
   static size_t lds(int n, int max_nodes) {
     return kRing + shared_lists(n, max_nodes);
@@ -574,7 +576,7 @@ __device__ __forceinline__ void load_rows_stage(const TreeArgs& a, const Stretch
   typedef RowsPlan<D, 1> Plan;
   constexpr int kLoads = Plan::kStage / 4096;
   const int64_t at = page * st.page_bytes + (int64_t)(rows_key(st, s) & (a.P - 1)) * (D * 2);
-  const int to = (s & 3) * Plan::kStage + wave_id() * kLoads * 1024;
+  const int to = (s & (Plan::kStages - 1)) * Plan::kStage + wave_id() * kLoads * 1024;
 #pragma unroll
   for (int x = 0; x < kLoads; ++x) load_to_lds(st.kb + at, st.k_off[x], st.k_lds + to + x * 1024);
 #pragma unroll
@@ -612,60 +614,78 @@ __device__ __forceinline__ void rows_stretch(const TreeArgs& a, const Stretch& r
     for (int mt = 0; mt < MT; ++mt) O[mt][nt] = f32x4{};
   }
   for (int s = st.s0; s < st.s1; ++s) {
-    // Stage s is there for everybody, and stage s - 1, whose place stage s + 3
-    // takes, is read by nobody any more.
-    wait_loads<4 * kLoads>();
+    // Stage s is there for everybody, and the stage before, whose place is loaded
+    // into, is read by nobody any more.
+    wait_loads<(Plan::kStages - 2) * 2 * kLoads>();
     __builtin_amdgcn_s_barrier();
-    load_rows_stage<D>(a, r, st, s + 3, page);
-    page = rows_page<D>(a, r, st, s + 4);
+    load_rows_stage<D>(a, r, st, s + Plan::kStages - 1, page);
+    page = rows_page<D>(a, r, st, s + Plan::kStages);
     if constexpr (NA > 0) {
+      // 64 keys at a time as far as registers go: their products are independent.
+      constexpr int NS = SK == 64 && NA <= 2 ? 2 : 1;
+      const char* const kt = st.k_lds + (s & (Plan::kStages - 1)) * Plan::kStage;
+      const char* const vt = st.v_lds + (s & (Plan::kStages - 1)) * Plan::kStage + g * (D * 16) + n16 * 16;
 #pragma unroll
-      for (int sub = 0; sub < SK / 32; ++sub) {
+      for (int sub = 0; sub < SK / 32; sub += NS) {
         const int key0 = s * SK + 32 * sub;
-        const char* kt = st.k_lds + (s & 3) * Plan::kStage + 32 * sub * D * 2;
-        const char* vt = st.v_lds + (s & 3) * Plan::kStage + (4 * sub + g) * (D * 16) + n16 * 16;
-        f32x4 S[2][NA];
+        f32x4 S[NS][2][NA];
+        bf16x8 V[NS][MT][1];
 #pragma unroll
-        for (int x = 0; x < 2; ++x) {
+        for (int z = 0; z < NS; ++z)
 #pragma unroll
-          for (int nt = 0; nt < NA; ++nt) S[x][nt] = f32x4{};
-          const int row = key_row + 4 * x;
+          for (int x = 0; x < 2; ++x) {
 #pragma unroll
-          for (int y = 0; y < KC; ++y) {
-            const bf16x8 k = *reinterpret_cast<const bf16x8*>(kt + row * D * 2 + (((4 * y + g) ^ swizzle(row)) << 4));
+            for (int nt = 0; nt < NA; ++nt) S[z][x][nt] = f32x4{};
+            const int row = 32 * (sub + z) + key_row + 4 * x;
 #pragma unroll
-            for (int nt = 0; nt < NA; ++nt) S[x][nt] = mma(k, q[y][nt], S[x][nt]);
+            for (int y = 0; y < KC; ++y) {
+              const bf16x8 k = *reinterpret_cast<const bf16x8*>(kt + row * D * 2 + (((4 * y + g) ^ swizzle(row)) << 4));
+#pragma unroll
+              for (int nt = 0; nt < NA; ++nt) S[z][x][nt] = mma(k, q[y][nt], S[z][x][nt]);
+            }
           }
-        }
-        bf16x8 V[MT][1];
 #pragma unroll
-        for (int mt = 0; mt < MT; ++mt) V[mt][0] = *reinterpret_cast<const bf16x8*>(vt + mt * 256);
-        const bool masked = key0 + 32 > r.len;
-        if (masked) mask_scores<NA>(S, tok, st.mask_s, key0 + 8 * g, r.len, r.total);
+        for (int z = 0; z < NS; ++z)
+#pragma unroll
+          for (int mt = 0; mt < MT; ++mt)
+            V[z][mt][0] = *reinterpret_cast<const bf16x8*>(vt + 4 * (sub + z) * (D * 16) + mt * 256);
+        const bool masked = key0 + 32 * NS > r.len;
+        if (masked)
+#pragma unroll
+          for (int z = 0; z < NS; ++z)
+            mask_scores<NA>(S[z], tok, st.mask_s, key0 + 32 * z + 8 * g, r.len, r.total);
         float m[NA];
         bool over = false;
 #pragma unroll
         for (int nt = 0; nt < NA; ++nt) {
-          m[nt] = largest(S[0][nt], S[1][nt]) * c;
+          m[nt] = largest(S[0][0][nt], S[0][1][nt]);
+          if (NS == 2) m[nt] = fmaxf(m[nt], largest(S[NS - 1][0][nt], S[NS - 1][1][nt]));
+          m[nt] *= c;
           over |= m[nt] > limit[nt];
         }
         if (__any(over)) raise<MT, NA>(m, shift, limit, l, O);
-        bf16x8 P[NA][1];
+        bf16x8 P[NS][NA][1];
 #pragma unroll
-        for (int nt = 0; nt < NA; ++nt) {
-          float p[8];
+        for (int z = 0; z < NS; ++z)
 #pragma unroll
-          for (int e = 0; e < 8; ++e) {
-            p[e] = exp2_fast(fmaf(S[e >> 2][nt][e & 3], c, -shift[nt]));
-            l[nt] += p[e];
+          for (int nt = 0; nt < NA; ++nt) {
+            float p[8];
+#pragma unroll
+            for (int e = 0; e < 8; ++e) {
+              p[e] = exp2_fast(fmaf(S[z][e >> 2][nt][e & 3], c, -shift[nt]));
+              l[nt] += p[e];
+            }
+            P[z][nt][0] = pack8(p);
           }
-          P[nt][0] = pack8(p);
-        }
-        if (masked) hide_nonfinite<MT, NA, 1>(V, P, O);
+        if (masked)
 #pragma unroll
-        for (int mt = 0; mt < MT; ++mt)
+          for (int z = 0; z < NS; ++z) hide_nonfinite<MT, NA, 1>(V[z], P[z], O);
 #pragma unroll
-          for (int nt = 0; nt < NA; ++nt) O[mt][nt] = mma(V[mt][0], P[nt][0], O[mt][nt]);
+        for (int z = 0; z < NS; ++z)
+#pragma unroll
+          for (int mt = 0; mt < MT; ++mt)
+#pragma unroll
+            for (int nt = 0; nt < NA; ++nt) O[mt][nt] = mma(V[z][mt][0], P[z][nt][0], O[mt][nt]);
       }
     }
   }
@@ -709,7 +729,7 @@ __global__ __launch_bounds__(256, 2) void tree_rows_kernel(TreeArgs a) {
   Request* const req_s = reinterpret_cast<Request*>(smem + Plan::kRing);
   RowsStage<D> st;
   st.k_lds = smem;
-  st.v_lds = smem + 4 * Plan::kStage;
+  st.v_lds = smem + Plan::kStages * Plan::kStage;
   st.mask_s = reinterpret_cast<uint32_t*>(req_s + a.n);
   int* const jump_s = reinterpret_cast<int*>(st.mask_s + a.max_nodes * kMaskRow);
   st.dead_s = reinterpret_cast<uint8_t*>(jump_s + a.max_nodes);
@@ -736,9 +756,10 @@ __global__ __launch_bounds__(256, 2) void tree_rows_kernel(TreeArgs a) {
     st.vb = a.v + r.hk * head_bytes;
     st.s0 = r.t0 * (kTile / SK);
     st.s1 = min(r.t1 * (kTile / SK), (r.total + SK - 1) / SK);
+    constexpr int kAhead = Plan::kStages - 1;
 #pragma unroll
-    for (int x = 0; x < 3; ++x) load_rows_stage<D>(a, r, st, st.s0 + x, rows_page<D>(a, r, st, st.s0 + x));
-    const int page = rows_page<D>(a, r, st, st.s0 + 3);
+    for (int x = 0; x < kAhead; ++x) load_rows_stage<D>(a, r, st, st.s0 + x, rows_page<D>(a, r, st, st.s0 + x));
+    const int page = rows_page<D>(a, r, st, st.s0 + kAhead);
     const bool tail = r.t1 * kTile > r.len, whole = r.t0 == 0 && r.t1 == r.tiles;
     if (tail) ancestors(a.parent + r.first, r.T, st.mask_s, jump_s, st.dead_s);
     const int slot = u == u_first ? 0 : 1;
