@@ -781,13 +781,32 @@ __global__ __launch_bounds__(256, 2) void tree_rows_kernel(TreeArgs a) {
   if (split_parts == 0 && tid == 0) ws.splits[blockIdx.x].parts = 0;
 }
 
-// Adds the parts of the row block that starts in workgroup blockIdx.x's stretch
-// and ends in a later one's; blockIdx.y four rows, a wave every fourth part.
-template <typename E, int D>
-__global__ __launch_bounds__(256) void tree_join_kernel(TreeArgs a, int groups, int RB) {
-  __shared__ float m_s[4][4], l_s[4][4], o_s[4][4][D];
+// Adds the parts of a row block that several workgroups share; blockIdx.y four rows,
+// a wave every W-th part.  blockIdx.x is the workgroup that has its first keys or
+// (W = 8), where a call has few row blocks of many rows, the block's rank among the
+// shared ones: then no workgroup comes for nothing, and each can have more waves.
+template <typename E, int D, int W>
+__global__ __launch_bounds__(64 * W) void tree_join_kernel(TreeArgs a, int groups, int RB) {
+  __shared__ float m_s[W][4], l_s[W][4], o_s[W][4][D];
   const Workspace ws(a.ws, groups, part_rows(a, RB), D);
-  const Split sp = ws.splits[blockIdx.x];
+  int group = blockIdx.x;
+  if constexpr (W == 8) {
+    // groups <= 512: each thread looks at one.
+    __shared__ int count_s[W], found_s;
+    const uint64_t there = __ballot((int)threadIdx.x < groups && ws.splits[threadIdx.x].parts != 0);
+    const int lane = threadIdx.x & 63, at = wave_id();
+    if (lane == 0) count_s[at] = __popcll(there);
+    if (threadIdx.x == 0) found_s = -1;
+    __syncthreads();
+    int before = 0;
+    for (int x = 0; x < at; ++x) before += count_s[x];
+    if ((there >> lane & 1) && before + __popcll(there & ((1ull << lane) - 1)) == (int)blockIdx.x)
+      found_s = threadIdx.x;
+    __syncthreads();
+    group = __builtin_amdgcn_readfirstlane(found_s);
+    if (group < 0) return;
+  }
+  const Split sp = ws.splits[group];
   const int row4 = blockIdx.y * 4;
   if (sp.parts == 0 || row4 >= sp.rows) return;
   const int tid = threadIdx.x, w = wave_id(), lr = (tid & 63) >> 4, od = (tid & 15) * (D / 16);
@@ -797,8 +816,8 @@ __global__ __launch_bounds__(256) void tree_join_kernel(TreeArgs a, int groups, 
 #pragma unroll
   for (int y = 0; y < D / 16; ++y) o[y] = 0.f;
 #pragma unroll 4
-  for (int p = w; p < sp.parts; p += 4) {
-    const float* from = ws.part(blockIdx.x + p, p == 0 ? sp.slot : 0, D) + row * (D + 2);
+  for (int p = w; p < sp.parts; p += W) {
+    const float* from = ws.part(group + p, p == 0 ? sp.slot : 0, D) + row * (D + 2);
     const f32x2 ml = *reinterpret_cast<const f32x2*>(from + D);
     dead |= ml[1] == -1.f;
     const float top = fmaxf(m, ml[0]);
@@ -820,11 +839,11 @@ __global__ __launch_bounds__(256) void tree_join_kernel(TreeArgs a, int groups, 
   for (int y = 0; y < D / 16; ++y) o_s[w][lr][od + y] = o[y];
   __syncthreads();
   if (w != 0 || row4 + lr >= sp.rows) return;
-  float top = -INFINITY, sum = 0.f, f[4];
+  float top = -INFINITY, sum = 0.f, f[W];
 #pragma unroll
-  for (int x = 0; x < 4; ++x) top = fmaxf(top, m_s[x][lr]);
+  for (int x = 0; x < W; ++x) top = fmaxf(top, m_s[x][lr]);
 #pragma unroll
-  for (int x = 0; x < 4; ++x) {
+  for (int x = 0; x < W; ++x) {
     f[x] = m_s[x][lr] == top ? 1.f : exp2_fast(m_s[x][lr] - top);
     dead |= l_s[x][lr] == -1.f;
     sum += l_s[x][lr] * f[x];
@@ -833,7 +852,7 @@ __global__ __launch_bounds__(256) void tree_join_kernel(TreeArgs a, int groups, 
   for (int y = 0; y < D / 16; ++y) {
     o[y] = 0.f;
 #pragma unroll
-    for (int x = 0; x < 4; ++x) o[y] += o_s[x][lr][od + y] * f[x];
+    for (int x = 0; x < W; ++x) o[y] += o_s[x][lr][od + y] * f[x];
   }
   write_row<E, D>(a, sp.first, sp.head, sp.row0 + row, od, o, dead || sum == 0.f ? 0.f : 1.f / sum);
 }
@@ -842,8 +861,16 @@ template <typename E, int D, typename Plan>
 hipError_t launch_join(const TreeArgs& a, hipStream_t s) {
   const hipError_t err = hipGetLastError();
   if (err != hipSuccess) return err;
-  const dim3 grid(Plan::kGroups, (part_rows(a, Plan::kRows) + 3) / 4);
-  tree_join_kernel<E, D><<<grid, 256, 0, s>>>(a, Plan::kGroups, Plan::kRows);
+  static_assert(Plan::kGroups <= 512, "one thread a workgroup");
+  const int rows = part_rows(a, Plan::kRows);
+  const int64_t blocks = (int64_t)a.n * a.Hkv * (((int64_t)a.G * a.max_nodes + Plan::kRows - 1) / Plan::kRows);
+  // Ranked: 16 nodes (64 rows) over 4093 tokens 22.4 -> 19.7 us, 64 nodes (512 rows)
+  // over 65537 117 -> 113; 4 rows over 2047 tokens 10.8 -> 12.0, 64 ragged trees
+  // 109 -> 113.
+  if (rows > 16 && blocks < Plan::kGroups / 4)
+    tree_join_kernel<E, D, 8><<<dim3((unsigned)blocks, (rows + 3) / 4), 512, 0, s>>>(a, Plan::kGroups, Plan::kRows);
+  else
+    tree_join_kernel<E, D, 4><<<dim3(Plan::kGroups, (rows + 3) / 4), 256, 0, s>>>(a, Plan::kGroups, Plan::kRows);
   return hipGetLastError();
 }
 
