@@ -81,32 +81,30 @@ __device__ __forceinline__ bf16x2 pack2(float a, float b) {
   return __builtin_convertvector(v, bf16x2);
 }
 
-// Whether any of eight bf16 values is an infinity or NaN, and the values with
-// those replaced by zero.
-__device__ __forceinline__ bool any_nonfinite(bf16x8 x) {
+// Nonzero where x holds an infinity or NaN: the top bit of each such element (an
+// exponent of ones, and only that, carries into it).
+__device__ __forceinline__ uint32_t nonfinite_bits(uint32_t two) {
+  return ((two & 0x7F807F80u) + 0x00800080u) & 0x80008000u;
+}
+__device__ __forceinline__ uint32_t any_nonfinite(bf16x8 x) {
   const u32x4 u = __builtin_bit_cast(u32x4, x);
-  bool bad = false;
+  return nonfinite_bits(u[0]) | nonfinite_bits(u[1]) | nonfinite_bits(u[2]) | nonfinite_bits(u[3]);
+}
+__device__ __forceinline__ uint32_t any_nonfinite(f32x4 x) {
+  uint32_t bad = 0;
 #pragma unroll
-  for (int i = 0; i < 4; ++i)
-    bad |= (u[i] & 0x7F80u) == 0x7F80u || (u[i] & 0x7F800000u) == 0x7F800000u;
+  for (int i = 0; i < 4; ++i) bad |= ((__float_as_uint(x[i]) & 0x7F800000u) + 0x00800000u) & 0x80000000u;
   return bad;
 }
+// x with those elements zero.
 __device__ __forceinline__ bf16x8 finite_only(bf16x8 x) {
   u32x4 u = __builtin_bit_cast(u32x4, x);
 #pragma unroll
   for (int i = 0; i < 4; ++i) {
-    if ((u[i] & 0x7F80u) == 0x7F80u) u[i] &= 0xFFFF0000u;
-    if ((u[i] & 0x7F800000u) == 0x7F800000u) u[i] &= 0xFFFFu;
+    const uint32_t t = nonfinite_bits(u[i]) >> 15;
+    u[i] &= ~((t << 16) - t);  // a bit becomes its half's sixteen
   }
   return __builtin_bit_cast(bf16x8, u);
-}
-
-__device__ __forceinline__ bool any_nonfinite(f32x4 x) {
-  const u32x4 u = __builtin_bit_cast(u32x4, x);
-  bool bad = false;
-#pragma unroll
-  for (int i = 0; i < 4; ++i) bad |= (u[i] & 0x7F800000u) == 0x7F800000u;
-  return bad;
 }
 __device__ __forceinline__ f32x4 finite_only(f32x4 x) {
 #pragma unroll
@@ -114,20 +112,17 @@ __device__ __forceinline__ f32x4 finite_only(f32x4 x) {
     if ((__float_as_uint(x[i]) & 0x7F800000u) == 0x7F800000u) x[i] = 0.f;
   return x;
 }
+// 1 for each of those elements, 0 for the others.
+__device__ __forceinline__ bf16x8 nonfinite_ones(bf16x8 x) {
+  u32x4 u = __builtin_bit_cast(u32x4, x);
+#pragma unroll
+  for (int i = 0; i < 4; ++i) u[i] = (nonfinite_bits(u[i]) >> 15) * 0x3F80u;
+  return __builtin_bit_cast(bf16x8, u);
+}
 __device__ __forceinline__ f32x4 nonfinite_ones(f32x4 x) {
 #pragma unroll
   for (int i = 0; i < 4; ++i) x[i] = (__float_as_uint(x[i]) & 0x7F800000u) == 0x7F800000u ? 1.f : 0.f;
   return x;
-}
-
-// 1 where a value is an infinity or NaN, else 0.
-__device__ __forceinline__ bf16x8 nonfinite_ones(bf16x8 x) {
-  u32x4 u = __builtin_bit_cast(u32x4, x);
-#pragma unroll
-  for (int i = 0; i < 4; ++i)
-    u[i] = ((u[i] & 0x7F80u) == 0x7F80u ? 0x3F80u : 0u) |
-           ((u[i] & 0x7F800000u) == 0x7F800000u ? 0x3F800000u : 0u);
-  return __builtin_bit_cast(bf16x8, u);
 }
 
 }  // namespace s2moe

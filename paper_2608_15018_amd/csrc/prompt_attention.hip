@@ -264,35 +264,45 @@ __global__ __launch_bounds__(256, (PromptTile<D, NT>::kPerCu)) void prompt_bf16_
       for (int i = 0; i < 16; ++i)
         if (32 * j + 16 * (i >> 3) + 8 * h + (i & 7) > tok[nt]) T[nt][i] = -INFINITY;
   };
-  // The second product where some rows do not see some keys: a weight of zero
-  // does not hide an infinity or NaN, so those values count as zero, and where a
-  // weight meets one the row's sum becomes NaN.
-  const auto products_v_masked = [&](int j, const bf16x8(&W)[2][NT]) {
-    bool bad = false;
+  // The second product of step j.  Where some rows do not see some keys a weight of
+  // zero does not hide an infinity or NaN, so those values count as zero there, and
+  // where a weight meets one the row's sum becomes NaN.
+  const auto products_v_checked = [&](int j, bool masked, const bf16x8(&W)[2][NT]) {
+    bf16x8 vf[2][MT];
 #pragma unroll
     for (int ks = 0; ks < 2; ++ks)
 #pragma unroll
-      for (int mt = 0; mt < MT; ++mt) {
-        const bf16x8 vf = value_tile(j, ks, mt);
-        bad |= any_nonfinite(vf);
-        const bf16x8 fine = finite_only(vf);
+      for (int mt = 0; mt < MT; ++mt) vf[ks][mt] = value_tile(j, ks, mt);
+    if (masked) {
+      uint32_t bad = 0;
 #pragma unroll
-        for (int nt = 0; nt < NT; ++nt)
-          O[mt][nt] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(fine, W[ks][nt], O[mt][nt], 0, 0, 0);
+      for (int ks = 0; ks < 2; ++ks)
+#pragma unroll
+        for (int mt = 0; mt < MT; ++mt) bad |= any_nonfinite(vf[ks][mt]);
+      if (__builtin_expect(__any(bad != 0), 0)) {
+#pragma unroll
+        for (int mt = 0; mt < MT; ++mt) {
+#pragma unroll
+          for (int nt = 0; nt < NT; ++nt) {
+            f32x16 met = {};
+#pragma unroll
+            for (int ks = 0; ks < 2; ++ks)
+              met = __builtin_amdgcn_mfma_f32_32x32x16_bf16(nonfinite_ones(vf[ks][mt]), W[ks][nt], met, 0, 0, 0);
+#pragma unroll
+            for (int i = 0; i < 16; ++i) O[mt][nt][i] = met[i] != 0.f ? NAN : O[mt][nt][i];
+          }
+#pragma unroll
+          for (int ks = 0; ks < 2; ++ks) vf[ks][mt] = finite_only(vf[ks][mt]);
+        }
       }
-    if (__builtin_expect(__any(bad), 0)) {
+    }
+#pragma unroll
+    for (int ks = 0; ks < 2; ++ks)
 #pragma unroll
       for (int mt = 0; mt < MT; ++mt)
 #pragma unroll
-        for (int nt = 0; nt < NT; ++nt) {
-          f32x16 met = {};
-#pragma unroll
-          for (int ks = 0; ks < 2; ++ks)
-            met = __builtin_amdgcn_mfma_f32_32x32x16_bf16(nonfinite_ones(value_tile(j, ks, mt)), W[ks][nt], met, 0, 0, 0);
-#pragma unroll
-          for (int i = 0; i < 16; ++i) O[mt][nt][i] = met[i] != 0.f ? NAN : O[mt][nt][i];
-        }
-    }
+        for (int nt = 0; nt < NT; ++nt)
+          O[mt][nt] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(vf[ks][mt], W[ks][nt], O[mt][nt], 0, 0, 0);
   };
   load_k(0);
   if constexpr (kRing == 4) load_k(1);
@@ -406,7 +416,7 @@ __global__ __launch_bounds__(256, (PromptTile<D, NT>::kPerCu)) void prompt_bf16_
       if (j >= n_full) mask(j, SA);
       raise(SA, PA);
       weights(SA, PA);
-      if (j < n_full) products_v(j, PA); else products_v_masked(j, PA);
+      products_v_checked(j, j >= n_full, PA);
     }
   }
   wait_loads<0>();  // no load into this workgroup's LDS outlives it
@@ -537,10 +547,10 @@ __global__ __launch_bounds__(256, 2) void prompt_f32_kernel(PromptArgs a) {
         l[nt] += P[nt][e];
       }
     if (masked) {  // as in the bf16 kernel
-      bool bad = false;
+      uint32_t bad = 0;
 #pragma unroll
       for (int mt = 0; mt < MT; ++mt) bad |= any_nonfinite(V[mt]);
-      if (__any(bad))
+      if (__any(bad != 0))
 #pragma unroll
         for (int mt = 0; mt < MT; ++mt) {
 #pragma unroll

@@ -268,12 +268,12 @@ __device__ __forceinline__ void raise(const float (&m)[NT], float (&shift)[NT], 
 // becomes NaN.
 template <int MT, int NT, int VC, typename frag>
 __device__ __forceinline__ void hide_nonfinite(frag (&V)[MT][VC], const frag (&P)[NT][VC], f32x4 (&O)[MT][NT]) {
-  bool bad = false;
+  uint32_t bad = 0;
 #pragma unroll
   for (int mt = 0; mt < MT; ++mt)
 #pragma unroll
     for (int y = 0; y < VC; ++y) bad |= any_nonfinite(V[mt][y]);
-  if (!__any(bad)) return;
+  if (!__any(bad != 0)) return;
 #pragma unroll
   for (int mt = 0; mt < MT; ++mt) {
 #pragma unroll
