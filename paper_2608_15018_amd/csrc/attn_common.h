@@ -76,6 +76,10 @@ __device__ __forceinline__ void wait_loads() {  // until at most N are in flight
   asm volatile("s_waitcnt vmcnt(%0)" : : "n"(N) : "memory");
 }
 
+// Until this wave's reads of LDS are done: before a barrier after which other
+// waves load over what was read.
+__device__ __forceinline__ void wait_lds() { asm volatile("s_waitcnt lgkmcnt(0)" : : : "memory"); }
+
 __device__ __forceinline__ bf16x2 pack2(float a, float b) {
   const f32x2 v = {a, b};
   return __builtin_convertvector(v, bf16x2);

@@ -410,6 +410,7 @@ __global__ __launch_bounds__(256, (PromptTile<D, NT>::kPerCu)) void prompt_bf16_
   }
   }
   for (; s < n_stage; ++s) {
+    wait_lds();
     sync(s);
     for (int j = 2 * s; j < 2 * s + 2 && j < n_all; ++j) {
       products_k(j, SA);

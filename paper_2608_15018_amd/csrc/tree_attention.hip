@@ -617,6 +617,7 @@ __device__ __forceinline__ void rows_stretch(const TreeArgs& a, const Stretch& r
     // Stage s is there for everybody, and the stage before, whose place is loaded
     // into, is read by nobody any more.
     wait_loads<(Plan::kStages - 2) * 2 * kLoads>();
+    wait_lds();
     __builtin_amdgcn_s_barrier();
     load_rows_stage<D>(a, r, st, s + Plan::kStages - 1, page);
     page = rows_page<D>(a, r, st, s + Plan::kStages);
