@@ -541,7 +541,8 @@ hipError_t launch_kv_free(const KvCache& c, int n, const int32_t* seqs, int32_t*
 
 hipError_t launch_kv_append(const KvCache& c, const AppendArgs& a, hipStream_t s) {
   // A wave takes a token where requests bring few, else eight, of which about one
-  // begins a group.
+  // begins a group.  us at one / eight, 8 heads of 128: 48 requests of 1 token 5.3 / 6.8,
+  // 16 of 6 5.5 / 6.6, 16 of 16 5.5 / 5.5, 5 of 3000 35 / 21.
   const bool few = a.n_tokens / a.n < 8;
   const int per = few ? 4 : 32;
   const dim3 grid((a.n_tokens + per - 1) / per, c.Hkv);

@@ -1,12 +1,37 @@
-// Causal attention of packed prompts: one wave per (token, query head).
+// Causal attention of packed prompts.
+//
+// Rows.  As over the cache: the G = Hq / Hkv query heads of a kv head read the same
+// keys, so a prompt of len tokens is len G rows, row r token r / G, and a workgroup
+// takes consecutive ones.  Consecutive rows are few tokens, so little of the
+// triangle's edge is computed in vain.
+//
+// Products (bf16).  S^T = K Q^T and O^T = V^T P^T in 32 x 32 x 16 matrix
+// instructions: a lane holds scores of one row, and they are, in the registers where
+// the first product leaves them, the operand of the second.  Keys and values come
+// through LDS, 64 tokens a stage, by loads that need no register; values, which the
+// second product wants by columns, are read with LDS's transposing load.
+//
+// Softmax.  One pass, the running maximum moved only when it is 2^8 behind.  In bf16
+// the weights enter the second product rounded to bf16 (its operands have one type);
+// their sum is taken in fp32 before that.
+//
+// Bound: the matrix cores at D = 128 (12289 tokens, 32/4 heads: 1.16-1.22 ms, 1.02-1.06
+// PFLOP/s where a large library product reaches 1.25), the weights' vector
+// instructions at D = 64 (8192 tokens, 64/8 heads: 0.57 ms, 0.97 PFLOP/s); short
+// prompts by what a workgroup waits for before its first product (24 of 512 tokens,
+// 32/8 heads of 128: 93 us, 0.55 PFLOP/s).
 #include "attention.h"
 #include "attn_common.h"
 
-#ifndef S2MOE_PROMPT_SHORT
-#define S2MOE_PROMPT_SHORT 1024
-#endif
 namespace s2moe {
 namespace {
+
+// Prompts of at most so many tokens on average take 32 rows a wave, so that two or
+// three workgroups share a compute unit and hide each other's starts.  us at 32 / 64
+// rows a wave, 32/8 heads of 128: 96 x 128 tokens 67 / 90, 24 x 512 93 / 114, 12 x 1024
+// 140 / 160, 8 x 2048 340 / 322; 64/8 heads of 64: 59 / 63, 96 / 99, 149 / 151, 357 /
+// 340.  Between 1280 and 1792 tokens 128 gains and 64 loses up to 5 %.
+constexpr int kShortPrompt = 1024;
 
 // Workgroup b of a kv head: which rows of which prompt.  Prompts take
 // ceil(len G / rows) workgroups each, last ones first (they see the most
@@ -399,6 +424,8 @@ __global__ __launch_bounds__(256, (PromptTile<D, NT>::kPerCu)) void prompt_bf16_
     raise(SB, PA);
 #pragma unroll
     for (int i = 0; i < 4; ++i) ahead[i] = key_tile(2, i);
+    // Nothing waits for LDS before the barrier: the reads of what is loaded over
+    // afterwards went into scores and sums that the step before it has used.
     for (s = 1; s < n_fast; ++s) {
       step(2 * s - 1, SB, SA, PA, PB, ahead);
       sync(s);
@@ -454,7 +481,8 @@ __global__ __launch_bounds__(256, (PromptTile<D, NT>::kPerCu)) void prompt_bf16_
 // LDS: a wave takes 32 rows and reads keys and values of 16 tokens a step into
 // registers, the next step's as soon as this one's are used.  Their operands hold one
 // k a lane, so values need no transposition: step e of a product takes key 4 g + e of
-// lane group g, where the scores of those keys are.
+// lane group g, where the scores of those keys are.  4 prompts of 1024 tokens: 0.44 ms
+// with 32/8 heads of 128 (78 TFLOP/s; a large library product reaches 153).
 // SPLIT: the four waves share 32 rows and take every fourth step, and their sums
 // are added at the end.
 template <int D, bool SPLIT>
@@ -631,14 +659,23 @@ hipError_t launch_bf16(const PromptArgs& a, hipStream_t s) {
 
 template <int D>
 hipError_t launch_bf16(const PromptArgs& a, hipStream_t s) {
-  return a.n_tokens / a.n < S2MOE_PROMPT_SHORT ? launch_bf16<D, 1>(a, s) : launch_bf16<D, 2>(a, s);
+  // Also where 64 rows a wave would make hardly more than the workgroups that run at
+  // once.  us at 32 / 64 rows a wave, one prompt, 32/8 heads of 128: 1536 tokens 42 / 50,
+  // 2048 57 / 63, 4000 148 / 137; 64/8 heads of 64: 33 / 44, 48 / 57, 3000 98 / 91.
+  typedef PromptTile<D, 2> Wide;
+  const int64_t wide = ((int64_t)a.n_tokens * a.G / Wide::kRows + a.n) * a.Hkv;
+  const bool few = wide <= 288 * Wide::kPerCu;
+  return few || a.n_tokens / a.n <= kShortPrompt ? launch_bf16<D, 1>(a, s) : launch_bf16<D, 2>(a, s);
 }
 
 template <int D>
 hipError_t launch_f32(const PromptArgs& a, hipStream_t s) {
-  // By keys while rows alone would not give every SIMD of the GPU a wave.
+  // By keys while rows alone would not give every SIMD of the GPU a wave, and for long
+  // prompts, whose workgroups of 32 rows end more evenly than those of 128.  us by keys
+  // / by rows: 3 x 150 tokens, 4/2 heads of 64, 9 / 16; 32/8 heads of 128: 64 x 64 96 /
+  // 63, 32 x 128 118 / 107, 16 x 256 162 / 194, 4 x 1024 440 / 588, 1 x 4096 1549 / 1757 (but 4 x 256 54 / 47).
   const auto blocks = [&](int rows) { return ((int64_t)a.n_tokens * a.G / rows + a.n) * a.Hkv; };
-  if (blocks(32) < 1024)
+  if (blocks(32) < 1024 || a.n_tokens / a.n >= 256)
     prompt_f32_kernel<D, true><<<(unsigned)blocks(32), 256, 0, s>>>(a);
   else
     prompt_f32_kernel<D, false><<<(unsigned)blocks(128), 256, 0, s>>>(a);

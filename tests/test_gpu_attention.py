@@ -413,3 +413,52 @@ def test_prompt_offsets_past_32_bits(dtype):
     ref = ao.prompt_attention(*(t[-90:].double().cpu().numpy() for t in (q, k, v)), [0, 10, 90], D ** -0.5)
     check(out[-90:], ref, dtype)
     assert not out[:-90].any()
+
+
+# Many heads and long prompts: 64 rows a wave in bf16, in fp32 the keys split over the waves.
+WIDE = [(64, 32, 128), (64, 32, 64)]
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("heads", WIDE)
+def test_prompt_many_rows(dtype, heads):
+    run_prompt(dtype, heads, [1187, 1290], seed=21)
+
+
+@pytest.mark.parametrize("heads", WIDE)
+def test_prompt_many_rows_large_scores(heads):
+    run_prompt("bf16", heads, [1187, 1290], seed=22, qscale=40.0, scale=0.5)
+
+
+@pytest.mark.parametrize("heads", WIDE)
+def test_prompt_many_rows_rising_scores(heads):
+    Hq, Hkv, D = heads
+    n = 1201
+    g = torch.Generator(device="cuda").manual_seed(23)
+    k = torch.zeros((2 * n, Hkv, D), device="cuda")
+    k[:, :, 0] = (torch.arange(2 * n, device="cuda") % n // 8)[:, None]
+    q = torch.ones((2 * n, Hq, D), device="cuda").bfloat16()
+    k, v = k.bfloat16(), torch.randn((2 * n, Hkv, D), generator=g, device="cuda").bfloat16()
+    out = s2.prompt_attention(q, k, v, ints([0, n, 2 * n]), scale=3.0)
+    check(out, ao.prompt_attention(*(t.double().cpu().numpy() for t in (q, k, v)), [0, n, 2 * n], 3.0), "bf16")
+
+
+@pytest.mark.parametrize("heads", WIDE)
+@pytest.mark.parametrize("at", [0, 700, 1180])
+def test_prompt_many_rows_later_tokens_do_not_matter(heads, at):
+    Hq, Hkv, D = heads
+    g = torch.Generator(device="cuda").manual_seed(24)
+    q, k, v = (torch.randn((2477, h, D), generator=g, device="cuda").bfloat16() for h in (Hq, Hkv, Hkv))
+    off = ints([0, 1187, 2477])
+    out = s2.prompt_attention(q, k, v, off)
+    k[at], v[at] = float("nan"), float("nan")
+    got = s2.prompt_attention(q, k, v, off)
+    assert torch.equal(got[:at], out[:at]) and torch.equal(got[1187:], out[1187:])
+    assert torch.isnan(got[at:1187]).all()
+
+
+@pytest.mark.parametrize("D", [64, 128])
+def test_prompt_f32_many_short(D):
+    """Short prompts, but many rows: a wave takes rows of its own."""
+    r = np.random.default_rng(25)
+    run_prompt("f32", (32, 8, D), [0, 1, 255] + r.integers(0, 130, 40).tolist(), seed=25)
