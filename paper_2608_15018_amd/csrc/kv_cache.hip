@@ -6,6 +6,13 @@
 // workgroup for all of them (reserve, whose grants depend on each other);
 // what they decide does not depend on timing: a free page is one that nobody
 // holds, and the lowest ids are taken first, in the order of the requests.
+//
+// Bound: latency for the integer work (64 requests: fork, free and the end of commit
+// 5 us each, reserve 11), memory for the
+// copies (the used slots of 16 pages of 64 tokens to four branches each, 24 layers, 8
+// heads of 128, 239 MB written and 60 read: 69 us, 4.3 TB/s) and the move (up to 16
+// accepted tokens of each branch over the same layers: 42 us, 2.2 TB/s) and
+// for new tokens (about 17000, 8 heads of 128: 34 us where a large copy takes 28).
 #include <type_traits>
 
 #include "attention.h"
