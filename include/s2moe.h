@@ -390,10 +390,12 @@ s2moe_status s2moe_kv_fork(const s2moe_kv_cache *cache, int32_t n, const int32_t
    first of them falls into a page that other sequences hold too, that page is
    copied first (its used slots, rounded up to a multiple of 8, in every
    layer), so that later writes reach no other sequence; of the sequences
-   that share a page, the last to ask keeps it.  Pages already reserved are
-   counted.  Requests are granted in order until the free pages run out: the
-   first that does not fit and every later one that needs a page get
-   S2MOE_KV_NO_PAGES.  Lengths do not change.
+   that share a page, the last to ask keeps it, once the others have their
+   copies.  Pages already reserved are counted.  Requests are granted in order
+   until the free pages run out: the first that does not fit and every later
+   one that needs a page get S2MOE_KV_NO_PAGES, the last of those that share a
+   page too if one of the others was refused its copy.  A request of status 0
+   can write all its slots.  Lengths do not change.
    seqs, extra, status: [n] int32; copied [n][2] int32 receives the page copied
    from and to, or -1 (the list of the copying launch). */
 s2moe_status s2moe_kv_reserve(const s2moe_kv_cache *cache, int32_t n, const int32_t *seqs,

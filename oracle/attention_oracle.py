@@ -127,28 +127,32 @@ class Cache:
                 want.append(None)
                 continue
             new = max(0, -(-(length + e) // self.P) - self.held(s))
-            copy = None
+            shared = copy = None
             if e > 0 and length % self.P:
                 p = int(self.table[s, length // self.P])
                 if self.refs[p] > 1:
+                    shared = p
                     rank = sharers.get(p, 0)
                     sharers[p] = rank + 1
                     copy = p if self.refs[p] - rank > 1 else None
             status.append(0)
-            want.append((new, copy))
+            want.append((new, copy, shared))
         free = [p for p in range(len(self.refs)) if self.refs[p] == 0]
         copied = np.full((n, 2), -1, dtype=np.int32)
         used, room = 0, len(free)
+        stay = set()  # shared pages whose copy was refused: the sharer holds them still
         for i in range(n):
             if want[i] is None:
                 continue
-            new, copy = want[i]
+            new, copy, shared = want[i]
             take = new + (copy is not None)
-            if take == 0:
-                continue
             used += take
-            if used > room:
+            if (take and used > room) or shared in stay:
                 status[i] = NO_PAGES
+                if copy is not None:
+                    stay.add(copy)
+                continue
+            if take == 0:
                 continue
             mine = free[used - take:used]
             s = int(seqs[i])

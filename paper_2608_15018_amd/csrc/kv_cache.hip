@@ -184,7 +184,7 @@ __global__ __launch_bounds__(1024) void kv_reserve_kernel(KvCache c, int n,
   }
   shared_s[i] = page;
   __syncthreads();
-  // Of the sequences that share a page the last keeps it.
+  // Of the sequences that share a page the last keeps it, if the others get their copies.
   const int copy = page >= 0 && refs - count_before(shared_s, i, page) > 1;
   const int take = need + copy;
   int total;
@@ -244,9 +244,16 @@ __global__ __launch_bounds__(1024) void kv_reserve_kernel(KvCache c, int n,
       __syncthreads();  // first_s and its like are complete
     }
   }
+  bool refused = take > 0 && first + take > free_pages;
+  if (total > free_pages) {
+    // Who got no copy still holds the page: the last sharer cannot write to it either.
+    shared_s[i] = refused && copy ? page : -1;
+    __syncthreads();
+    refused |= page >= 0 && !copy && count_before(shared_s, i, page) > 0;
+  }
   __syncthreads();  // to_s is complete
   if (live) {
-    if (take > 0 && first + take > free_pages) st = kKvNoPages;
+    if (refused) st = kKvNoPages;
     const int to = st ? -1 : to_s[i];
     if (to >= 0) {
       row[last] = to;
