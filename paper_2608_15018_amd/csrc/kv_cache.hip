@@ -105,20 +105,20 @@ __global__ __launch_bounds__(256) void kv_free_kernel(KvCache c, const int32_t* 
 }
 
 // Sum of x over the threads before this one; *total over all.
-__device__ int scan_block(int x, int* total, int* waves) {
+__device__ int64_t scan_block(int64_t x, int64_t* total, int64_t* waves) {
   const int lane = threadIdx.x & 63, w = threadIdx.x >> 6, nw = blockDim.x >> 6;
-  int inc = x;
+  int64_t inc = x;
 #pragma unroll
   for (int d = 1; d < 64; d <<= 1) {
-    const int y = __shfl_up(inc, d);
+    const int64_t y = __shfl_up(inc, d);
     if (lane >= d) inc += y;
   }
   __syncthreads();  // `waves` is free again
   if (lane == 63) waves[w] = inc;
   __syncthreads();
-  int before = 0, all = 0;
+  int64_t before = 0, all = 0;
   for (int j = 0; j < nw; ++j) {
-    const int y = waves[j];
+    const int64_t y = waves[j];
     before += j < w ? y : 0;
     all += y;
   }
@@ -146,6 +146,7 @@ __global__ __launch_bounds__(1024) void kv_reserve_kernel(KvCache c, int n,
                                                           int32_t* __restrict__ status) {
   __shared__ __attribute__((aligned(16))) int seq_s[1024], shared_s[1024];
   __shared__ int first_s[1024], held_s[1024], copy_s[1024], to_s[1024], waves[16];
+  __shared__ int64_t sums_s[16];
   const int i = threadIdx.x, lane = i & 63, w = i >> 6, nw = blockDim.x >> 6;
   const bool live = i < n;
   const int s = live ? seqs[i] : -1;
@@ -187,9 +188,11 @@ __global__ __launch_bounds__(1024) void kv_reserve_kernel(KvCache c, int n,
   // Of the sequences that share a page the last keeps it, if the others get their copies.
   const int copy = page >= 0 && refs - count_before(shared_s, i, page) > 1;
   const int take = need + copy;
-  int total;
-  const int first = scan_block(take, &total, waves);
-  first_s[i] = first;
+  // 1024 requests of up to 2^27 pages pass 32 bits; past the pool's pages all are alike.
+  int64_t all;
+  const int64_t first = scan_block(take, &all, sums_s);
+  const int total = (int)min(all, (int64_t)c.n_pages + 1);
+  first_s[i] = (int)min(first, (int64_t)c.n_pages + 1);
   held_s[i] = held;
   copy_s[i] = copy;
   // How many free pages there are, up to `total`; then who gets which.

@@ -143,3 +143,19 @@ def test_many_sharers_of_one_page():
     assert c.reserve(order, [1] * 1000) == [0] * 600 + [ao.NO_PAGES] * 400
     c.free(order[600:999])
     assert c.reserve([order[999]], [1]) == [0]
+
+
+@pytest.mark.gpu
+def test_wants_that_add_up_to_more_than_32_bits():
+    """40 requests of 2^27 - 1 pages each: none fits, and the sums of what they want do not wrap."""
+    import paper_2608_15018_amd as s2
+    import torch
+
+    maxp, n = (1 << 27) - 1, 40
+    c = s2.KVCache(1, 1, 64, 12, 16, n + 2, maxp)
+    ints = lambda x: torch.tensor(x, dtype=torch.int32, device="cuda")  # noqa: E731
+    order = [n] + list(range(n)) + [n + 1]
+    c.reserve(ints(order), ints([40] + [16 * maxp] * n + [0]))
+    assert c.status[:n + 2].tolist() == [0] + [ao.NO_PAGES] * n + [0]
+    assert c.refs.tolist() == [1, 1, 1] + [0] * 9 and c.table[n, :4].tolist() == [0, 1, 2, -1]
+    assert int((c.table[:n] >= 0).sum()) == 0
