@@ -59,6 +59,14 @@ def _rows(t, name, heads, head_dim, dtype):
     return t.data_ptr(), s0 if n > 1 else heads * head_dim, n
 
 
+def _same_gpu(dev, **tensors):
+    """Every tensor on GPU `dev`: the kernels follow its pointer."""
+    for name, t in tensors.items():
+        if dev < 0 or t.get_device() != dev:
+            where = f"GPU {dev}" if dev >= 0 else "a GPU"
+            raise _lib.S2moeError(_lib.EINVAL, f"{name} is on {t.device}, not on {where}")
+
+
 class KVCache:
     """Pages of keys and values of `n_layers` layers for up to `max_seqs`
     sequences of up to `max_pages` pages each.  Allocates the arrays that are
@@ -91,6 +99,8 @@ class KVCache:
         self.n_pages, self.page_size = n_pages, page_size
         self.max_seqs, self.max_pages, self.dtype = max_seqs, max_pages, dtype
         dev = self.k.device
+        self._gpu = self.k.get_device()
+        _same_gpu(self._gpu, **{name: getattr(self, name) for name in want})
         self.status = torch.zeros(KV_MAX_REQUESTS, dtype=i32, device=dev)
         self.copied = torch.full((KV_MAX_REQUESTS, 2), -1, dtype=i32, device=dev)
         self.struct = _lib.KvCacheStruct(n_layers, n_kv_heads, head_dim, n_pages, page_size,
@@ -110,16 +120,18 @@ class KVCache:
     def fork(self, src, dst, stream=None):
         """Sequence dst[i] becomes a copy of src[i] on the same pages."""
         n = src.shape[0]
-        _lib._check(self._lib.s2moe_kv_fork(self._ref, n, _ints(src, "src", n),
-                                            _ints(dst, "dst", n), self._status,
+        ps, pd = _ints(src, "src", n), _ints(dst, "dst", n)
+        _same_gpu(self._gpu, src=src, dst=dst)
+        _lib._check(self._lib.s2moe_kv_fork(self._ref, n, ps, pd, self._status,
                                             _lib._stream(stream)))
 
     def reserve(self, seqs, extra, stream=None):
         """Pages for extra[i] more tokens of seqs[i]; a shared page that they
         would be written to is copied."""
         n = seqs.shape[0]
-        _lib._check(self._lib.s2moe_kv_reserve(self._ref, n, _ints(seqs, "seqs", n),
-                                               _ints(extra, "extra", n), self._copied,
+        ps, pe = _ints(seqs, "seqs", n), _ints(extra, "extra", n)
+        _same_gpu(self._gpu, seqs=seqs, extra=extra)
+        _lib._check(self._lib.s2moe_kv_reserve(self._ref, n, ps, pe, self._copied,
                                                self._status, _lib._stream(stream)))
 
     def append(self, layer: int, k, v, seqs, tok_off, stream=None):
@@ -130,9 +142,10 @@ class KVCache:
         vp, ldv, tv = _rows(v, "v", self.n_kv_heads, self.head_dim, self.dtype)
         if tv != t:
             raise ValueError(f"v holds {tv} tokens, k {t}")
-        _lib._check(self._lib.s2moe_kv_append(self._ref, layer, n, t, _ints(seqs, "seqs", n),
-                                              _ints(tok_off, "tok_off", n + 1), kp, ldk, vp,
-                                              ldv, _lib._stream(stream)))
+        ps, po = _ints(seqs, "seqs", n), _ints(tok_off, "tok_off", n + 1)
+        _same_gpu(self._gpu, k=k, v=v, seqs=seqs, tok_off=tok_off)
+        _lib._check(self._lib.s2moe_kv_append(self._ref, layer, n, t, ps, po, kp, ldk, vp, ldv,
+                                              _lib._stream(stream)))
 
     def commit(self, seqs, path, n_accept, stream=None):
         """Keeps nodes path[i, :n_accept[i]] of each drafted tree (ascending);
@@ -143,15 +156,20 @@ class KVCache:
         if path is not None:
             _lib._expect(path, "path", _I32, (n, most))
             pp = _lib._ptr(path)
-        _lib._check(self._lib.s2moe_kv_commit(self._ref, n, most, _ints(seqs, "seqs", n), pp,
-                                              _ints(n_accept, "n_accept", n), self._status,
+        ps, pa = _ints(seqs, "seqs", n), _ints(n_accept, "n_accept", n)
+        _same_gpu(self._gpu, seqs=seqs, n_accept=n_accept)
+        if path is not None:
+            _same_gpu(self._gpu, path=path)
+        _lib._check(self._lib.s2moe_kv_commit(self._ref, n, most, ps, pp, pa, self._status,
                                               _lib._stream(stream)))
 
     def free(self, seqs, stream=None):
         """Empties the sequences."""
         n = seqs.shape[0]
-        _lib._check(self._lib.s2moe_kv_free(self._ref, n, _ints(seqs, "seqs", n),
-                                            self._status, _lib._stream(stream)))
+        ps = _ints(seqs, "seqs", n)
+        _same_gpu(self._gpu, seqs=seqs)
+        _lib._check(self._lib.s2moe_kv_free(self._ref, n, ps, self._status,
+                                            _lib._stream(stream)))
 
 
 class TreeAttention:
@@ -181,6 +199,9 @@ class TreeAttention:
             raise ValueError(f"{n} sequences, the workspace is for {self.max_seqs}")
         D, Hq = c.head_dim, self.n_heads
         qp, ldq, t = _rows(q, "q", Hq, D, c.dtype)
+        ps, po = _ints(seqs, "seqs", n), _ints(tok_off, "tok_off", n + 1)
+        pp = _ints(parent, "parent", t)
+        _same_gpu(c._gpu, q=q, seqs=seqs, tok_off=tok_off, parent=parent)
         if out is None:
             out = q.new_empty((t, Hq, D))
             op, ldo = out.data_ptr(), Hq * D
@@ -188,10 +209,10 @@ class TreeAttention:
             op, ldo, to = _rows(out, "out", Hq, D, c.dtype)
             if to != t:
                 raise ValueError(f"out holds {to} tokens, q {t}")
+            _same_gpu(c._gpu, out=out)
         self.attn.ldq, self.attn.ldo = ldq, ldo
         _lib._check(self._lib.s2moe_tree_attention(
-            c._ref, layer, self._ref, n, t, self.max_nodes, qp, _ints(seqs, "seqs", n),
-            _ints(tok_off, "tok_off", n + 1), _ints(parent, "parent", t),
+            c._ref, layer, self._ref, n, t, self.max_nodes, qp, ps, po, pp,
             self.workspace.data_ptr(), self.bytes, op, _lib._stream(stream)))
         return out
 
@@ -217,7 +238,8 @@ def prompt_attention(q, k, v, tok_off, out=None, scale: float | None = None, str
     a = _lib.Attn(Hq, Hkv, D, _code(dt), D ** -0.5 if scale is None else scale, ldq, ldk, ldv,
                   ldo)
     n = tok_off.shape[0] - 1
-    _lib._check(_lib.load().s2moe_prompt_attention(
-        ctypes.byref(a), n, t, qp, kp, vp, _ints(tok_off, "tok_off", n + 1), op,
-        _lib._stream(stream)))
+    po = _ints(tok_off, "tok_off", n + 1)
+    _same_gpu(q.get_device(), q=q, k=k, v=v, tok_off=tok_off, out=out)
+    _lib._check(_lib.load().s2moe_prompt_attention(ctypes.byref(a), n, t, qp, kp, vp, po, op,
+                                                   _lib._stream(stream)))
     return out

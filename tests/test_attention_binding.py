@@ -1,0 +1,106 @@
+"""The Python side of the cache and attention operators, without a GPU: the library is
+replaced by a recorder, and tensors on the host that say they are on a GPU stand for
+tensors there."""
+
+import pytest
+
+torch = pytest.importorskip("torch")
+
+import paper_2608_15018_amd as s2  # noqa: E402
+from paper_2608_15018_amd import _lib, attention  # noqa: E402
+
+
+class OnGpu(torch.Tensor):
+    """A host tensor that says it is on GPU 0."""
+
+    def get_device(self):
+        return 0
+
+
+def gpu(t):
+    return t.as_subclass(OnGpu)
+
+
+def ints(x):
+    return torch.tensor(x, dtype=torch.int32)
+
+
+class Recorder:
+    """Every entry point: notes its name and arguments and reports success."""
+
+    def __init__(self):
+        self.calls = []
+
+    def __getattr__(self, name):
+        def call(*args):
+            self.calls.append((name, args))
+            return 64 if name.endswith("workspace_bytes") else _lib.OK
+        return call
+
+
+@pytest.fixture
+def lib(monkeypatch):
+    r = Recorder()
+    monkeypatch.setattr(_lib, "load", lambda: r)
+    return r
+
+
+L, HKV, D, PAGES, P, S, MAXP, HQ, BF16 = 2, 2, 64, 6, 16, 4, 3, 4, torch.bfloat16
+
+
+def arrays():
+    return dict(k=torch.zeros((L, PAGES, HKV, P, D), dtype=BF16), v=torch.zeros((L, PAGES, HKV, P // 8, D, 8), dtype=BF16),
+                table=torch.full((S, MAXP), -1, dtype=torch.int32), length=torch.zeros(S, dtype=torch.int32),
+                refs=torch.zeros(PAGES, dtype=torch.int32))
+
+
+def make_cache(**kw):
+    return s2.KVCache(L, HKV, D, PAGES, P, S, MAXP, **dict({n: gpu(t) for n, t in arrays().items()}, **kw))
+
+
+def calls(cache, att):
+    """(name, function, its tensors) of every call that takes tensors."""
+    t = 5
+    kv = torch.zeros((t, HKV, D), dtype=BF16)
+    q = torch.zeros((t, HQ, D), dtype=BF16)
+    seqs, off = ints([0, 1]), ints([0, 3, 5])
+    return [
+        ("fork", lambda a: cache.fork(a["src"], a["dst"], stream=0), dict(src=seqs, dst=seqs + 2)),
+        ("reserve", lambda a: cache.reserve(a["seqs"], a["extra"], stream=0), dict(seqs=seqs, extra=seqs)),
+        ("append", lambda a: cache.append(0, a["k"], a["v"], a["seqs"], a["tok_off"], stream=0),
+         dict(k=kv, v=kv, seqs=seqs, tok_off=off)),
+        ("commit", lambda a: cache.commit(a["seqs"], a["path"], a["n_accept"], stream=0),
+         dict(seqs=seqs, path=ints([[0], [0]]), n_accept=seqs)),
+        ("free", lambda a: cache.free(a["seqs"], stream=0), dict(seqs=seqs)),
+        ("tree", lambda a: att(0, a["q"], a["seqs"], a["tok_off"], a["parent"], out=a["out"], stream=0),
+         dict(q=q, seqs=seqs, tok_off=off, parent=ints([-1] * t), out=torch.zeros_like(q))),
+        ("prompt", lambda a: s2.prompt_attention(a["q"], a["k"], a["v"], a["tok_off"], out=a["out"], stream=0),
+         dict(q=q, k=kv, v=kv, tok_off=off, out=torch.zeros_like(q))),
+    ]
+
+
+@pytest.mark.parametrize("which", range(7))
+def test_a_tensor_on_the_host_is_refused_before_the_library(lib, which):
+    cache = make_cache()
+    name, call, args = calls(cache, s2.TreeAttention(cache, HQ, 2, 4))[which]
+    lib.calls.clear()
+    call({n: gpu(t) for n, t in args.items()})
+    assert [c[0] for c in lib.calls] == [{"tree": "s2moe_tree_attention", "prompt": "s2moe_prompt_attention"}.get(name, "s2moe_kv_" + name)]
+    lib.calls.clear()
+    for host in args:
+        with pytest.raises(s2.S2moeError) as e:
+            call({n: t if n == host else gpu(t) for n, t in args.items()})
+        assert e.value.status == _lib.EINVAL and "cpu" in str(e.value), (name, host)
+    with pytest.raises(s2.S2moeError):
+        call(args)
+    assert not lib.calls
+
+
+def test_a_cache_on_the_host_is_refused(lib):
+    with pytest.raises(s2.S2moeError):
+        s2.KVCache(L, HKV, D, PAGES, P, S, MAXP, device="cpu")
+    for name, t in arrays().items():
+        with pytest.raises(s2.S2moeError) as e:
+            make_cache(**{name: t})
+        assert "cpu" in str(e.value)
+    assert not lib.calls
