@@ -67,6 +67,20 @@ def _same_gpu(dev, **tensors):
             raise _lib.S2moeError(_lib.EINVAL, f"{name} is on {t.device}, not on {where}")
 
 
+def _result(like, shape, stream):
+    """Memory for what `stream` writes.  From that stream's pool: the current
+    stream's may hold blocks that work queued there still uses.  The caller goes on
+    with it on the current stream, so it is not given back while work there has it."""
+    if stream is None or _lib._stream(stream) == _lib._stream(None):
+        return like.new_empty(shape)
+    if not isinstance(stream, torch.cuda.Stream):
+        stream = torch.cuda.ExternalStream(int(stream), device=like.device)
+    with torch.cuda.stream(stream):
+        out = like.new_empty(shape)
+    out.record_stream(torch.cuda.current_stream())
+    return out
+
+
 class KVCache:
     """Pages of keys and values of `n_layers` layers for up to `max_seqs`
     sequences of up to `max_pages` pages each.  Allocates the arrays that are
@@ -203,7 +217,7 @@ class TreeAttention:
         pp = _ints(parent, "parent", t)
         _same_gpu(c._gpu, q=q, seqs=seqs, tok_off=tok_off, parent=parent)
         if out is None:
-            out = q.new_empty((t, Hq, D))
+            out = _result(q, (t, Hq, D), stream)
             op, ldo = out.data_ptr(), Hq * D
         else:
             op, ldo, to = _rows(out, "out", Hq, D, c.dtype)
@@ -223,23 +237,24 @@ def prompt_attention(q, k, v, tok_off, out=None, scale: float | None = None, str
     if q.dim() != 3 or k.dim() != 3:
         raise ValueError("q, k, v: expected [n_tokens, heads, head_dim]")
     Hq, D, Hkv, dt = q.shape[1], q.shape[2], k.shape[1], q.dtype
+    code = _code(dt)
     qp, ldq, t = _rows(q, "q", Hq, D, dt)
     kp, ldk, tk = _rows(k, "k", Hkv, D, dt)
     vp, ldv, tv = _rows(v, "v", Hkv, D, dt)
-    if out is None:
-        out = q.new_empty((t, Hq, D))
-        op, ldo, to = out.data_ptr(), Hq * D, t
-    else:
-        op, ldo, to = _rows(out, "out", Hq, D, dt)
+    op, ldo, to = (None, Hq * D, t) if out is None else _rows(out, "out", Hq, D, dt)
     if not (tk == tv == to == t):
         raise ValueError(f"q, k, v, out hold {t}, {tk}, {tv}, {to} tokens")
     if tok_off.dim() != 1 or tok_off.shape[0] < 1:
         raise ValueError("tok_off: expected int32 [n + 1]")
-    a = _lib.Attn(Hq, Hkv, D, _code(dt), D ** -0.5 if scale is None else scale, ldq, ldk, ldv,
-                  ldo)
     n = tok_off.shape[0] - 1
     po = _ints(tok_off, "tok_off", n + 1)
-    _same_gpu(q.get_device(), q=q, k=k, v=v, tok_off=tok_off, out=out)
+    _same_gpu(q.get_device(), q=q, k=k, v=v, tok_off=tok_off)
+    if out is None:
+        out = _result(q, (t, Hq, D), stream)
+        op = out.data_ptr()
+    else:
+        _same_gpu(q.get_device(), out=out)
+    a = _lib.Attn(Hq, Hkv, D, code, D ** -0.5 if scale is None else scale, ldq, ldk, ldv, ldo)
     _lib._check(_lib.load().s2moe_prompt_attention(ctypes.byref(a), n, t, qp, kp, vp, po, op,
                                                    _lib._stream(stream)))
     return out

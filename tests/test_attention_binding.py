@@ -104,3 +104,50 @@ def test_a_cache_on_the_host_is_refused(lib):
             make_cache(**{name: t})
         assert "cpu" in str(e.value)
     assert not lib.calls
+
+
+class Streams:
+    """Which stream is current, and which one each tensor was allocated on and recorded on."""
+
+    def __init__(self, monkeypatch):
+        self.current, self.made, self.recorded = 11, [], []
+        monkeypatch.setattr(_lib, "_stream", lambda s: self.current if s is None else int(s))
+        monkeypatch.setattr(torch.cuda, "ExternalStream", lambda handle, device=None: handle)
+        monkeypatch.setattr(torch.cuda, "stream", self.under)
+        monkeypatch.setattr(torch.cuda, "current_stream", lambda device=None: self.current)
+        monkeypatch.setattr(OnGpu, "new_empty", self.new_empty, raising=False)
+        monkeypatch.setattr(OnGpu, "record_stream", lambda t, s: self.recorded.append(s), raising=False)
+
+    def new_empty(self, shape, **kw):
+        self.made.append(self.current)
+        return gpu(torch.zeros(shape, dtype=kw.get("dtype", BF16)))
+
+    def under(self, s):
+        import contextlib
+
+        @contextlib.contextmanager
+        def manager():
+            before, self.current = self.current, s
+            yield
+            self.current = before
+        return manager()
+
+
+@pytest.mark.parametrize("which", ["tree", "prompt"])
+def test_a_result_is_allocated_on_the_stream_that_writes_it(lib, monkeypatch, which):
+    """Memory of the current stream's may still be in use there when another stream writes it; and what
+    another stream's allocator gets back may still be in use here."""
+    streams = Streams(monkeypatch)
+    cache = make_cache()
+    att = s2.TreeAttention(cache, HQ, 2, 4)
+    q, kv = gpu(torch.zeros((5, HQ, D), dtype=BF16)), gpu(torch.zeros((5, HKV, D), dtype=BF16))
+    seqs, off, parent = (gpu(ints(x)) for x in ([0, 1], [0, 3, 5], [-1] * 5))
+    for stream, made, recorded in ((None, [11], []), (11, [11], []), (22, [22], [11])):
+        streams.made, streams.recorded = [], []
+        if which == "tree":
+            out = att(0, q, seqs, off, parent, stream=stream)
+        else:
+            out = s2.prompt_attention(q, kv, kv, off, stream=stream)
+        assert out.shape == (5, HQ, D) and streams.current == 11
+        assert streams.made == made and streams.recorded == recorded, stream
+        assert lib.calls[-1][1][-1] == (stream or 11)
