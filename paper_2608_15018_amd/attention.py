@@ -195,9 +195,8 @@ class TreeAttention:
         self.cache, self.n_heads = cache, n_heads
         self.max_seqs, self.max_nodes = max_seqs, max_nodes
         D = cache.head_dim
-        self.attn = _lib.Attn(n_heads, cache.n_kv_heads, D, cache.struct.dtype,
-                              D ** -0.5 if scale is None else scale, n_heads * D, 0, 0,
-                              n_heads * D)
+        self.scale = D ** -0.5 if scale is None else scale
+        self.attn = self._strided(n_heads * D, n_heads * D)
         self._ref = ctypes.byref(self.attn)
         self._lib = _lib.load()
         self.bytes = self._lib.s2moe_tree_attention_workspace_bytes(cache._ref, self._ref,
@@ -205,6 +204,11 @@ class TreeAttention:
         if self.bytes == 0:
             raise _lib.S2moeError(_lib.EINVAL, _lib.last_error())
         self.workspace = torch.empty(self.bytes, dtype=torch.uint8, device=cache.k.device)
+
+    def _strided(self, ldq, ldo):
+        c = self.cache
+        return _lib.Attn(self.n_heads, c.n_kv_heads, c.head_dim, c.struct.dtype, self.scale, ldq,
+                         0, 0, ldo)
 
     def __call__(self, layer: int, q, seqs, tok_off, parent, out=None, stream=None):
         """q [n_tokens, n_heads, head_dim] -> out of the same shape."""
@@ -224,9 +228,13 @@ class TreeAttention:
             if to != t:
                 raise ValueError(f"out holds {to} tokens, q {t}")
             _same_gpu(c._gpu, out=out)
-        self.attn.ldq, self.attn.ldo = ldq, ldo
+        # A struct of its own for other strides than those of whole rows: another thread
+        # may be in a call with self.attn.
+        ref = self._ref
+        if ldq != Hq * D or ldo != Hq * D:
+            ref = ctypes.byref(self._strided(ldq, ldo))
         _lib._check(self._lib.s2moe_tree_attention(
-            c._ref, layer, self._ref, n, t, self.max_nodes, qp, ps, po, pp,
+            c._ref, layer, ref, n, t, self.max_nodes, qp, ps, po, pp,
             self.workspace.data_ptr(), self.bytes, op, _lib._stream(stream)))
         return out
 

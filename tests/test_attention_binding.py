@@ -151,3 +151,23 @@ def test_a_result_is_allocated_on_the_stream_that_writes_it(lib, monkeypatch, wh
         assert out.shape == (5, HQ, D) and streams.current == 11
         assert streams.made == made and streams.recorded == recorded, stream
         assert lib.calls[-1][1][-1] == (stream or 11)
+
+
+def tree_call(cache, att, rows=HQ, **kw):
+    """A call whose q is HQ of `rows` heads of a wider array."""
+    q = gpu(torch.zeros((5, rows, D), dtype=BF16))[:, :HQ]
+    return att(0, q, *(gpu(ints(x)) for x in ([0, 1], [0, 3, 5], [-1] * 5)), **kw)
+
+
+def test_a_call_does_not_change_the_strides_of_another(lib, monkeypatch):
+    """The library reads the struct while other threads may be in the same object."""
+    Streams(monkeypatch)
+    cache = make_cache()
+    att = s2.TreeAttention(cache, HQ, 2, 4)
+    lib.calls.clear()
+    wide = gpu(torch.zeros((5, 3 * HQ, D), dtype=BF16))
+    for rows, out in ((HQ, None), (2 * HQ, None), (HQ, wide[:, HQ:2 * HQ]), (HQ, None)):
+        tree_call(cache, att, rows, out=out)
+    got = [args[2]._obj for _, args in lib.calls]
+    assert [(a.ldq, a.ldo) for a in got] == [(HQ * D, HQ * D), (2 * HQ * D, HQ * D), (HQ * D, 3 * HQ * D), (HQ * D, HQ * D)]
+    assert {(a.n_heads, a.n_kv_heads, a.head_dim, a.dtype, a.scale) for a in got} == {(HQ, HKV, D, _lib.BF16, 0.125)}
