@@ -457,7 +457,10 @@ typedef struct s2moe_attn {
    call, at most S2MOE_MAX_TOKENS (further nodes of a tree are left out), and n
    at most S2MOE_KV_MAX_REQUESTS.  workspace must hold
    s2moe_tree_attention_workspace_bytes (0 on bad arguments) for n, max_nodes
-   or more; its contents do not matter.  out must not overlap q. */
+   or more; its contents do not matter, but a call's second launch reads there
+   what its first has left: one workspace serves one call at a time, and calls
+   that may run side by side (streams, a graph's replay beside other calls,
+   threads that enqueue on one stream) need one each.  out must not overlap q. */
 size_t s2moe_tree_attention_workspace_bytes(const s2moe_kv_cache *cache, const s2moe_attn *attn,
                                             int32_t n, int32_t max_nodes);
 s2moe_status s2moe_tree_attention(const s2moe_kv_cache *cache, int32_t layer,

@@ -16,6 +16,7 @@ parent within its tree, -1 below the last kept token):
 from __future__ import annotations
 
 import ctypes
+import threading
 
 import torch
 
@@ -67,15 +68,22 @@ def _same_gpu(dev, **tensors):
             raise _lib.S2moeError(_lib.EINVAL, f"{name} is on {t.device}, not on {where}")
 
 
-def _result(like, shape, stream):
-    """Memory for what `stream` writes.  From that stream's pool: the current
+def _other(stream, device):
+    """`stream` as torch's object, or None if it is the current one."""
+    if stream is None or _lib._stream(stream) == _lib._stream(None):
+        return None
+    if isinstance(stream, torch.cuda.Stream):
+        return stream
+    return torch.cuda.ExternalStream(int(stream), device=device)
+
+
+def _result(like, shape, other):
+    """Memory for what a stream writes.  From that stream's pool: the current
     stream's may hold blocks that work queued there still uses.  The caller goes on
     with it on the current stream, so it is not given back while work there has it."""
-    if stream is None or _lib._stream(stream) == _lib._stream(None):
+    if other is None:
         return like.new_empty(shape)
-    if not isinstance(stream, torch.cuda.Stream):
-        stream = torch.cuda.ExternalStream(int(stream), device=like.device)
-    with torch.cuda.stream(stream):
+    with torch.cuda.stream(other):
         out = like.new_empty(shape)
     out.record_stream(torch.cuda.current_stream())
     return out
@@ -187,8 +195,11 @@ class KVCache:
 
 
 class TreeAttention:
-    """Attention of drafted trees over `cache`, with the workspace of calls of
-    up to `max_seqs` sequences and `max_nodes` nodes each."""
+    """Attention of drafted trees over `cache`, with the workspaces of calls of
+    up to `max_seqs` sequences and `max_nodes` nodes each: one for every stream that
+    calls come on, since the second launch of a call reads there what the first has
+    left.  A call that a graph captures has memory of that graph's own, as its replay
+    runs beside other calls.  Threads may share an object."""
 
     def __init__(self, cache: KVCache, n_heads: int, max_seqs: int, max_nodes: int,
                  scale: float | None = None):
@@ -203,7 +214,23 @@ class TreeAttention:
                                                                     max_seqs, max_nodes)
         if self.bytes == 0:
             raise _lib.S2moeError(_lib.EINVAL, _lib.last_error())
-        self.workspace = torch.empty(self.bytes, dtype=torch.uint8, device=cache.k.device)
+        self.workspace = self._new_space()
+        self._spaces = {_lib._stream(None): self.workspace}  # by stream handle
+        self._lock = threading.Lock()  # both launches of a call before another's on its stream
+
+    def _new_space(self):
+        return torch.empty(self.bytes, dtype=torch.uint8, device=self.cache.k.device)
+
+    def _space(self, handle, other):
+        if other is not None:
+            with torch.cuda.stream(other):
+                return self._space(handle, None)
+        if torch.cuda.is_current_stream_capturing():
+            return self._new_space()
+        space = self._spaces.get(handle)
+        if space is None:
+            space = self._spaces[handle] = self._new_space()
+        return space
 
     def _strided(self, ldq, ldo):
         c = self.cache
@@ -220,8 +247,9 @@ class TreeAttention:
         ps, po = _ints(seqs, "seqs", n), _ints(tok_off, "tok_off", n + 1)
         pp = _ints(parent, "parent", t)
         _same_gpu(c._gpu, q=q, seqs=seqs, tok_off=tok_off, parent=parent)
+        other = _other(stream, q.device)
         if out is None:
-            out = _result(q, (t, Hq, D), stream)
+            out = _result(q, (t, Hq, D), other)
             op, ldo = out.data_ptr(), Hq * D
         else:
             op, ldo, to = _rows(out, "out", Hq, D, c.dtype)
@@ -233,9 +261,12 @@ class TreeAttention:
         ref = self._ref
         if ldq != Hq * D or ldo != Hq * D:
             ref = ctypes.byref(self._strided(ldq, ldo))
-        _lib._check(self._lib.s2moe_tree_attention(
-            c._ref, layer, ref, n, t, self.max_nodes, qp, ps, po, pp,
-            self.workspace.data_ptr(), self.bytes, op, _lib._stream(stream)))
+        handle = _lib._stream(stream)
+        with self._lock:
+            space = self._space(handle, other)
+            _lib._check(self._lib.s2moe_tree_attention(
+                c._ref, layer, ref, n, t, self.max_nodes, qp, ps, po, pp, space.data_ptr(),
+                self.bytes, op, handle))
         return out
 
 
@@ -258,7 +289,7 @@ def prompt_attention(q, k, v, tok_off, out=None, scale: float | None = None, str
     po = _ints(tok_off, "tok_off", n + 1)
     _same_gpu(q.get_device(), q=q, k=k, v=v, tok_off=tok_off)
     if out is None:
-        out = _result(q, (t, Hq, D), stream)
+        out = _result(q, (t, Hq, D), _other(stream, q.device))
         op = out.data_ptr()
     else:
         _same_gpu(q.get_device(), out=out)

@@ -42,6 +42,8 @@ class Recorder:
 def lib(monkeypatch):
     r = Recorder()
     monkeypatch.setattr(_lib, "load", lambda: r)
+    monkeypatch.setattr(_lib, "_stream", lambda s: 11 if s is None else int(s))
+    monkeypatch.setattr(torch.cuda, "is_current_stream_capturing", lambda: False)
     return r
 
 
@@ -65,16 +67,16 @@ def calls(cache, att):
     q = torch.zeros((t, HQ, D), dtype=BF16)
     seqs, off = ints([0, 1]), ints([0, 3, 5])
     return [
-        ("fork", lambda a: cache.fork(a["src"], a["dst"], stream=0), dict(src=seqs, dst=seqs + 2)),
-        ("reserve", lambda a: cache.reserve(a["seqs"], a["extra"], stream=0), dict(seqs=seqs, extra=seqs)),
-        ("append", lambda a: cache.append(0, a["k"], a["v"], a["seqs"], a["tok_off"], stream=0),
+        ("fork", lambda a: cache.fork(a["src"], a["dst"], stream=11), dict(src=seqs, dst=seqs + 2)),
+        ("reserve", lambda a: cache.reserve(a["seqs"], a["extra"], stream=11), dict(seqs=seqs, extra=seqs)),
+        ("append", lambda a: cache.append(0, a["k"], a["v"], a["seqs"], a["tok_off"], stream=11),
          dict(k=kv, v=kv, seqs=seqs, tok_off=off)),
-        ("commit", lambda a: cache.commit(a["seqs"], a["path"], a["n_accept"], stream=0),
+        ("commit", lambda a: cache.commit(a["seqs"], a["path"], a["n_accept"], stream=11),
          dict(seqs=seqs, path=ints([[0], [0]]), n_accept=seqs)),
-        ("free", lambda a: cache.free(a["seqs"], stream=0), dict(seqs=seqs)),
-        ("tree", lambda a: att(0, a["q"], a["seqs"], a["tok_off"], a["parent"], out=a["out"], stream=0),
+        ("free", lambda a: cache.free(a["seqs"], stream=11), dict(seqs=seqs)),
+        ("tree", lambda a: att(0, a["q"], a["seqs"], a["tok_off"], a["parent"], out=a["out"], stream=11),
          dict(q=q, seqs=seqs, tok_off=off, parent=ints([-1] * t), out=torch.zeros_like(q))),
-        ("prompt", lambda a: s2.prompt_attention(a["q"], a["k"], a["v"], a["tok_off"], out=a["out"], stream=0),
+        ("prompt", lambda a: s2.prompt_attention(a["q"], a["k"], a["v"], a["tok_off"], out=a["out"], stream=11),
          dict(q=q, k=kv, v=kv, tok_off=off, out=torch.zeros_like(q))),
     ]
 
@@ -171,3 +173,68 @@ def test_a_call_does_not_change_the_strides_of_another(lib, monkeypatch):
     got = [args[2]._obj for _, args in lib.calls]
     assert [(a.ldq, a.ldo) for a in got] == [(HQ * D, HQ * D), (2 * HQ * D, HQ * D), (HQ * D, 3 * HQ * D), (HQ * D, HQ * D)]
     assert {(a.n_heads, a.n_kv_heads, a.head_dim, a.dtype, a.scale) for a in got} == {(HQ, HKV, D, _lib.BF16, 0.125)}
+
+
+def test_calls_on_different_streams_have_workspaces_of_their_own(lib, monkeypatch):
+    """The second launch of a call reads there what the first has left."""
+    streams = Streams(monkeypatch)
+    cache = make_cache()
+    att = s2.TreeAttention(cache, HQ, 2, 4)
+    capturing = []
+    monkeypatch.setattr(torch.cuda, "is_current_stream_capturing", lambda: streams.current in capturing)
+    space = lambda **kw: (lib.calls.clear(), tree_call(cache, att, **kw), lib.calls[-1][1][10])[2]  # noqa: E731
+    here, there = space(), space(stream=22)
+    assert here == att.workspace.data_ptr() and there != here
+    assert [space(), space(stream=22), space(stream=11), space(stream=33)][:3] == [here, there, here]
+    assert space(stream=33) not in (here, there)
+    with torch.cuda.stream(22):
+        assert [space(), space(stream=11)] == [there, here]
+    # A graph is replayed beside other calls, so it has memory of its own.
+    capturing[:] = [11, 22]
+    assert space() not in (here, there) and space(stream=22) not in (here, there)
+    capturing.clear()
+    assert [space(), space(stream=22)] == [here, there]
+
+
+def run_threads(*functions):
+    import threading
+
+    threads = [threading.Thread(target=f) for f in functions]
+    for t in threads:
+        t.start()
+    for t in threads:
+        t.join()
+
+
+class Slow(Recorder):
+    """Calls take a while, and note when two are under way at once."""
+
+    def __init__(self, names):
+        super().__init__()
+        self.names, self.inside, self.met = names, 0, []
+
+    def __getattr__(self, name):
+        import time
+
+        call = super().__getattr__(name)
+        if name not in self.names:
+            return call
+
+        def slow(*args):
+            self.inside += 1
+            if self.inside > 1:
+                self.met.append(name)
+            time.sleep(0.02)
+            self.inside -= 1
+            return call(*args)
+        return slow
+
+
+def test_the_launches_of_two_threads_calls_do_not_mix(lib, monkeypatch):
+    Streams(monkeypatch)
+    slow = Slow(["s2moe_tree_attention"])
+    monkeypatch.setattr(_lib, "load", lambda: slow)
+    cache = make_cache()
+    att = s2.TreeAttention(cache, HQ, 2, 4)
+    run_threads(*[lambda: [tree_call(cache, att) for _ in range(3)]] * 3)
+    assert len([c for c in slow.calls if c[0] == "s2moe_tree_attention"]) == 9 and not slow.met

@@ -71,3 +71,44 @@ def test_the_default_stream_by_its_handle():
         out = att(*args, stream=0)
     torch.cuda.synchronize()
     assert torch.equal(out, want)
+
+
+def test_calls_on_two_streams_at_once():
+    """One object, its calls interleaved on two streams: each keeps its parts in a workspace of its own."""
+    cache, att, args, want, _ = run_tree("bf16", (32, 8, 128), 64, [9000, 4000], [16, 9])
+    layer, q, seqs, off, par = args
+    swapped = (layer, torch.cat([q[16:], q[:16]]), ints([1, 0]), ints([0, 9, 25]), torch.cat([par[16:], par[:16]]))
+    first = att(*swapped)
+    a, b = torch.cuda.Stream(), torch.cuda.Stream()
+    torch.cuda.synchronize()
+    out = [(torch.empty_like(want), torch.empty_like(first)) for _ in range(30)]
+    for x, y in out:
+        att(*args, out=x, stream=a)
+        att(*swapped, out=y, stream=b)
+    torch.cuda.synchronize()
+    for x, y in out:
+        assert torch.equal(x, want) and torch.equal(y, first)
+
+
+def test_a_replay_beside_eager_calls():
+    cache, att, args, want, _ = run_tree("bf16", (32, 8, 128), 64, [9000, 4000], [16, 9])
+    layer, q, seqs, off, par = args
+    swapped = (layer, torch.cat([q[16:], q[:16]]), ints([1, 0]), ints([0, 9, 25]), torch.cat([par[16:], par[:16]]))
+    first = att(*swapped)
+    dst, s = torch.empty_like(want), torch.cuda.Stream()
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph, stream=s):
+        att(*args, out=dst)
+    for _ in range(20):
+        dst.zero_()
+        torch.cuda.synchronize()
+        with torch.cuda.stream(s):
+            graph.replay()
+        got = [att(*swapped) for _ in range(3)]
+        torch.cuda.synchronize()
+        assert torch.equal(dst, want) and all(torch.equal(g, first) for g in got)
+    with torch.cuda.stream(s):
+        again = att(*args)
+    torch.cuda.synchronize()
+    assert torch.equal(again, want)
