@@ -97,7 +97,9 @@ class KVCache:
 
     `status` holds one word per request of the last page operation (bits KV_*,
     0: done) and `copied` the pages that the last reserve copied, both on the
-    device."""
+    device; every operation writes them.  Threads may share a cache; operations on
+    different streams, which all read and write its table, lengths and counts, are the
+    caller's to order."""
 
     def __init__(self, n_layers: int, n_kv_heads: int, head_dim: int, n_pages: int,
                  page_size: int, max_seqs: int, max_pages: int, dtype=torch.bfloat16,
@@ -131,21 +133,24 @@ class KVCache:
                                            for n in ("k", "v", "table", "length", "refs")])
         self._ref = ctypes.byref(self.struct)
         self._lib = _lib.load()
+        self._lock = threading.Lock()  # the launches of an operation before another's
         self._status, self._copied = self.status.data_ptr(), self.copied.data_ptr()
         if fresh:
             self.clear()
 
     def clear(self, stream=None):
         """Every sequence empty, every page free."""
-        _lib._check(self._lib.s2moe_kv_init(self._ref, _lib._stream(stream)))
+        with self._lock:
+            _lib._check(self._lib.s2moe_kv_init(self._ref, _lib._stream(stream)))
 
     def fork(self, src, dst, stream=None):
         """Sequence dst[i] becomes a copy of src[i] on the same pages."""
         n = src.shape[0]
         ps, pd = _ints(src, "src", n), _ints(dst, "dst", n)
         _same_gpu(self._gpu, src=src, dst=dst)
-        _lib._check(self._lib.s2moe_kv_fork(self._ref, n, ps, pd, self._status,
-                                            _lib._stream(stream)))
+        with self._lock:
+            _lib._check(self._lib.s2moe_kv_fork(self._ref, n, ps, pd, self._status,
+                                                _lib._stream(stream)))
 
     def reserve(self, seqs, extra, stream=None):
         """Pages for extra[i] more tokens of seqs[i]; a shared page that they
@@ -153,8 +158,9 @@ class KVCache:
         n = seqs.shape[0]
         ps, pe = _ints(seqs, "seqs", n), _ints(extra, "extra", n)
         _same_gpu(self._gpu, seqs=seqs, extra=extra)
-        _lib._check(self._lib.s2moe_kv_reserve(self._ref, n, ps, pe, self._copied,
-                                               self._status, _lib._stream(stream)))
+        with self._lock:
+            _lib._check(self._lib.s2moe_kv_reserve(self._ref, n, ps, pe, self._copied,
+                                                   self._status, _lib._stream(stream)))
 
     def append(self, layer: int, k, v, seqs, tok_off, stream=None):
         """New tokens' keys and values [n_tokens, n_kv_heads, head_dim] into
@@ -182,16 +188,18 @@ class KVCache:
         _same_gpu(self._gpu, seqs=seqs, n_accept=n_accept)
         if path is not None:
             _same_gpu(self._gpu, path=path)
-        _lib._check(self._lib.s2moe_kv_commit(self._ref, n, most, ps, pp, pa, self._status,
-                                              _lib._stream(stream)))
+        with self._lock:
+            _lib._check(self._lib.s2moe_kv_commit(self._ref, n, most, ps, pp, pa, self._status,
+                                                  _lib._stream(stream)))
 
     def free(self, seqs, stream=None):
         """Empties the sequences."""
         n = seqs.shape[0]
         ps = _ints(seqs, "seqs", n)
         _same_gpu(self._gpu, seqs=seqs)
-        _lib._check(self._lib.s2moe_kv_free(self._ref, n, ps, self._status,
-                                            _lib._stream(stream)))
+        with self._lock:
+            _lib._check(self._lib.s2moe_kv_free(self._ref, n, ps, self._status,
+                                                _lib._stream(stream)))
 
 
 class TreeAttention:

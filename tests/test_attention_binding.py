@@ -238,3 +238,17 @@ def test_the_launches_of_two_threads_calls_do_not_mix(lib, monkeypatch):
     att = s2.TreeAttention(cache, HQ, 2, 4)
     run_threads(*[lambda: [tree_call(cache, att) for _ in range(3)]] * 3)
     assert len([c for c in slow.calls if c[0] == "s2moe_tree_attention"]) == 9 and not slow.met
+
+
+PAGE_CALLS = ["s2moe_kv_init", "s2moe_kv_fork", "s2moe_kv_reserve", "s2moe_kv_commit", "s2moe_kv_free"]
+
+
+def test_the_launches_of_two_threads_page_operations_do_not_mix(lib, monkeypatch):
+    """reserve's second launch reads `copied`, commit's what the first has checked."""
+    slow = Slow(PAGE_CALLS)
+    monkeypatch.setattr(_lib, "load", lambda: slow)
+    cache = make_cache()
+    seqs = gpu(ints([0, 1]))
+    run_threads(cache.clear, lambda: cache.fork(seqs, seqs), lambda: cache.reserve(seqs, seqs), lambda: cache.reserve(seqs, seqs),
+                lambda: cache.commit(seqs, None, seqs), lambda: cache.free(seqs))
+    assert sorted(c[0] for c in slow.calls) == sorted(PAGE_CALLS + ["s2moe_kv_reserve"]) and not slow.met
