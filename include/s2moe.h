@@ -450,8 +450,11 @@ typedef struct s2moe_attn {
      out_{i,h} = sum_{j in C u A(i)} softmax_j(scale q_{i,h} . k_{j,g}) v_{j,g}
    with g the kv head of h.  A node whose parent is neither -1 nor an earlier
    node, and every node below it, gets zeros.  What masked slots hold does not
-   matter, infinities and NaN included.  Sums and softmax statistics are fp32;
-   the softmax numerators of BF16 caches enter the second product as bf16.
+   matter, infinities and NaN included.  An infinite value that a row sees makes
+   that coordinate of the row infinite, infinities of both signs or a NaN make it
+   NaN (and so may an infinity whose weight has underflowed to zero), wherever
+   the token lies.  Sums and softmax statistics are fp32; the softmax numerators
+   of BF16 caches enter the second product as bf16.
    q [n_tokens][n_heads][D], parent [n_tokens] int32, seqs [n], tok_off
    [n + 1], out [n_tokens][n_heads][D]; max_nodes is the largest tree of the
    call, at most S2MOE_MAX_TOKENS (further nodes of a tree are left out), and n
@@ -474,8 +477,8 @@ s2moe_status s2moe_tree_attention(const s2moe_kv_cache *cache, int32_t layer,
    rows tok_off[t] .. tok_off[t + 1] - 1 of q, k, v and out are prompt t, and
    row i sees the rows of its prompt up to itself.  k, v [n_tokens][n_kv_heads]
    [D].  tok_off [n + 1] int32, ascending from 0 to n_tokens; rows outside
-   it are not written.  n <= S2MOE_KV_MAX_REQUESTS.  out must not overlap q, k
-   or v. */
+   it are not written.  Infinities, NaN and precision as in s2moe_tree_attention.
+   n <= S2MOE_KV_MAX_REQUESTS.  out must not overlap q, k or v. */
 s2moe_status s2moe_prompt_attention(const s2moe_attn *attn, int32_t n, int32_t n_tokens,
                                     const void *q, const void *k, const void *v,
                                     const int32_t *tok_off, void *out, void *stream);

@@ -116,17 +116,48 @@ __device__ __forceinline__ f32x4 finite_only(f32x4 x) {
     if ((__float_as_uint(x[i]) & 0x7F800000u) == 0x7F800000u) x[i] = 0.f;
   return x;
 }
-// 1 for each of those elements, 0 for the others.
-__device__ __forceinline__ bf16x8 nonfinite_ones(bf16x8 x) {
+// What a product with such elements gives, where some weights are zero because a row
+// does not see the key: each element as a number (infinity 1, minus infinity 2^8, NaN
+// 2^16, finite 0), times 1 for a key that the row sees, 2^16 if its weight has
+// underflowed to zero, 0 for one that it does not see.  Up to 32 keys add up, in any
+// order, to a number that tells what there was.
+constexpr float kNan = 65536.f;
+__device__ __forceinline__ bf16x8 special_numbers(bf16x8 x) {
   u32x4 u = __builtin_bit_cast(u32x4, x);
 #pragma unroll
-  for (int i = 0; i < 4; ++i) u[i] = (nonfinite_bits(u[i]) >> 15) * 0x3F80u;
+  for (int i = 0; i < 4; ++i) {
+    const uint32_t t = nonfinite_bits(u[i]) >> 15;  // a bit for each half
+    const uint32_t nan = t & (((u[i] & 0x007F007Fu) + 0x007F007Fu) >> 7), minus = t & (u[i] >> 15) & ~nan;
+    u[i] = t * 0x3F80u + minus * (0x4380u - 0x3F80u) + nan * (0x4780u - 0x3F80u);
+  }
   return __builtin_bit_cast(bf16x8, u);
 }
-__device__ __forceinline__ f32x4 nonfinite_ones(f32x4 x) {
+__device__ __forceinline__ f32x4 special_numbers(f32x4 x) {
 #pragma unroll
-  for (int i = 0; i < 4; ++i) x[i] = (__float_as_uint(x[i]) & 0x7F800000u) == 0x7F800000u ? 1.f : 0.f;
+  for (int i = 0; i < 4; ++i)
+    x[i] = x[i] != x[i] ? kNan : x[i] == INFINITY ? 1.f : x[i] == -INFINITY ? 256.f : 0.f;
   return x;
+}
+// What the weights become there: bit e of `seen` is element e's key.
+__device__ __forceinline__ bf16x8 sight(uint32_t seen, bf16x8 weights) {
+  u32x4 u = __builtin_bit_cast(u32x4, weights);
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    const uint32_t weighs = (((u[i] & 0x7FFF7FFFu) + 0x7FFF7FFFu) >> 15) & 0x00010001u;
+    const uint32_t two = (seen >> (2 * i) & 1) | (seen >> (2 * i + 1) & 1) << 16;
+    u[i] = (0x47804780u - weighs * (0x4780u - 0x3F80u)) & (two * 0xFFFFu);
+  }
+  return __builtin_bit_cast(bf16x8, u);
+}
+__device__ __forceinline__ f32x4 sight(uint32_t seen, f32x4 weights) {
+#pragma unroll
+  for (int i = 0; i < 4; ++i) weights[i] = !(seen >> i & 1) ? 0.f : weights[i] == 0.f ? kNan : 1.f;
+  return weights;
+}
+__device__ __forceinline__ float special_sum(float number) {
+  const int n = number >= kNan ? 0x101 : (int)number;
+  const float plus = (n & 255) != 0 ? INFINITY : 0.f, minus = n >> 8 != 0 ? -INFINITY : 0.f;
+  return plus + minus;  // NaN where both are there
 }
 
 }  // namespace s2moe

@@ -291,7 +291,7 @@ __global__ __launch_bounds__(256, (PromptTile<D, NT>::kPerCu)) void prompt_bf16_
   };
   // The second product of step j.  Where some rows do not see some keys a weight of
   // zero does not hide an infinity or NaN, so those values count as zero there, and
-  // where a weight meets one the row's sum becomes NaN.
+  // rows that see them get what they add up to.
   const auto products_v_checked = [&](int j, bool masked, const bf16x8(&W)[2][NT]) {
     bf16x8 vf[2][MT];
 #pragma unroll
@@ -309,12 +309,16 @@ __global__ __launch_bounds__(256, (PromptTile<D, NT>::kPerCu)) void prompt_bf16_
         for (int mt = 0; mt < MT; ++mt) {
 #pragma unroll
           for (int nt = 0; nt < NT; ++nt) {
+            __builtin_amdgcn_sched_barrier(0);  // one after the other: registers
             f32x16 met = {};
 #pragma unroll
-            for (int ks = 0; ks < 2; ++ks)
-              met = __builtin_amdgcn_mfma_f32_32x32x16_bf16(nonfinite_ones(vf[ks][mt]), W[ks][nt], met, 0, 0, 0);
+            for (int ks = 0; ks < 2; ++ks) {
+              const int n = tok[nt] + 1 - (32 * j + 16 * ks + 8 * h);  // of the eight keys
+              const bf16x8 sees = sight(n < 0 ? 0 : (1u << min(n, 8)) - 1, W[ks][nt]);
+              met = __builtin_amdgcn_mfma_f32_32x32x16_bf16(special_numbers(vf[ks][mt]), sees, met, 0, 0, 0);
+            }
 #pragma unroll
-            for (int i = 0; i < 16; ++i) O[mt][nt][i] = met[i] != 0.f ? NAN : O[mt][nt][i];
+            for (int i = 0; i < 16; ++i) O[mt][nt][i] += special_sum(met[i]);
           }
 #pragma unroll
           for (int ks = 0; ks < 2; ++ks) vf[ks][mt] = finite_only(vf[ks][mt]);
@@ -584,9 +588,11 @@ __global__ __launch_bounds__(256, 2) void prompt_f32_kernel(PromptArgs a) {
         for (int mt = 0; mt < MT; ++mt) {
 #pragma unroll
           for (int nt = 0; nt < 2; ++nt) {
-            const f32x4 met = mma(nonfinite_ones(V[mt]), P[nt], f32x4{});
+            __builtin_amdgcn_sched_barrier(0);  // one after the other: registers
+            const int n = tok[nt] + 1 - (16 * t + 4 * g);  // of the four keys
+            const f32x4 met = mma(special_numbers(V[mt]), sight(n < 0 ? 0 : (1u << min(n, 4)) - 1, P[nt]), f32x4{});
 #pragma unroll
-            for (int e = 0; e < 4; ++e) O[mt][nt][e] = met[e] != 0.f ? NAN : O[mt][nt][e];
+            for (int e = 0; e < 4; ++e) O[mt][nt][e] += special_sum(met[e]);
           }
           V[mt] = finite_only(V[mt]);
         }

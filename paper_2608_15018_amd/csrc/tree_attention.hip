@@ -276,25 +276,32 @@ __device__ __forceinline__ void raise(const float (&m)[NT], float (&shift)[NT], 
 }
 
 // Where some rows do not see some keys: a weight of zero does not hide an infinity
-// or NaN, so those values count as zero, and where a weight meets one the row's sum
-// becomes NaN.
+// or NaN, so those values count as zero, and rows that see them get what they add up
+// to.  Keys as in mask_scores.
 template <int MT, int NT, int VC, typename frag>
-__device__ __forceinline__ void hide_nonfinite(frag (&V)[MT][VC], const frag (&P)[NT][VC], f32x4 (&O)[MT][NT]) {
+__device__ __forceinline__ void hide_nonfinite(frag (&V)[MT][VC], const frag (&P)[NT][VC], f32x4 (&O)[MT][NT],
+                                               const int (&tok)[NT], const uint32_t* mask_s, int key, int len, int total) {
   uint32_t bad = 0;
 #pragma unroll
   for (int mt = 0; mt < MT; ++mt)
 #pragma unroll
     for (int y = 0; y < VC; ++y) bad |= any_nonfinite(V[mt][y]);
-  if (!__any(bad != 0)) return;
+  if (__builtin_expect(!__any(bad != 0), 1)) return;
+  uint32_t seen[NT];
+#pragma unroll
+  for (int nt = 0; nt < NT; ++nt)
+    seen[nt] = seen8(mask_s + tok[nt] * kMaskRow, key - len) & ((1u << min(max(total - key, 0), 8)) - 1);
 #pragma unroll
   for (int mt = 0; mt < MT; ++mt) {
 #pragma unroll
     for (int nt = 0; nt < NT; ++nt) {
+      __builtin_amdgcn_sched_barrier(0);  // one after the other: registers
       f32x4 met = {};
 #pragma unroll
-      for (int y = 0; y < VC; ++y) met = mma(nonfinite_ones(V[mt][y]), P[nt][y], met);
+      for (int y = 0; y < VC; ++y)
+        met = mma(special_numbers(V[mt][y]), sight(seen[nt] >> (8 / VC * y), P[nt][y]), met);
 #pragma unroll
-      for (int e = 0; e < 4; ++e) O[mt][nt][e] = met[e] != 0.f ? NAN : O[mt][nt][e];
+      for (int e = 0; e < 4; ++e) O[mt][nt][e] += special_sum(met[e]);
     }
 #pragma unroll
     for (int y = 0; y < VC; ++y) V[mt][y] = finite_only(V[mt][y]);
@@ -466,7 +473,7 @@ __global__ __launch_bounds__(256, (KeysPlan<E, D, NT>::kPerCu)) void tree_keys_k
           P[nt][0] = pack8(p[nt]);
         }
       }
-      if (masked) hide_nonfinite<MT, NT, VC>(V, P, O);
+      if (masked) hide_nonfinite<MT, NT, VC>(V, P, O, tok, mask_s, key0 + 8 * g, r.len, r.total);
 #pragma unroll
       for (int mt = 0; mt < MT; ++mt)
 #pragma unroll
@@ -692,7 +699,8 @@ __device__ __forceinline__ void rows_stretch(const TreeArgs& a, const Stretch& r
           }
         if (masked)
 #pragma unroll
-          for (int z = 0; z < NS; ++z) hide_nonfinite<MT, NA, 1>(V[z], P[z], O);
+          for (int z = 0; z < NS; ++z)
+            hide_nonfinite<MT, NA, 1>(V[z], P[z], O, tok, st.mask_s, key0 + 32 * z + 8 * g, r.len, r.total);
 #pragma unroll
         for (int z = 0; z < NS; ++z)
 #pragma unroll
