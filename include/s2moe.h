@@ -453,8 +453,9 @@ typedef struct s2moe_attn {
    matter, infinities and NaN included.  An infinite value that a row sees makes
    that coordinate of the row infinite, infinities of both signs or a NaN make it
    NaN (and so may an infinity whose weight has underflowed to zero), wherever
-   the token lies.  Sums and softmax statistics are fp32; the softmax numerators
-   of BF16 caches enter the second product as bf16.
+   the token lies.  A row whose scores are all minus infinity gets zeros (if no
+   value is infinite or NaN).  Sums and softmax statistics are fp32; the softmax
+   numerators of BF16 caches enter the second product as bf16.
    q [n_tokens][n_heads][D], parent [n_tokens] int32, seqs [n], tok_off
    [n + 1], out [n_tokens][n_heads][D]; max_nodes is the largest tree of the
    call, at most S2MOE_MAX_TOKENS (further nodes of a tree are left out), and n

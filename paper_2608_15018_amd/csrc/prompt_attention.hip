@@ -457,7 +457,8 @@ __global__ __launch_bounds__(256, (PromptTile<D, NT>::kPerCu)) void prompt_bf16_
 #pragma unroll
   for (int nt = 0; nt < NT; ++nt) {
     const int r = row0 + 32 * nt + l32;
-    const float inv = 1.f / sum_halves(l[nt]);
+    const float sum = sum_halves(l[nt]);
+    const float inv = sum == 0.f ? 0.f : 1.f / sum;  // 0: every score is minus infinity
     // A lane has four elements of every eight; the half-waves exchange fours, so
     // that each stores 16 bytes.
     uint16_t* p = out + (int64_t)(first + tok[nt]) * a.ldo + (hk * a.G + r - tok[nt] * a.G) * D + 8 * h;
@@ -641,7 +642,8 @@ __global__ __launch_bounds__(256, 2) void prompt_f32_kernel(PromptArgs a) {
 #pragma unroll
   for (int nt = 0; nt < 2; ++nt) {
     const int row = row0 + 16 * nt + n16;
-    const float inv = 1.f / (SPLIT ? l[nt] : sum_groups(l[nt]));
+    const float sum = SPLIT ? l[nt] : sum_groups(l[nt]);
+    const float inv = sum == 0.f ? 0.f : 1.f / sum;  // as in the bf16 kernel
     if (row >= R) continue;
     float* p = reinterpret_cast<float*>(a.out) + (int64_t)(first + tok[nt]) * a.ldo +
                (hk * a.G + row - tok[nt] * a.G) * D + 4 * g;

@@ -9,7 +9,7 @@ import numpy as np
 import pytest
 
 from oracle import attention_oracle as ao
-from tests.test_gpu_attention import DT, ints, random_parents, run_prompt, run_tree
+from tests.test_gpu_attention import DT, check, ints, random_parents, run_prompt, run_tree
 
 pytestmark = pytest.mark.gpu
 
@@ -101,3 +101,37 @@ def test_an_infinity_of_no_weight_is_treated_alike(dtype):
     assert out[100:, :, 9].isnan().all() and out[:100].isfinite().all()
     out[100:, :, 9] = 0
     assert out.isfinite().all()
+
+
+# Forms of the prompt kernels: few rows and short, many rows and short, many rows and long.
+FORMS = [((4, 2, 64), [60, 131, 30]), ((4, 2, 128), [60, 131, 30]), ((32, 8, 64), [40] * 60), ((32, 8, 128), [40] * 60),
+         ((64, 32, 64), [1187, 1290]), ((64, 32, 128), [1187, 1290])]
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("heads,lens", FORMS)
+def test_prompt_rows_of_scores_of_minus_infinity(dtype, heads, lens):
+    """Keys that weigh nothing: the rows that see no other get zeros, the later ones what the others give."""
+    q, k, v, off, _ = run_prompt(dtype, heads, lens, seed=8, wide=False)
+    first, n, hidden = lens[0], lens[1], 37
+    q[:, :, 0] = q[:, :, 0].abs() + 0.25
+    k2 = k.clone()
+    k2[first:first + hidden, :, 0] = -INF
+    out = s2.prompt_attention(q, k2, v, off)
+    assert not out[first:first + hidden].any()
+    cut = ints([0, n - hidden])
+    part = [t[first + hidden:first + n].contiguous() for t in (q, k, v)]
+    want = ao.prompt_attention(*(t.double().cpu().numpy() for t in part), cut.tolist(), heads[2] ** -0.5)
+    check(out[first + hidden:first + n], want, dtype)
+    assert torch.equal(out[:first], s2.prompt_attention(q, k, v, off)[:first])
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("heads,T", [((2, 1, 64), 7), ((2, 1, 128), 7), ((4, 2, 64), 40), ((4, 2, 128), 40)])
+def test_tree_rows_of_scores_of_minus_infinity(dtype, heads, T):
+    cache, att, args, _, _ = run_tree(dtype, heads, 16, [300], [T], seed=9)
+    layer, q, *rest = args
+    q = q.clone()
+    q[:, :, 0] = q[:, :, 0].abs() + 0.25
+    cache.k[0, :, :, :, 0] = -INF
+    assert not att(layer, q, *rest).any()
