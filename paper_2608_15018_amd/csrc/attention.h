@@ -4,6 +4,8 @@
 #include <hip/hip_runtime.h>
 #include <stdint.h>
 
+#include <atomic>
+
 namespace s2moe {
 
 constexpr int kKvMaxRequests = 1024;  // S2MOE_KV_MAX_REQUESTS
@@ -27,6 +29,19 @@ struct KvCache {
   __host__ __device__ int64_t page_bytes() const { return head_bytes() * Hkv; }
   __host__ __device__ int64_t layer_bytes() const { return page_bytes() * n_pages; }
 };
+
+// Lets `kernel` have up to `bytes` of dynamic LDS on the current device; `done`, the
+// kernel's own, has a bit for each device where that has been asked for.
+inline hipError_t allow_lds(const void* kernel, size_t bytes, std::atomic<uint64_t>& done) {
+  int dev = 0;
+  hipError_t e = hipGetDevice(&dev);
+  if (e != hipSuccess) return e;
+  const uint64_t bit = dev >= 0 && dev < 64 ? 1ull << dev : 0;
+  if (done.load(std::memory_order_relaxed) & bit) return hipSuccess;
+  e = hipFuncSetAttribute(kernel, hipFuncAttributeMaxDynamicSharedMemorySize, (int)bytes);
+  if (e == hipSuccess) done.fetch_or(bit, std::memory_order_relaxed);
+  return e;
+}
 
 hipError_t launch_kv_init(const KvCache& c, hipStream_t s);
 hipError_t launch_kv_fork(const KvCache& c, int n, const int32_t* src, const int32_t* dst,

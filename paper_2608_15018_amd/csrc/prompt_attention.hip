@@ -655,10 +655,9 @@ __global__ __launch_bounds__(256, 2) void prompt_f32_kernel(PromptArgs a) {
 template <int D, int NT>
 hipError_t launch_bf16(const PromptArgs& a, hipStream_t s) {
   typedef PromptTile<D, NT> Tile;
-  static const hipError_t ready =
-      hipFuncSetAttribute(reinterpret_cast<const void*>(prompt_bf16_kernel<D, NT>),
-                          hipFuncAttributeMaxDynamicSharedMemorySize, Tile::kLds);
-  if (ready != hipSuccess) return ready;
+  static std::atomic<uint64_t> ready{0};
+  const hipError_t err = allow_lds(reinterpret_cast<const void*>(prompt_bf16_kernel<D, NT>), Tile::kLds, ready);
+  if (err != hipSuccess) return err;
   // At most one unfilled workgroup per prompt.
   const int64_t blocks = ((int64_t)a.n_tokens * a.G / Tile::kRows + a.n) * a.Hkv;
   prompt_bf16_kernel<D, NT><<<(unsigned)blocks, 256, Tile::kLds, s>>>(a);

@@ -900,10 +900,10 @@ struct ByKeys {
   typedef KeysPlan<E, D_, NT> Plan;
   static constexpr int D = D_;
   static hipError_t launch(const TreeArgs& a, hipStream_t s) {
-    static const hipError_t ready = hipFuncSetAttribute(
-        reinterpret_cast<const void*>(tree_keys_kernel<E, D, NT>),
-        hipFuncAttributeMaxDynamicSharedMemorySize, (int)Plan::lds(kKvMaxRequests, kMaxNodes));
-    if (ready != hipSuccess) return ready;
+    static std::atomic<uint64_t> ready{0};
+    const hipError_t err =
+        allow_lds(reinterpret_cast<const void*>(tree_keys_kernel<E, D, NT>), Plan::lds(kKvMaxRequests, kMaxNodes), ready);
+    if (err != hipSuccess) return err;
     tree_keys_kernel<E, D, NT><<<Plan::kGroups, 256, Plan::lds(a.n, a.max_nodes), s>>>(a);
     return launch_join<E, D, Plan>(a, s);
   }
@@ -914,10 +914,10 @@ struct ByRows {
   typedef RowsPlan<D_, NT> Plan;
   static constexpr int D = D_;
   static hipError_t launch(const TreeArgs& a, hipStream_t s) {
-    static const hipError_t ready = hipFuncSetAttribute(
-        reinterpret_cast<const void*>(tree_rows_kernel<D, NT>),
-        hipFuncAttributeMaxDynamicSharedMemorySize, (int)Plan::lds(kKvMaxRequests, kMaxNodes));
-    if (ready != hipSuccess) return ready;
+    static std::atomic<uint64_t> ready{0};
+    const hipError_t err =
+        allow_lds(reinterpret_cast<const void*>(tree_rows_kernel<D, NT>), Plan::lds(kKvMaxRequests, kMaxNodes), ready);
+    if (err != hipSuccess) return err;
     tree_rows_kernel<D, NT><<<Plan::kGroups, 256, Plan::lds(a.n, a.max_nodes), s>>>(a);
     return launch_join<uint16_t, D, Plan>(a, s);
   }
