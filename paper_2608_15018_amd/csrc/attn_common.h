@@ -69,7 +69,7 @@ __device__ __forceinline__ void load_to_lds(const char* base, uint32_t off, cons
   asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %2"
                :
                : "s"(at), "v"(off), "s"(base)
-               : "memory");
+               : "memory", "m0");
 }
 template <int N>
 __device__ __forceinline__ void wait_loads() {  // until at most N are in flight
