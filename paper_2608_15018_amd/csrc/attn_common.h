@@ -63,7 +63,10 @@ __device__ __forceinline__ bf16x8 pack8(const float* x) {
 // 16 bytes per lane from base + off (off per lane) to 1 KB of LDS at `lds`,
 // lane after lane, without a register between.  In asm, because the compiler
 // would wait for every such load before the next read of LDS; whoever reads
-// the data waits for it by count and passes a barrier first.
+// the data waits for it by count and passes a barrier first.  (The compiler warns that
+// m0 is reserved; named, it is not expected to hold a value across the statement.)
+#pragma clang diagnostic push
+#pragma clang diagnostic ignored "-Winline-asm"
 __device__ __forceinline__ void load_to_lds(const char* base, uint32_t off, const char* lds) {
   const uint32_t at = __builtin_amdgcn_readfirstlane((uint32_t)(uintptr_t)(lds_void*)lds);
   asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %2"
@@ -71,6 +74,7 @@ __device__ __forceinline__ void load_to_lds(const char* base, uint32_t off, cons
                : "s"(at), "v"(off), "s"(base)
                : "memory", "m0");
 }
+#pragma clang diagnostic pop
 template <int N>
 __device__ __forceinline__ void wait_loads() {  // until at most N are in flight
   asm volatile("s_waitcnt vmcnt(%0)" : : "n"(N) : "memory");
