@@ -60,17 +60,18 @@ def _rows(t, name, heads, head_dim, dtype):
     return t.data_ptr(), s0 if n > 1 else heads * head_dim, n
 
 
-def _same_gpu(dev, **tensors):
-    """Every tensor on GPU `dev`: the kernels follow its pointer."""
+def _refuse(gpu, **tensors):
+    """Says which of the tensors, which the kernels would read by their pointers, is
+    not on GPU `gpu`."""
     for name, t in tensors.items():
-        if dev < 0 or t.get_device() != dev:
-            where = f"GPU {dev}" if dev >= 0 else "a GPU"
+        if gpu < 0 or t.get_device() != gpu:
+            where = f"GPU {gpu}" if gpu >= 0 else "a GPU"
             raise _lib.S2moeError(_lib.EINVAL, f"{name} is on {t.device}, not on {where}")
 
 
 def _other(stream, device):
     """`stream` as torch's object, or None if it is the current one."""
-    if stream is None or _lib._stream(stream) == _lib._stream(None):
+    if _lib._stream(stream) == _lib._stream(None):
         return None
     if isinstance(stream, torch.cuda.Stream):
         return stream
@@ -124,7 +125,7 @@ class KVCache:
         self.max_seqs, self.max_pages, self.dtype = max_seqs, max_pages, dtype
         dev = self.k.device
         self._gpu = self.k.get_device()
-        _same_gpu(self._gpu, **{name: getattr(self, name) for name in want})
+        _refuse(self._gpu, **{name: getattr(self, name) for name in want})
         self.status = torch.zeros(KV_MAX_REQUESTS, dtype=i32, device=dev)
         self.copied = torch.full((KV_MAX_REQUESTS, 2), -1, dtype=i32, device=dev)
         self.struct = _lib.KvCacheStruct(n_layers, n_kv_heads, head_dim, n_pages, page_size,
@@ -147,7 +148,8 @@ class KVCache:
         """Sequence dst[i] becomes a copy of src[i] on the same pages."""
         n = src.shape[0]
         ps, pd = _ints(src, "src", n), _ints(dst, "dst", n)
-        _same_gpu(self._gpu, src=src, dst=dst)
+        if src.get_device() != self._gpu or dst.get_device() != self._gpu:
+            _refuse(self._gpu, src=src, dst=dst)
         with self._lock:
             _lib._check(self._lib.s2moe_kv_fork(self._ref, n, ps, pd, self._status,
                                                 _lib._stream(stream)))
@@ -157,7 +159,8 @@ class KVCache:
         would be written to is copied."""
         n = seqs.shape[0]
         ps, pe = _ints(seqs, "seqs", n), _ints(extra, "extra", n)
-        _same_gpu(self._gpu, seqs=seqs, extra=extra)
+        if seqs.get_device() != self._gpu or extra.get_device() != self._gpu:
+            _refuse(self._gpu, seqs=seqs, extra=extra)
         with self._lock:
             _lib._check(self._lib.s2moe_kv_reserve(self._ref, n, ps, pe, self._copied,
                                                    self._status, _lib._stream(stream)))
@@ -171,7 +174,9 @@ class KVCache:
         if tv != t:
             raise ValueError(f"v holds {tv} tokens, k {t}")
         ps, po = _ints(seqs, "seqs", n), _ints(tok_off, "tok_off", n + 1)
-        _same_gpu(self._gpu, k=k, v=v, seqs=seqs, tok_off=tok_off)
+        g = self._gpu
+        if not (g == k.get_device() == v.get_device() == seqs.get_device() == tok_off.get_device()):
+            _refuse(g, k=k, v=v, seqs=seqs, tok_off=tok_off)
         _lib._check(self._lib.s2moe_kv_append(self._ref, layer, n, t, ps, po, kp, ldk, vp, ldv,
                                               _lib._stream(stream)))
 
@@ -184,10 +189,11 @@ class KVCache:
         if path is not None:
             _lib._expect(path, "path", _I32, (n, most))
             pp = _lib._ptr(path)
+            if path.get_device() != self._gpu:
+                _refuse(self._gpu, path=path)
         ps, pa = _ints(seqs, "seqs", n), _ints(n_accept, "n_accept", n)
-        _same_gpu(self._gpu, seqs=seqs, n_accept=n_accept)
-        if path is not None:
-            _same_gpu(self._gpu, path=path)
+        if seqs.get_device() != self._gpu or n_accept.get_device() != self._gpu:
+            _refuse(self._gpu, seqs=seqs, n_accept=n_accept)
         with self._lock:
             _lib._check(self._lib.s2moe_kv_commit(self._ref, n, most, ps, pp, pa, self._status,
                                                   _lib._stream(stream)))
@@ -196,7 +202,8 @@ class KVCache:
         """Empties the sequences."""
         n = seqs.shape[0]
         ps = _ints(seqs, "seqs", n)
-        _same_gpu(self._gpu, seqs=seqs)
+        if seqs.get_device() != self._gpu:
+            _refuse(self._gpu, seqs=seqs)
         with self._lock:
             _lib._check(self._lib.s2moe_kv_free(self._ref, n, ps, self._status,
                                                 _lib._stream(stream)))
@@ -254,8 +261,10 @@ class TreeAttention:
         qp, ldq, t = _rows(q, "q", Hq, D, c.dtype)
         ps, po = _ints(seqs, "seqs", n), _ints(tok_off, "tok_off", n + 1)
         pp = _ints(parent, "parent", t)
-        _same_gpu(c._gpu, q=q, seqs=seqs, tok_off=tok_off, parent=parent)
-        other = _other(stream, q.device)
+        g = c._gpu
+        if not (g == q.get_device() == seqs.get_device() == tok_off.get_device() == parent.get_device()):
+            _refuse(g, q=q, seqs=seqs, tok_off=tok_off, parent=parent)
+        other = None if stream is None else _other(stream, q.device)
         if out is None:
             out = _result(q, (t, Hq, D), other)
             op, ldo = out.data_ptr(), Hq * D
@@ -263,7 +272,8 @@ class TreeAttention:
             op, ldo, to = _rows(out, "out", Hq, D, c.dtype)
             if to != t:
                 raise ValueError(f"out holds {to} tokens, q {t}")
-            _same_gpu(c._gpu, out=out)
+            if out.get_device() != g:
+                _refuse(g, out=out)
         # A struct of its own for other strides than those of whole rows: another thread
         # may be in a call with self.attn.
         ref = self._ref
@@ -295,12 +305,14 @@ def prompt_attention(q, k, v, tok_off, out=None, scale: float | None = None, str
         raise ValueError("tok_off: expected int32 [n + 1]")
     n = tok_off.shape[0] - 1
     po = _ints(tok_off, "tok_off", n + 1)
-    _same_gpu(q.get_device(), q=q, k=k, v=v, tok_off=tok_off)
+    g = q.get_device()
+    if g < 0 or not g == k.get_device() == v.get_device() == tok_off.get_device():
+        _refuse(g, q=q, k=k, v=v, tok_off=tok_off)
     if out is None:
-        out = _result(q, (t, Hq, D), _other(stream, q.device))
+        out = _result(q, (t, Hq, D), None if stream is None else _other(stream, q.device))
         op = out.data_ptr()
-    else:
-        _same_gpu(q.get_device(), out=out)
+    elif out.get_device() != g:
+        _refuse(g, out=out)
     a = _lib.Attn(Hq, Hkv, D, code, D ** -0.5 if scale is None else scale, ldq, ldk, ldv, ldo)
     _lib._check(_lib.load().s2moe_prompt_attention(ctypes.byref(a), n, t, qp, kp, vp, po, op,
                                                    _lib._stream(stream)))
