@@ -458,8 +458,9 @@ typedef struct s2moe_attn {
    numerators of BF16 caches enter the second product as bf16.
    q [n_tokens][n_heads][D], parent [n_tokens] int32, seqs [n], tok_off
    [n + 1], out [n_tokens][n_heads][D]; max_nodes is the largest tree of the
-   call, at most S2MOE_MAX_TOKENS (further nodes of a tree are left out), and n
-   at most S2MOE_KV_MAX_REQUESTS.  workspace must hold
+   call, at most S2MOE_MAX_TOKENS (further nodes of a tree are left out, their
+   rows of out not written; the kernel is chosen by max_nodes, so that one far
+   above the call's trees costs time), and n at most S2MOE_KV_MAX_REQUESTS.  workspace must hold
    s2moe_tree_attention_workspace_bytes (0 on bad arguments) for n, max_nodes
    or more; its contents do not matter, but a call's second launch reads there
    what its first has left: one workspace serves one call at a time, and calls

@@ -17,9 +17,11 @@
 //
 // Bound: the matrix cores at D = 128 (12289 tokens, 32/4 heads: 1.16-1.22 ms, 1.02-1.06
 // PFLOP/s where a large library product reaches 1.25), the weights' vector
-// instructions at D = 64 (8192 tokens, 64/8 heads: 0.57 ms, 0.97 PFLOP/s); short
-// prompts by what a workgroup waits for before its first product (24 of 512 tokens,
-// 32/8 heads of 128: 93 us, 0.55 PFLOP/s).
+// instructions at D = 64 (8192 tokens, 64/8 heads: 0.57-0.60 ms, 0.92-0.97 PFLOP/s);
+// short prompts by what a workgroup waits for before its first product and by the
+// vector instructions (24 of 512 tokens, 32/8 heads of 128: 93 us, 0.55 PFLOP/s; 24 of
+// up to 1024, 64/8 heads of 64: of all cycles vector units 53 %, matrix cores 22 %, and
+// 38 % of the waves' time is spent waiting).
 #include "attention.h"
 #include "attn_common.h"
 
@@ -679,8 +681,9 @@ template <int D>
 hipError_t launch_f32(const PromptArgs& a, hipStream_t s) {
   // By keys while rows alone would not give every SIMD of the GPU a wave, and for long
   // prompts, whose workgroups of 32 rows end more evenly than those of 128.  us by keys
-  // / by rows: 3 x 150 tokens, 4/2 heads of 64, 9 / 16; 32/8 heads of 128: 64 x 64 96 /
-  // 63, 32 x 128 118 / 107, 16 x 256 162 / 194, 4 x 1024 440 / 588, 1 x 4096 1549 / 1757 (but 4 x 256 54 / 47).
+  // / by rows: 3 x 150 tokens, 4/2 heads of 64, 9 / 16; 8 x 2000 201 / 319; 32/8 heads of
+  // 128: 64 x 64 99 / 59, 32 x 128 121 / 103, 16 x 256 167 / 188, 4 x 1024 443 / 567,
+  // 1 x 4096 1511 / 1721 (but 4 x 256 54 / 45); of 64: 32 x 128 70 / 57, 4 x 1024 215 / 292.
   const auto blocks = [&](int rows) { return ((int64_t)a.n_tokens * a.G / rows + a.n) * a.Hkv; };
   if (blocks(32) < 1024 || a.n_tokens / a.n >= 256)
     prompt_f32_kernel<D, true><<<(unsigned)blocks(32), 256, 0, s>>>(a);

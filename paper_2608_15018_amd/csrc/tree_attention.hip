@@ -27,10 +27,15 @@
 // Bound: reading the keys and values (16 sequences of 8192 tokens, 32/8 heads of 128,
 // one node each: 101 us, 5.3 TB/s; 256 of 2048: 5.8; a plain read stream reaches 6.9);
 // of the two workgroups on a compute unit the older ends at 73 us, the younger at 89.
-// With hundreds of rows the matrix and vector units (64 nodes over
-// 65537 tokens, 64/8 heads of 64: 113 us, 0.61 PFLOP/s).  A single short sequence by
-// dependent loads (offsets, length, page, keys) and the second launch: 11 us for one
-// node over 2047 tokens.
+// Ragged trees of up to 72 rows (64 sequences, 110 us, 3.9 TB/s) by waiting: 80 % of the
+// waves' time, the matrix cores have 7 % of the cycles.  With hundreds of rows a wave's
+// products and weights take turns and two waves a SIMD overlap them only in part (64
+// nodes over 65537 tokens, 64/8 heads of 64: 107-117 us, 0.61 PFLOP/s; vector units 44 %
+// of the cycles, matrix cores 25 %).  A single short sequence by dependent loads
+// (offsets, length, page, keys) and the second launch: 11 us for one node over 2047
+// tokens, 6.9 + 2.7.  16 nodes over 4093 take 14.6 + 4.5: 264 units for 512 workgroups,
+// so half of them have nothing, and the others walk their 128 keys in four stages with
+// a barrier each and leave 64 rows of parts.
 #include "attention.h"
 #include "attn_common.h"
 
@@ -332,7 +337,9 @@ __device__ __forceinline__ void write_row(const TreeArgs& a, int first, int hk, 
 template <typename E, int D, int NT>
 struct KeysPlan {
   static constexpr int kRows = 16 * NT;
-  // Workgroups that fit a compute unit.
+  // Workgroups that fit a compute unit.  fp32 at D = 128 needs all registers: with two
+  // it spills, 16 sequences of 4096 tokens (32/8 heads) 103 -> 206 us at one node each,
+  // 135 -> 307 at eight, one of 2047 12.8 -> 25.5.
   static constexpr int kPerCu = D * sizeof(E) == 512 ? 1 : 2;
   static constexpr int kGroups = 256 * kPerCu;
   static constexpr int kSums = 4 * 16 * (D + 4) * 4;  // bytes of the waves' sums of 16 rows
@@ -885,9 +892,12 @@ hipError_t launch_join(const TreeArgs& a, hipStream_t s) {
   static_assert(Plan::kGroups <= 512, "one thread a workgroup");
   const int rows = part_rows(a, Plan::kRows);
   const int64_t blocks = (int64_t)a.n * a.Hkv * (((int64_t)a.G * a.max_nodes + Plan::kRows - 1) / Plan::kRows);
-  // Ranked: 16 nodes (64 rows) over 4093 tokens 22.4 -> 19.7 us, 64 nodes (512 rows)
-  // over 65537 117 -> 113; 4 rows over 2047 tokens 10.8 -> 12.0, 64 ragged trees
-  // 109 -> 113.
+  // Ranked, measured both ways for 1 to 64 sequences of 1000 to 65537 tokens and 1 to 64
+  // nodes, six head layouts: where the rule ranks 0.63 to 1.06 times the other time,
+  // mostly below 1 (one sequence of 16000, 32/4 heads of 128, 16 nodes 46 -> 29 us; 4 of
+  // 2000, 32/8, 16 nodes 33 -> 22; 4 of 9000, 64 nodes 71 -> 74); where it does not 0.90
+  // to 1.5 times, mostly above (16 of 1000, 64/8 heads of 64, 40 nodes 53 -> 79; 64 of
+  // 1500, 32/4, one node 36 -> 37; but one of 16000, 32/4, one node 18.1 -> 16.4).
   if (rows > 16 && blocks < Plan::kGroups / 4)
     tree_join_kernel<E, D, 8><<<dim3((unsigned)blocks, (rows + 3) / 4), 512, 0, s>>>(a, Plan::kGroups, Plan::kRows);
   else
@@ -927,7 +937,9 @@ struct ByRows {
 // rows the waves split the keys.  us by rows / by keys, 32/8 heads of 128: over 4096 tokens 4
 // rows 11.2 / 11.5, 16 rows 14 / 15, 20 rows 13 / 17, 32 rows 14 / 18; 16 sequences of
 // 8192 101 / 101, 106 / 105, 108 / 126, 113 / 129; 64 of up to 6000 163 / 156, 168 /
-// 161, 175 / 198, 175 / 197.  fp32 goes by keys only.
+// 161, 175 / 198, 175 / 197.  fp32 goes by keys only.  The rows are those of max_nodes,
+// since the host knows no other: one node a sequence announced as 16 takes 11.1 us for
+// 10.3 (one of 2047 tokens), 14.6 for 12.5 (4 of 2000), 79 for 74 (64 of 1500).
 template <int D, typename F>
 auto choose(int64_t rows, bool f32, F f) {
   if (f32) return rows <= 16 ? f(ByKeys<float, D, 1>{}) : f(ByKeys<float, D, 2>{});
