@@ -109,7 +109,8 @@ __device__ __forceinline__ Request request(const TreeArgs& a, int i) {
   r.seq = a.seqs[i];
   const bool good = r.first >= 0 && r.first < end && end <= a.n_tokens && r.seq >= 0 && r.seq < a.max_seqs;
   r.T = good ? min(end - r.first, a.max_nodes) : 0;
-  const int cap = a.max_pages << a.log_p;
+  // No memory holds 2^31 tokens; below that tiles may be rounded up in 32 bits.
+  const int cap = min(a.max_pages << a.log_p, 0x7FFFFF00);
   r.len = good ? min(max(a.length[r.seq], 0), cap) : 0;
   r.total = r.len + min(r.T, cap - r.len);
   return r;

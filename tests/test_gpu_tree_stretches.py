@@ -101,3 +101,29 @@ def test_one_long_sequence_of_many_tiles_a_workgroup():
     run("bf16", (8, 8, 128), [70000], [1], 8, seed=35, P=256)
     run("bf16", (4, 1, 64), [140000], [5], 2, seed=36, P=64)
     run("f32", (4, 1, 64), [140000], [4], 2, seed=37, P=64)
+
+
+@pytest.mark.parametrize("dtype,heads,T", [("bf16", (2, 1, 64), 3), ("bf16", (32, 1, 64), 3), ("f32", (2, 1, 64), 3)])
+def test_a_length_of_no_sense_among_others(dtype, heads, T):
+    """A table whose rows could hold 2^31 - 16 tokens, and a length word that says so: its own rows get something,
+    the other sequences' what they should."""
+    import paper_2608_15018_amd as s2
+    from tests.test_gpu_attention import DT, ints
+
+    Hq, Hkv, D = heads
+    g = torch.Generator(device="cuda").manual_seed(41)
+    cache = s2.KVCache(1, Hkv, D, 64, 16, 3, (1 << 27) - 1, dtype=DT[dtype])
+    cache.k.normal_(generator=g), cache.v.normal_(generator=g)
+    lengths = [150, 0, 333]
+    cache.reserve(ints([0, 2]), ints([150 + T, 333 + T]))
+    cache.length.copy_(ints(lengths))
+    q = torch.randn((3 * T, Hq, D), generator=g, device="cuda").to(DT[dtype])
+    par = [-1, 0, 1] * 3
+    att = s2.TreeAttention(cache, Hq, 3, T)
+    sane = att(0, q[:2 * T], ints([0, 2]), ints([0, T, 2 * T]), ints(par[:2 * T]))
+    for wrong in (2**31 - 1, 2**31 - 17, 2**31 - 16 - T):
+        cache.length[1] = wrong
+        got = att(0, torch.cat([q[:T], q[2 * T:], q[T:2 * T]]), ints([0, 1, 2]), ints([0, T, 2 * T, 3 * T]), ints(par))
+        torch.cuda.synchronize()
+        for a, b in ((got[:T], sane[:T]), (got[2 * T:], sane[T:])):
+            check(a, b.double().cpu().numpy(), dtype)
