@@ -479,7 +479,7 @@ s2moe_status s2moe_tree_attention(const s2moe_kv_cache *cache, int32_t layer,
    rows tok_off[t] .. tok_off[t + 1] - 1 of q, k, v and out are prompt t, and
    row i sees the rows of its prompt up to itself.  k, v [n_tokens][n_kv_heads]
    [D].  tok_off [n + 1] int32, ascending from 0 to n_tokens; rows outside
-   it are not written.  Infinities, NaN and precision as in s2moe_tree_attention.
+   it are not written, and none at all where it does not ascend.  Infinities, NaN and precision as in s2moe_tree_attention.
    n <= S2MOE_KV_MAX_REQUESTS.  out must not overlap q, k or v. */
 s2moe_status s2moe_prompt_attention(const s2moe_attn *attn, int32_t n, int32_t n_tokens,
                                     const void *q, const void *k, const void *v,

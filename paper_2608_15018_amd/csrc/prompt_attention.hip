@@ -37,12 +37,14 @@ constexpr int kShortPrompt = 1024;
 
 // Workgroup b of a kv head: which rows of which prompt.  Prompts take
 // ceil(len G / rows) workgroups each, last ones first (they see the most
-// keys); 256 threads share the offsets.
+// keys); 256 threads share the offsets.  None where the offsets do not ascend: prompts
+// that overlap could be more workgroups than 32 bits count.
 __device__ bool find_block(const PromptArgs& a, int b, int rows, int* first, int* len, int* qb) {
   __shared__ int wave_s[4], found_s[3];
   const int tid = threadIdx.x, lane = tid & 63, w = tid >> 6;
   const int per = (a.n + 255) >> 8;  // consecutive prompts a thread looks at
   int n[4], f[4], mine = 0;
+  bool falls = false;
 #pragma unroll
   for (int i = 0; i < 4; ++i) {
     const int s = per * tid + i;
@@ -50,6 +52,7 @@ __device__ bool find_block(const PromptArgs& a, int b, int rows, int* first, int
     if (i < per && s < a.n) {
       f[i] = a.tok_off[s];
       const int end = a.tok_off[s + 1];
+      falls |= end < f[i];
       n[i] = f[i] >= 0 && f[i] < end && end <= a.n_tokens ? end - f[i] : 0;
     }
     mine += (n[i] * a.G + rows - 1) / rows;
@@ -60,15 +63,17 @@ __device__ bool find_block(const PromptArgs& a, int b, int rows, int* first, int
     const int y = __shfl_up(inc, d);
     if (lane >= d) inc += y;
   }
-  if (lane == 63) wave_s[w] = inc;
+  const bool any = __any(falls);
+  if (lane == 63) wave_s[w] = any ? -1 : inc;
   __syncthreads();
-  int at = inc - mine, total = 0;
+  int at = inc - mine, total = 0, sign = 0;
 #pragma unroll
   for (int i = 0; i < 4; ++i) {
     at += i < w ? wave_s[i] : 0;
     total += wave_s[i];
+    sign |= wave_s[i];
   }
-  if (b >= total) return false;
+  if (sign < 0 || b >= total) return false;
   b = total - 1 - b;
 #pragma unroll
   for (int i = 0; i < 4; ++i) {
