@@ -11,6 +11,10 @@ parent within its tree, -1 below the last kept token):
     o = attention(layer, q, seqs, tok_off, parent)
     ...                                           # the layer's experts, the other layers
     cache.commit(seqs, path, n_accept)            # once per step: keep the accepted path
+
+Calls are made with the cache's GPU current.  With `stream`, the inputs have to be
+ready there, and kept (or recorded on it) until it is done with them, as with any torch
+tensor that another stream reads.
 """
 
 from __future__ import annotations
