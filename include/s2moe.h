@@ -68,7 +68,11 @@ typedef enum s2moe_dtype {
      and activation must therefore stay below 65504 (larger finite values
      become infinite, with no error), and magnitudes below about 6.1e-5
      keep fewer significant bits (fp16 subnormals). */
-  S2MOE_Q4G32 = 2
+  S2MOE_Q4G32 = 2,
+  /* rows and weights of s2moe_scaled_matmul: 8-bit floating point with four
+     exponent and three mantissa bits (largest value 448, no infinities), one
+     fp32 scale for each block of S2MOE_SCALE_BLOCK elements. */
+  S2MOE_E4M3 = 3
 } s2moe_dtype;
 
 /* Readings of the paper's gating where the text leaves a choice (0 = default). */
@@ -414,6 +418,47 @@ s2moe_status s2moe_kv_append(const s2moe_kv_cache *cache, int32_t layer, int32_t
                              const void *k, int64_t ldk, const void *v, int64_t ldv,
                              void *stream);
 
+/* Positions of new tokens: pos[tok_off[i] + j] is the length of sequence seqs[i]
+   plus j, or with `parent` (as s2moe_tree_attention takes it) plus the number of
+   node j's ancestors within the tree.  Trees may have any number of nodes; a node
+   whose parent is neither -1 nor an earlier node counts as one below the last kept
+   token.  One call serves all layers of a step.  pos, parent: [n_tokens] int32,
+   parent may be NULL; pos must overlap no input.  Rows of pos outside the requests
+   are not written.  n_tokens <= 2^28. */
+s2moe_status s2moe_kv_positions(const s2moe_kv_cache *cache, int32_t n, int32_t n_tokens,
+                                const int32_t *seqs, const int32_t *tok_off,
+                                const int32_t *parent, int32_t *pos, void *stream);
+
+/* How queries and keys turn with their position.  Strides are in elements from one
+   token to the next, as in s2moe_kv_append. */
+typedef struct s2moe_rotation {
+  int32_t n_heads;    /* query heads, 1 .. 1024                                     */
+  int32_t rot_dim;    /* coordinates of a head that turn: the first rot_dim, a
+                         multiple of 16, <= head_dim; the others stay as they are   */
+  int32_t neighbours; /* 1: pair j is coordinates 2 j and 2 j + 1;
+                         0: coordinates j and j + rot_dim / 2                       */
+  int64_t ldq, ldk, ldv, ldqo, ldko; /* of q, k, v, q_out, k_out                    */
+} s2moe_rotation;
+
+/* s2moe_kv_append with queries and keys rotated on the way: pair j of a token of
+   position pos[t], coordinates (a, b), becomes (a cos - b sin, b cos + a sin) of the
+   angle pos[t] inv_freq[j] (radians; positions may be any int32, and far ones keep
+   their angle).  Writes the rotated queries to q_out [n_tokens][n_heads][head_dim],
+   the rotated keys and the values into the cache's slots as s2moe_kv_append does,
+   and, unless k_out is NULL, the rotated keys of every token of a request to k_out
+   [n_tokens][n_kv_heads][head_dim] as well, whether or not its slot could be
+   written (the keys of s2moe_prompt_attention).  q, k, v, q_out and k_out have the
+   cache's dtype.  q_out may be q and k_out may be k with the same stride (in place),
+   and otherwise they must not overlap q, k, v or each other.  pos [n_tokens] int32,
+   inv_freq [rot_dim / 2] fp32.  Sines, cosines and products are fp32, rounded once.
+   Rows outside the requests are not written. */
+s2moe_status s2moe_kv_append_rotated(const s2moe_kv_cache *cache, int32_t layer,
+                                     const s2moe_rotation *rotation, int32_t n, int32_t n_tokens,
+                                     const int32_t *seqs, const int32_t *tok_off,
+                                     const int32_t *pos, const float *inv_freq, const void *q,
+                                     const void *k, const void *v, void *q_out, void *k_out,
+                                     void *stream);
+
 /* Keeps the accepted path of each drafted tree: slot length + path[i][j] moves
    to slot length + j for j < n_accept[i] in every layer (path ascending), the
    length grows by n_accept[i], and pages past it are given back.  With path
@@ -484,6 +529,60 @@ s2moe_status s2moe_tree_attention(const s2moe_kv_cache *cache, int32_t layer,
 s2moe_status s2moe_prompt_attention(const s2moe_attn *attn, int32_t n, int32_t n_tokens,
                                     const void *q, const void *k, const void *v,
                                     const int32_t *tok_off, void *out, void *stream);
+
+/* ---------------------------------------------------------------------------
+   The dense half of a layer: the norm before each half, and projections in 8-bit
+   floating point.
+
+   A matrix of rows in E4M3 is codes [n][cols] (one byte each) and scales
+   [ceil(cols / 128)][n], one fp32 number for each block of 128 elements of a row:
+   element j of row i stands for codes[i][j] * scales[j / 128][i].  The scale of a
+   block is its largest magnitude / 448 (2^-100 / 448 where it is less than 2^-100),
+   so that the largest code is 448 exactly.  The scales of one block of all rows lie
+   together, which is how a product reads them.  Weights are codes [n][k] and
+   scales [ceil(n / 128)][ceil(k / 128)], one for 128 x 128 elements.  A row with an
+   infinity or NaN has unspecified values, and no other row is touched by it.
+
+   Strides ld* are in elements from one row to the next, at most 2^22; rows of
+   inputs and of codes begin at multiples of 16 bytes.  Scales need 4-byte alignment
+   only. */
+#define S2MOE_SCALE_BLOCK 128
+
+/* h = x + residual, residual <- h, out = h * weight / sqrt(mean(h^2) + eps) of each of
+   n rows of `hidden` elements (a multiple of 16, at most 16384).  Sums and the norm
+   are fp32, from h before it is rounded to the residual's type; squares are summed as
+   they are, so rows should stay below about 1e17.  residual may be NULL: h = x.  x, residual and weight [hidden] are F32 or BF16,
+   each by itself; out F32, BF16 or E4M3 with `scales` (NULL otherwise), lds >= n.
+   No output may overlap an input or another output.  eps > 0, finite.  n <= 2^22. */
+s2moe_status s2moe_add_norm(int32_t n, int32_t hidden, const void *x, int64_t ldx, int32_t x_dtype,
+                            void *residual, int64_t ldr, int32_t r_dtype, const void *weight,
+                            int32_t w_dtype, float eps, void *out, int64_t ldo, int32_t out_dtype,
+                            float *scales, int64_t lds, void *stream);
+
+/* Rows in E4M3.  cols: a multiple of 16, at most 2^18; n <= 2^22. */
+s2moe_status s2moe_quantize(int32_t n, int32_t cols, const void *x, int64_t ldx, int32_t x_dtype,
+                            void *codes, int64_t ldc, float *scales, int64_t lds, void *stream);
+
+/* Weights in E4M3, once at model load: w [rows][cols], scales [ceil(rows / 128)][lds],
+   lds >= ceil(cols / 128).  Limits as in s2moe_quantize. */
+s2moe_status s2moe_quantize_weight(int32_t rows, int32_t cols, const void *w, int64_t ldw,
+                                   int32_t w_dtype, void *codes, int64_t ldc, float *scales,
+                                   int64_t lds, void *stream);
+
+/* out[i][j] = sum_b x_scales[b][i] w_scales[j / 128][b] sum_{k in block b} x[i][k] w[j][k]
+   for m rows of x and n rows of w, in fp32, rounded once to out's type (F32 or BF16).
+   x, w: codes; k a multiple of 16, at most 2^18, m, n <= 2^22.  x_scales [ceil(k / 128)]
+   [ldxs], ldxs >= m; w_scales [ceil(n / 128)][ldws], ldws >= ceil(k / 128).  out [m][n],
+   16-byte aligned, ldo >= n (any: rows may begin anywhere an element may).  out must
+   not overlap an input.  Sums are in a fixed order: equal calls give equal bits.
+   F32 results hold fp32 sums of exact products.  BF16 ones come from the 8-bit matrix
+   instructions, twice as fast where the matrix cores are the bound, which cut each
+   product off 13 bits below the largest exponent among its eight neighbours: about
+   1.4e-5 of the result on normal data, where bf16's own rounding is 1.7e-3. */
+s2moe_status s2moe_scaled_matmul(int32_t m, int32_t n, int32_t k, const void *x, int64_t ldx,
+                                 const float *x_scales, int64_t ldxs, const void *w, int64_t ldw,
+                                 const float *w_scales, int64_t ldws, void *out, int64_t ldo,
+                                 int32_t out_dtype, void *stream);
 
 /* Diagnostic, not a step of the verify pass: read `bytes` of device memory
    at `src` once, front to back, with the same 16-byte nontemporal loads the

@@ -54,3 +54,12 @@ from .attention import (  # noqa: F401
     TreeAttention,
     prompt_attention,
 )
+from .dense import (  # noqa: F401
+    E4M3,
+    Fp8Rows,
+    Fp8Weight,
+    add_norm,
+    fp8_matmul,
+    quantize,
+    quantize_weight,
+)

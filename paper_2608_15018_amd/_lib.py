@@ -21,7 +21,7 @@ LIB_PATH = os.environ.get("S2MOE_LIBRARY") or os.path.join(
 HEADER_PATH = os.path.join(os.path.dirname(os.path.dirname(os.path.abspath(__file__))),
                            "include", "s2moe.h")
 
-F32, BF16, Q4G32 = 0, 1, 2
+F32, BF16, Q4G32, E4M3 = 0, 1, 2, 3
 DTYPE_CODES = {"f32": F32, "bf16": BF16, "q4g32": Q4G32}
 PREF_ACTIVATED_ONLY, BIAS_ABSOLUTE, GATE_FROM_BIASED, PACKED_WEIGHTS = 1, 2, 4, 8
 OK, EINVAL, EUNSUPPORTED, EWORKSPACE, EHIP = 0, 1, 2, 3, 4
@@ -81,6 +81,12 @@ class Attn(ctypes.Structure):
                 ("ldv", ctypes.c_int64), ("ldo", ctypes.c_int64)]
 
 
+class Rotation(ctypes.Structure):
+    _fields_ = [("n_heads", ctypes.c_int32), ("rot_dim", ctypes.c_int32),
+                ("neighbours", ctypes.c_int32), ("ldq", ctypes.c_int64), ("ldk", ctypes.c_int64),
+                ("ldv", ctypes.c_int64), ("ldqo", ctypes.c_int64), ("ldko", ctypes.c_int64)]
+
+
 _lib = None
 
 
@@ -122,7 +128,13 @@ def load():
             ("kv_append", [Cp, I, I, I, P, P, P, N, P, N, P]),
             ("kv_commit", [Cp, I, I, P, P, P, P, P]), ("kv_free", [Cp, I, P, P, P]),
             ("tree_attention", [Cp, I, Ap, I, I, I, P, P, P, P, P, ctypes.c_size_t, P, P]),
-            ("prompt_attention", [Ap, I, I, P, P, P, P, P, P])):
+            ("prompt_attention", [Ap, I, I, P, P, P, P, P, P]),
+            ("kv_positions", [Cp, I, I, P, P, P, P, P]),
+            ("kv_append_rotated", [Cp, I, ctypes.POINTER(Rotation), I, I] + [P] * 10),
+            ("add_norm", [I, I, P, N, I, P, N, I, P, I, ctypes.c_float, P, N, I, P, N, P]),
+            ("quantize", [I, I, P, N, I, P, N, P, N, P]),
+            ("quantize_weight", [I, I, P, N, I, P, N, P, N, P]),
+            ("scaled_matmul", [I, I, I, P, N, P, N, P, N, P, N, P, N, I, P])):
         f = getattr(lib, "s2moe_" + name)
         f.argtypes = types
         f.restype = ctypes.c_int

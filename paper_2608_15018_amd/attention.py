@@ -184,6 +184,67 @@ class KVCache:
         _lib._check(self._lib.s2moe_kv_append(self._ref, layer, n, t, ps, po, kp, ldk, vp, ldv,
                                               _lib._stream(stream)))
 
+    def positions(self, seqs, tok_off, n_tokens: int, parent=None, out=None, stream=None):
+        """Positions [n_tokens] int32 of new tokens, once per step for all layers: the
+        sequence's length plus the token's place among its new ones, or with `parent` plus
+        its depth in the drafted tree."""
+        n = seqs.shape[0]
+        ps, po = _ints(seqs, "seqs", n), _ints(tok_off, "tok_off", n + 1)
+        pp = None if parent is None else _ints(parent, "parent", n_tokens)
+        g = self._gpu
+        if not (g == seqs.get_device() == tok_off.get_device() == (g if parent is None else parent.get_device())):
+            _refuse(g, seqs=seqs, tok_off=tok_off, **({} if parent is None else {"parent": parent}))
+        if out is None:
+            out = _result(seqs, (n_tokens,), None if stream is None else _other(stream, seqs.device))
+        po_out = _ints(out, "out", n_tokens)
+        if out.get_device() != g:
+            _refuse(g, out=out)
+        _lib._check(self._lib.s2moe_kv_positions(self._ref, n, n_tokens, ps, po, pp, po_out,
+                                                 _lib._stream(stream)))
+        return out
+
+    def append_rotated(self, layer: int, q, k, v, seqs, tok_off, pos, inv_freq,
+                       neighbours: bool = False, out=None, k_out=None, stream=None):
+        """append with queries q [n_tokens, n_heads, head_dim] and keys turned by the angles
+        pos * inv_freq on the way; returns the turned queries.  inv_freq [rot_dim / 2]
+        float32: the first rot_dim coordinates turn, pairs of neighbours or of halves.
+        `out` takes the queries (q itself: in place), `k_out` the turned keys of every token
+        (k itself: in place), as the prompts' own attention reads them."""
+        n, Hkv, D, dt = seqs.shape[0], self.n_kv_heads, self.head_dim, self.dtype
+        if q.dim() != 3:
+            raise ValueError(f"q: expected [n_tokens, heads, {D}], got {tuple(q.shape)}")
+        Hq = q.shape[1]
+        qp, ldq, t = _rows(q, "q", Hq, D, dt)
+        kp, ldk, tk = _rows(k, "k", Hkv, D, dt)
+        vp, ldv, tv = _rows(v, "v", Hkv, D, dt)
+        ps, po, pp = _ints(seqs, "seqs", n), _ints(tok_off, "tok_off", n + 1), _ints(pos, "pos", t)
+        if inv_freq.dtype is not torch.float32 or inv_freq.dim() != 1 or not inv_freq.is_contiguous():
+            raise ValueError(f"inv_freq: expected contiguous float32 [rot_dim / 2], got "
+                             f"{inv_freq.dtype} {tuple(inv_freq.shape)}")
+        g = self._gpu
+        if not (g == q.get_device() == k.get_device() == v.get_device() == seqs.get_device()
+                == tok_off.get_device() == pos.get_device() == inv_freq.get_device()):
+            _refuse(g, q=q, k=k, v=v, seqs=seqs, tok_off=tok_off, pos=pos, inv_freq=inv_freq)
+        if out is None:
+            out = _result(q, (t, Hq, D), None if stream is None else _other(stream, q.device))
+            op, ldqo, to = out.data_ptr(), Hq * D, t
+        else:
+            op, ldqo, to = _rows(out, "out", Hq, D, dt)
+            if out.get_device() != g:
+                _refuse(g, out=out)
+        kop, ldko, tko = None, 0, t
+        if k_out is not None:
+            kop, ldko, tko = _rows(k_out, "k_out", Hkv, D, dt)
+            if k_out.get_device() != g:
+                _refuse(g, k_out=k_out)
+        if not (tk == tv == to == tko == t):
+            raise ValueError(f"q, k, v, out, k_out hold {t}, {tk}, {tv}, {to}, {tko} tokens")
+        r = _lib.Rotation(Hq, 2 * inv_freq.shape[0], int(neighbours), ldq, ldk, ldv, ldqo, ldko)
+        _lib._check(self._lib.s2moe_kv_append_rotated(
+            self._ref, layer, ctypes.byref(r), n, t, ps, po, pp, inv_freq.data_ptr(), qp, kp, vp,
+            op, kop, _lib._stream(stream)))
+        return out
+
     def commit(self, seqs, path, n_accept, stream=None):
         """Keeps nodes path[i, :n_accept[i]] of each drafted tree (ascending);
         path None: the first n_accept[i] tokens as they lie."""

@@ -6,6 +6,7 @@
 #include <cstdint>
 
 #include "attention.h"
+#include "rows.h"
 #include "s2moe.h"
 #include "status.h"
 
@@ -22,16 +23,12 @@ namespace {
 
 using s2moe::aligned;
 using s2moe::aligned16;
+using s2moe::bytes_meet;
+using s2moe::check_rows;
 using s2moe::fail;
 using s2moe::hip_status;
 using s2moe::ok;
-
-// Integer arrays may start anywhere a 32-bit integer may.
-#define S2MOE_REQUIRE_INTS(p)                                                              \
-  do {                                                                                     \
-    if ((p) == nullptr) return fail(S2MOE_EINVAL, "%s: %s is NULL", fn, #p);               \
-    if (!aligned(p, 4)) return fail(S2MOE_EINVAL, "%s: %s is not 4-byte aligned", fn, #p); \
-  } while (0)
+using s2moe::rows_meet;
 
 s2moe_status check_cache(const char* fn, const s2moe_kv_cache* cache, s2moe::KvCache* out) {
   if (cache == nullptr) return fail(S2MOE_EINVAL, "%s: cache is NULL", fn);
@@ -94,29 +91,11 @@ s2moe_status check_layer_index(const char* fn, const s2moe::KvCache& c, int32_t 
   return S2MOE_OK;
 }
 
-// Rows of `heads` heads, `ld` elements apart.
-s2moe_status check_rows(const char* fn, const char* name, int64_t ld, int heads, int D, int elt) {
-  if (ld < (int64_t)heads * D)
-    return fail(S2MOE_EINVAL, "%s: %s = %lld must be at least %d heads of %d", fn, name,
-                (long long)ld, heads, D);
-  if (ld > (int64_t)1 << 22)
-    return fail(S2MOE_EUNSUPPORTED, "%s: %s = %lld exceeds 2^22 elements", fn, name, (long long)ld);
-  if (ld * elt % 16 != 0)
-    return fail(S2MOE_EINVAL, "%s: %s = %lld elements is not a multiple of 16 bytes", fn, name,
-                (long long)ld);
+s2moe_status check_tokens(const char* fn, int32_t n_tokens) {
+  if (n_tokens < 0) return fail(S2MOE_EINVAL, "%s: n_tokens = %d < 0", fn, n_tokens);
+  if (n_tokens > 1 << 28)
+    return fail(S2MOE_EUNSUPPORTED, "%s: n_tokens = %d exceeds 2^28", fn, n_tokens);
   return S2MOE_OK;
-}
-
-// Whether rows of wa bytes every lda meet rows of wb bytes every ldb (n rows
-// each): rows of one wider array may lie side by side.
-bool rows_meet(const void* a, int64_t lda, int64_t wa, const void* b, int64_t ldb, int64_t wb,
-               int64_t n) {
-  const int64_t x = (int64_t)reinterpret_cast<uintptr_t>(a);
-  const int64_t y = (int64_t)reinterpret_cast<uintptr_t>(b);
-  if (y >= x + (n - 1) * lda + wa || x >= y + (n - 1) * ldb + wb) return false;
-  if (lda != ldb) return true;
-  const int64_t at = ((y - x) % lda + lda) % lda;  // where b's rows start within a's period
-  return at < wa || at + wb > lda;
 }
 
 s2moe_status check_attn(const char* fn, const s2moe_attn* attn) {
@@ -244,6 +223,108 @@ s2moe_status s2moe_kv_append(const s2moe_kv_cache* cache, int32_t layer, int32_t
   a.ldk = ldk;
   a.ldv = ldv;
   return hip_status(fn, s2moe::launch_kv_append(c, a, static_cast<hipStream_t>(stream)));
+}
+
+s2moe_status s2moe_kv_positions(const s2moe_kv_cache* cache, int32_t n, int32_t n_tokens,
+                                const int32_t* seqs, const int32_t* tok_off, const int32_t* parent,
+                                int32_t* pos, void* stream) {
+  const char* fn = "s2moe_kv_positions";
+  s2moe::KvCache c;
+  s2moe_status st = check_cache(fn, cache, &c);
+  if (st == S2MOE_OK) st = check_requests(fn, n);
+  if (st == S2MOE_OK) st = check_tokens(fn, n_tokens);
+  if (st != S2MOE_OK) return st;
+  if (n == 0 || n_tokens == 0) return ok();
+  S2MOE_REQUIRE_INTS(seqs);
+  S2MOE_REQUIRE_INTS(tok_off);
+  S2MOE_REQUIRE_INTS(pos);
+  if (parent != nullptr && !aligned(parent, 4))
+    return fail(S2MOE_EINVAL, "%s: parent is not 4-byte aligned", fn);
+  const int64_t bytes = (int64_t)n_tokens * 4;
+  if (bytes_meet(pos, bytes, seqs, (int64_t)n * 4) ||
+      bytes_meet(pos, bytes, tok_off, ((int64_t)n + 1) * 4) ||
+      (parent != nullptr && bytes_meet(pos, bytes, parent, bytes)))
+    return fail(S2MOE_EINVAL, "%s: pos overlaps seqs, tok_off or parent", fn);
+  return hip_status(fn, s2moe::launch_positions(c, n, n_tokens, seqs, tok_off, parent, pos,
+                                                static_cast<hipStream_t>(stream)));
+}
+
+s2moe_status s2moe_kv_append_rotated(const s2moe_kv_cache* cache, int32_t layer,
+                                     const s2moe_rotation* rotation, int32_t n, int32_t n_tokens,
+                                     const int32_t* seqs, const int32_t* tok_off,
+                                     const int32_t* pos, const float* inv_freq, const void* q,
+                                     const void* k, const void* v, void* q_out, void* k_out,
+                                     void* stream) {
+  const char* fn = "s2moe_kv_append_rotated";
+  s2moe::KvCache c;
+  s2moe_status st = check_cache(fn, cache, &c);
+  if (st == S2MOE_OK) st = check_requests(fn, n);
+  if (st == S2MOE_OK) st = check_layer_index(fn, c, layer);
+  if (st == S2MOE_OK) st = check_tokens(fn, n_tokens);
+  if (st != S2MOE_OK) return st;
+  if (rotation == nullptr) return fail(S2MOE_EINVAL, "%s: rotation is NULL", fn);
+  const s2moe_rotation& r = *rotation;
+  if (r.n_heads < 1) return fail(S2MOE_EINVAL, "%s: n_heads = %d < 1", fn, r.n_heads);
+  if (r.n_heads > 1024)
+    return fail(S2MOE_EUNSUPPORTED, "%s: n_heads = %d exceeds 1024", fn, r.n_heads);
+  if (r.rot_dim < 16 || r.rot_dim > c.D || r.rot_dim % 16 != 0)
+    return fail(S2MOE_EINVAL, "%s: rot_dim = %d must be a multiple of 16 in [16, %d]", fn,
+                r.rot_dim, c.D);
+  if (r.neighbours != 0 && r.neighbours != 1)
+    return fail(S2MOE_EINVAL, "%s: neighbours = %d must be 0 or 1", fn, r.neighbours);
+  if (n == 0 || n_tokens == 0) return ok();
+  S2MOE_REQUIRE_INTS(seqs);
+  S2MOE_REQUIRE_INTS(tok_off);
+  S2MOE_REQUIRE_INTS(pos);
+  S2MOE_REQUIRE_INTS(inv_freq);
+  S2MOE_REQUIRE_PTR(q);
+  S2MOE_REQUIRE_PTR(k);
+  S2MOE_REQUIRE_PTR(v);
+  S2MOE_REQUIRE_PTR(q_out);
+  if (k_out != nullptr && !aligned16(k_out))
+    return fail(S2MOE_EINVAL, "%s: k_out is not 16-byte aligned", fn);
+  const int e = c.elt();
+  if ((st = check_rows(fn, "ldq", r.ldq, r.n_heads, c.D, e)) != S2MOE_OK) return st;
+  if ((st = check_rows(fn, "ldk", r.ldk, c.Hkv, c.D, e)) != S2MOE_OK) return st;
+  if ((st = check_rows(fn, "ldv", r.ldv, c.Hkv, c.D, e)) != S2MOE_OK) return st;
+  if ((st = check_rows(fn, "ldqo", r.ldqo, r.n_heads, c.D, e)) != S2MOE_OK) return st;
+  if (k_out != nullptr && (st = check_rows(fn, "ldko", r.ldko, c.Hkv, c.D, e)) != S2MOE_OK)
+    return st;
+  const int64_t wq = (int64_t)r.n_heads * c.D * e, wk = (int64_t)c.Hkv * c.D * e;
+  const int64_t lq = r.ldq * e, lk = r.ldk * e, lv = r.ldv * e, lqo = r.ldqo * e, lko = r.ldko * e;
+  // In place: each element is read and written by one lane.
+  const bool same_q = q_out == q && lqo == lq, same_k = k_out == k && lko == lk;
+  if ((!same_q && rows_meet(q_out, lqo, wq, q, lq, wq, n_tokens)) ||
+      rows_meet(q_out, lqo, wq, k, lk, wk, n_tokens) ||
+      rows_meet(q_out, lqo, wq, v, lv, wk, n_tokens))
+    return fail(S2MOE_EINVAL, "%s: q_out overlaps q (other than in place), k or v", fn);
+  if (k_out != nullptr && ((!same_k && rows_meet(k_out, lko, wk, k, lk, wk, n_tokens)) ||
+                           rows_meet(k_out, lko, wk, q, lq, wq, n_tokens) ||
+                           rows_meet(k_out, lko, wk, v, lv, wk, n_tokens) ||
+                           rows_meet(k_out, lko, wk, q_out, lqo, wq, n_tokens)))
+    return fail(S2MOE_EINVAL, "%s: k_out overlaps k (other than in place), q, v or q_out", fn);
+  s2moe::RotateArgs a;
+  a.layer = layer;
+  a.n = n;
+  a.n_tokens = n_tokens;
+  a.Hq = r.n_heads;
+  a.rot = r.rot_dim;
+  a.neighbours = r.neighbours != 0;
+  a.seqs = seqs;
+  a.tok_off = tok_off;
+  a.pos = pos;
+  a.freq = inv_freq;
+  a.q = static_cast<const char*>(q);
+  a.k = static_cast<const char*>(k);
+  a.v = static_cast<const char*>(v);
+  a.q_out = static_cast<char*>(q_out);
+  a.k_out = static_cast<char*>(k_out);
+  a.ldq = r.ldq;
+  a.ldk = r.ldk;
+  a.ldv = r.ldv;
+  a.ldqo = r.ldqo;
+  a.ldko = r.ldko;
+  return hip_status(fn, s2moe::launch_append_rotated(c, a, static_cast<hipStream_t>(stream)));
 }
 
 s2moe_status s2moe_kv_commit(const s2moe_kv_cache* cache, int32_t n, int32_t max_path,

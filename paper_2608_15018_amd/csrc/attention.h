@@ -64,6 +64,27 @@ struct AppendArgs {
 };
 hipError_t launch_kv_append(const KvCache& c, const AppendArgs& a, hipStream_t s);
 
+// Without parents: each request's tokens one after another.
+hipError_t launch_positions(const KvCache& c, int n, int n_tokens, const int32_t* seqs,
+                            const int32_t* tok_off, const int32_t* parent, int32_t* pos,
+                            hipStream_t s);
+
+struct RotateArgs {
+  int layer, n, n_tokens, Hq, rot;
+  bool neighbours;  // pairs of coordinates 2 j and 2 j + 1, else j and j + rot / 2
+  const int32_t* seqs;
+  const int32_t* tok_off;
+  const int32_t* pos;
+  const float* freq;
+  const char* q;
+  const char* k;
+  const char* v;
+  char* q_out;
+  char* k_out;  // or null
+  int64_t ldq, ldk, ldv, ldqo, ldko;  // elements
+};
+hipError_t launch_append_rotated(const KvCache& c, const RotateArgs& a, hipStream_t s);
+
 struct TreeArgs {
   const char* k;  // the layer's pools
   const char* v;

@@ -1,0 +1,260 @@
+// Rows added to the residual stream and normalised, and rows and weights in 8 bits.
+//
+//   h = x + r,  r <- h,  y = h * w / sqrt(mean(h^2) + eps)
+//
+// in fp32 from the loads to one rounding of each output.  In 8 bits a block of 128
+// elements has one scale s = max(|y|, 2^-100) / 448, so that its largest element becomes
+// e4m3's largest, and the codes are y / s.  A row is read once: it stays in registers
+// between the sum of squares and the outputs.
+#include <type_traits>
+
+#include "attn_common.h"
+#include "dense.h"
+
+namespace s2moe {
+namespace {
+
+template <int N>
+__device__ __forceinline__ float ror(float x) {  // from N lanes on, within 16 lanes
+  return __uint_as_float(__builtin_amdgcn_update_dpp(0, __float_as_uint(x), 0x120 + N, 0xF, 0xF, true));
+}
+__device__ __forceinline__ float max16(float x) {
+  x = fmaxf(x, ror<8>(x));
+  x = fmaxf(x, ror<4>(x));
+  x = fmaxf(x, ror<2>(x));
+  return fmaxf(x, ror<1>(x));
+}
+__device__ __forceinline__ float sum16(float x) {
+  x += ror<8>(x);
+  x += ror<4>(x);
+  x += ror<2>(x);
+  return x + ror<1>(x);
+}
+
+// Eight neighbouring elements of a row.
+template <int T>
+struct Raw {
+  u32x4 v[T == kF32 ? 2 : 1];
+};
+template <int T>
+__device__ __forceinline__ Raw<T> load8(const char* row, int col) {
+  Raw<T> r;
+  const u32x4* p = reinterpret_cast<const u32x4*>(row + (int64_t)col * (T == kF32 ? 4 : 2));
+  r.v[0] = p[0];
+  if constexpr (T == kF32) r.v[1] = p[1];
+  return r;
+}
+template <int T>
+__device__ __forceinline__ void floats(const Raw<T>& r, float* f) {
+#pragma unroll
+  for (int i = 0; i < 8; ++i) {
+    if constexpr (T == kF32)
+      f[i] = __uint_as_float(r.v[i / 4][i % 4]);
+    else
+      f[i] = __uint_as_float(i & 1 ? r.v[0][i / 2] & 0xFFFF0000u : r.v[0][i / 2] << 16);
+  }
+}
+template <int T>
+__device__ __forceinline__ void store8(char* row, int col, const float* f) {
+  if constexpr (T == kF32) {
+    f32x4* p = reinterpret_cast<f32x4*>(row + (int64_t)col * 4);
+    p[0] = f32x4{f[0], f[1], f[2], f[3]};
+    p[1] = f32x4{f[4], f[5], f[6], f[7]};
+  } else {
+    *reinterpret_cast<bf16x8*>(row + (int64_t)col * 2) = pack8(f);
+  }
+}
+
+// The codes of eight elements whose block's scale is 1 / inv.  |y| inv is at most 448
+// and a rounding of fp32, which e4m3 rounds to 448.
+__device__ __forceinline__ uint2 codes8(const float* y, float inv) {
+  int lo = 0, hi = 0;
+  lo = __builtin_amdgcn_cvt_pk_fp8_f32(y[0] * inv, y[1] * inv, lo, false);
+  lo = __builtin_amdgcn_cvt_pk_fp8_f32(y[2] * inv, y[3] * inv, lo, true);
+  hi = __builtin_amdgcn_cvt_pk_fp8_f32(y[4] * inv, y[5] * inv, hi, false);
+  hi = __builtin_amdgcn_cvt_pk_fp8_f32(y[6] * inv, y[7] * inv, hi, true);
+  return uint2{(uint32_t)lo, (uint32_t)hi};
+}
+__device__ __forceinline__ float most8(const float* y) {
+  float top = 0.f;
+#pragma unroll
+  for (int i = 0; i < 8; ++i) top = fmaxf(top, fabsf(y[i]));
+  return top;
+}
+
+// Sixteen lanes' eight elements each, one block: codes and the scale.  `live` lanes have
+// elements, the others zeros.
+__device__ __forceinline__ void store_block(char* codes, float* scales, int64_t lds, int row, int col, bool live,
+                                            const float* y) {
+  const float scale = fmaxf(max16(most8(y)), kLeast) / kLargest;
+  if (!live) return;
+  *reinterpret_cast<uint2*>(codes + col) = codes8(y, 1.f / scale);
+  if ((threadIdx.x & 15) == 0) scales[(col / kBlock) * lds + row] = scale;
+}
+
+// kLanes lanes a row (64, or the whole workgroup), kChunks times eight elements each.
+template <int X, int R, int O, int kLanes, int kChunks>
+__global__ __launch_bounds__(256) void add_norm_kernel(NormArgs a) {
+  __shared__ float part[4];
+  const int lane = threadIdx.x % kLanes;
+  const int row0 = blockIdx.x * (256 / kLanes) + threadIdx.x / kLanes;
+  const int row = min(row0, a.n - 1);
+  const bool mine = row0 < a.n;
+  const char* x = a.x + row * a.ldx * (X == kF32 ? 4 : 2);
+  char* r = R == kNone ? nullptr : a.residual + row * a.ldr * (R == kF32 ? 4 : 2);
+  Raw<X> xs[kChunks];
+  Raw<R == kNone ? kBf16 : R> rs[kChunks];
+  u32x4 ws[kChunks][2];
+#pragma unroll
+  for (int c = 0; c < kChunks; ++c) {
+    const int col = (c * kLanes + lane) * 8;
+    if (col < a.H) {
+      xs[c] = load8<X>(x, col);
+      if constexpr (R != kNone) rs[c] = load8<R>(r, col);
+      if (a.w_type == kF32) {
+        ws[c][0] = reinterpret_cast<const u32x4*>(a.weight)[col / 4];
+        ws[c][1] = reinterpret_cast<const u32x4*>(a.weight)[col / 4 + 1];
+      } else {
+        ws[c][0] = reinterpret_cast<const u32x4*>(a.weight)[col / 8];
+      }
+    }
+  }
+  float h[kChunks][8], sum = 0.f;
+#pragma unroll
+  for (int c = 0; c < kChunks; ++c) {
+    const int col = (c * kLanes + lane) * 8;
+#pragma unroll
+    for (int i = 0; i < 8; ++i) h[c][i] = 0.f;
+    if (col < a.H) {
+      floats<X>(xs[c], h[c]);
+      if constexpr (R != kNone) {
+        float old[8];
+        floats<R>(rs[c], old);
+#pragma unroll
+        for (int i = 0; i < 8; ++i) h[c][i] += old[i];
+        if (mine) store8<R>(r, col, h[c]);
+      }
+#pragma unroll
+      for (int i = 0; i < 8; ++i) sum = fmaf(h[c][i], h[c][i], sum);
+    }
+  }
+  sum = sum_groups(sum16(sum));
+  if constexpr (kLanes > 64) {
+    if ((threadIdx.x & 63) == 0) part[threadIdx.x >> 6] = sum;
+    __syncthreads();
+    sum = (part[0] + part[1]) + (part[2] + part[3]);
+  }
+  const float norm = 1.f / sqrtf(sum / (float)a.H + a.eps);
+  if (!mine) return;
+  char* out = a.out + row * a.ldo * (O == kF32 ? 4 : O == kBf16 ? 2 : 1);
+#pragma unroll
+  for (int c = 0; c < kChunks; ++c) {
+    const int col = (c * kLanes + lane) * 8;
+    const bool live = col < a.H;
+    float y[8] = {};
+    if (live) {
+      float w[8];
+      if (a.w_type == kF32)
+        floats<kF32>(Raw<kF32>{{ws[c][0], ws[c][1]}}, w);
+      else
+        floats<kBf16>(Raw<kBf16>{{ws[c][0]}}, w);
+#pragma unroll
+      for (int i = 0; i < 8; ++i) y[i] = h[c][i] * norm * w[i];
+    }
+    if constexpr (O == kE4m3) {
+      store_block(out, a.scales, a.lds, row, col, live, y);
+    } else {
+      if (live) store8<O>(out, col, y);
+    }
+  }
+}
+
+// A wave takes 512 columns of a row.
+template <int X>
+__global__ __launch_bounds__(256) void quantize_kernel(QuantizeArgs a) {
+  const int lane = threadIdx.x & 63, parts = (a.cols + 511) / 512;
+  const int64_t all = (int64_t)a.n * parts;
+  for (int64_t at = (int64_t)blockIdx.x * 4 + wave_id(); at < all; at += (int64_t)gridDim.x * 4) {
+    const int row = (int)(at / parts), col = (int)(at % parts) * 512 + lane * 8;
+    const bool live = col < a.cols;
+    float y[8] = {};
+    if (live) floats<X>(load8<X>(a.x + row * a.ldx * (X == kF32 ? 4 : 2), col), y);
+    store_block(a.codes + row * a.ldc, a.scales, a.lds, row, col, live, y);
+  }
+}
+
+// A workgroup takes a block: sixteen lanes a row, sixteen rows at a time.
+template <int X>
+__global__ __launch_bounds__(256) void quantize_weight_kernel(QuantizeArgs a) {
+  __shared__ float part[4];
+  const int col = blockIdx.x * kBlock + (threadIdx.x & 15) * 8;
+  const int row0 = blockIdx.y * kBlock + (threadIdx.x >> 4);
+  float y[8][8] = {}, top = 0.f;
+#pragma unroll
+  for (int i = 0; i < 8; ++i) {
+    const int row = row0 + 16 * i;
+    if (row < a.n && col < a.cols) floats<X>(load8<X>(a.x + row * a.ldx * (X == kF32 ? 4 : 2), col), y[i]);
+    top = fmaxf(top, most8(y[i]));
+  }
+  top = max_groups(max16(top));
+  if ((threadIdx.x & 63) == 0) part[threadIdx.x >> 6] = top;
+  __syncthreads();
+  top = fmaxf(fmaxf(part[0], part[1]), fmaxf(part[2], part[3]));
+  const float scale = fmaxf(top, kLeast) / kLargest;
+  if (threadIdx.x == 0) a.scales[blockIdx.y * a.lds + blockIdx.x] = scale;
+#pragma unroll
+  for (int i = 0; i < 8; ++i) {
+    const int row = row0 + 16 * i;
+    if (row < a.n && col < a.cols)
+      *reinterpret_cast<uint2*>(a.codes + row * a.ldc + col) = codes8(y[i], 1.f / scale);
+  }
+}
+
+template <int T>
+using Type = std::integral_constant<int, T>;
+
+template <typename F>
+void by_float(int type, F f) {
+  if (type == kF32) f(Type<kF32>{});
+  else f(Type<kBf16>{});
+}
+
+template <int X, int R, int O>
+void launch_norm(const NormArgs& a, hipStream_t s) {
+  if (a.H <= 512) add_norm_kernel<X, R, O, 64, 1><<<(a.n + 3) / 4, 256, 0, s>>>(a);
+  else if (a.H <= 2048) add_norm_kernel<X, R, O, 256, 1><<<a.n, 256, 0, s>>>(a);
+  else if (a.H <= 4096) add_norm_kernel<X, R, O, 256, 2><<<a.n, 256, 0, s>>>(a);
+  else if (a.H <= 8192) add_norm_kernel<X, R, O, 256, 4><<<a.n, 256, 0, s>>>(a);
+  else add_norm_kernel<X, R, O, 256, 8><<<a.n, 256, 0, s>>>(a);
+}
+
+}  // namespace
+
+hipError_t launch_add_norm(const NormArgs& a, hipStream_t s) {
+  by_float(a.x_type, [&](auto x) {
+    const auto with = [&](auto r) {
+      constexpr int X = decltype(x)::value, R = decltype(r)::value;
+      if (a.out_type == kE4m3) launch_norm<X, R, kE4m3>(a, s);
+      else if (a.out_type == kF32) launch_norm<X, R, kF32>(a, s);
+      else launch_norm<X, R, kBf16>(a, s);
+    };
+    if (a.r_type == kNone) with(Type<kNone>{});
+    else by_float(a.r_type, with);
+  });
+  return hipGetLastError();
+}
+
+hipError_t launch_quantize(const QuantizeArgs& a, hipStream_t s) {
+  const int64_t groups = ((int64_t)a.n * ((a.cols + 511) / 512) + 3) / 4;
+  const unsigned grid = groups < 1 << 20 ? (unsigned)groups : 1 << 20;
+  by_float(a.x_type, [&](auto x) { quantize_kernel<decltype(x)::value><<<grid, 256, 0, s>>>(a); });
+  return hipGetLastError();
+}
+
+hipError_t launch_quantize_weight(const QuantizeArgs& a, hipStream_t s) {
+  const dim3 grid((a.cols + kBlock - 1) / kBlock, (a.n + kBlock - 1) / kBlock);
+  by_float(a.x_type, [&](auto x) { quantize_weight_kernel<decltype(x)::value><<<grid, 256, 0, s>>>(a); });
+  return hipGetLastError();
+}
+
+}  // namespace s2moe
