@@ -571,7 +571,7 @@ s2moe_status s2moe_quantize_weight(int32_t rows, int32_t cols, const void *w, in
 
 /* out[i][j] = sum_b x_scales[b][i] w_scales[j / 128][b] sum_{k in block b} x[i][k] w[j][k]
    for m rows of x and n rows of w, in fp32, rounded once to out's type (F32 or BF16).
-   x, w: codes; k a multiple of 16, at most 2^18, m, n <= 2^22.  x_scales [ceil(k / 128)]
+   x, w: codes; k a multiple of 16, at most 2^18, m, n <= 2^22, m n <= 2^34.  x_scales [ceil(k / 128)]
    [ldxs], ldxs >= m; w_scales [ceil(n / 128)][ldws], ldws >= ceil(k / 128).  out [m][n],
    16-byte aligned, ldo >= n (any: rows may begin anywhere an element may).  out must
    not overlap an input.  Sums are in a fixed order: equal calls give equal bits.

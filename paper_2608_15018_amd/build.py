@@ -29,7 +29,8 @@ HIPCC = shutil.which("hipcc") or "/opt/rocm/bin/hipcc"
 DEVICE_FLAGS = ["-Xclang", "-target-feature", "-Xclang", "-packed-fp32-ops"]
 # Kernels that read their matrix products with vector instructions in the same
 # step want those results in ordinary registers, not in accumulation registers.
-SOURCE_FLAGS = {"prompt_attention.hip": ["-mllvm", "-amdgpu-mfma-vgpr-form=1"]}
+SOURCE_FLAGS = {"prompt_attention.hip": ["-mllvm", "-amdgpu-mfma-vgpr-form=1"],
+                "matmul_e4m3.hip": ["-mllvm", "-amdgpu-mfma-vgpr-form=1"]}
 COMMON = ["-O3", "-std=c++17", "-fPIC", f"--offload-arch={ARCH}", "-I", INCLUDE, "-I", CSRC,
           "-Wall", "-Wno-unused-function"]
 

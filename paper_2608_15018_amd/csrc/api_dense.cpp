@@ -214,6 +214,8 @@ s2moe_status s2moe_scaled_matmul(int32_t m, int32_t n, int32_t k, const void* x,
   if (st == S2MOE_OK) st = check_count(fn, "n", n, 1, kMaxRows);
   if (st == S2MOE_OK) st = check_cols(fn, "k", k, kMaxCols);
   if (st != S2MOE_OK) return st;
+  if ((int64_t)m * n > (int64_t)1 << 34)
+    return fail(S2MOE_EUNSUPPORTED, "%s: m n = %d %d exceeds 2^34", fn, m, n);
   if (!is_float(out_dtype))
     return fail(S2MOE_EINVAL, "%s: out_dtype = %d must be F32 or BF16", fn, out_dtype);
   if (m == 0) return ok();

@@ -206,6 +206,41 @@ def test_products_of_small_whole_numbers_are_exact(m, n, k, out):
     assert torch.equal(s2.fp8_matmul(x, w, out_dtype=DT[out]).cpu(), torch.from_numpy(want).float().to(DT[out]))
 
 
+# Between them every form of the kernel for either type, whole tiles and a few tokens past them.
+LARGE = [(257, 512, 400), (384, 2048, 1040), (700, 2050, 1024), (768, 5120, 1040), (1024, 5121, 1024), (1536, 5120, 2064), (2048, 2048, 1024),
+         (257, 16400, 1024), (1025, 16384, 1040), (384, 32000, 1024), (2052, 6144, 2880), (90, 32000, 272), (33, 20000, 144), (16, 30001, 1168)]
+
+
+@pytest.mark.parametrize("out", ["bf16", "f32"])
+@pytest.mark.parametrize("m,n,k", LARGE)
+def test_large_products(m, n, k, out):
+    """Whole numbers exactly, everywhere; other codes at rows and columns drawn."""
+    g = gen(m + n + k)
+    whole = lambda *s: torch.randint(-2, 3, s, generator=g, device="cuda").float().to(DT["e4m3"])  # noqa: E731
+    size = lambda *s: torch.exp2(torch.randint(0, 3, s, generator=g, device="cuda").float())  # noqa: E731
+    kb = do.blocks_of(k)
+    x, w = s2.Fp8Rows(whole(m, k), size(kb, m)), s2.Fp8Weight(whole(n, k), size(do.blocks_of(n), kb))
+    a = x.codes.double() * x.scales.t().repeat_interleave(128, 1)[:, :k]
+    b = w.codes.double() * w.scales.repeat_interleave(128, 0)[:n].repeat_interleave(128, 1)[:, :k]
+    got = s2.fp8_matmul(x, w, out_dtype=DT[out])
+    assert torch.equal(got, (a @ b.t().contiguous()).float().to(DT[out]))
+    x, w = operands(m, n, k, g)
+    got = s2.fp8_matmul(x, w, out_dtype=DT[out])
+    assert torch.equal(got, s2.fp8_matmul(x, w, out_dtype=DT[out]))
+    rows = torch.cat([torch.randperm(m, generator=g, device="cuda")[:40], torch.tensor([0, m - 1], device="cuda")])
+    cols = torch.cat([torch.randperm(n, generator=g, device="cuda")[:128], torch.tensor([0, n - 1], device="cuda")])
+    part = np64(got[rows][:, cols])
+    xc, wc = np64(x.codes.float()[rows]), np64(w.codes.float()[cols])
+    xs = np64(x.scales[:, rows])
+    a, b = xc * do.spread_rows(xs, k), wc * np.repeat(np64(w.scales)[(cols // 128).cpu().numpy()], 128, axis=1)[:, :k]
+    want, mag = a @ b.T, np.abs(a) @ np.abs(b).T
+    slack = mag * (2 * 128 + 2 * kb + 16) * 2.0 ** -24
+    if out == "bf16":  # eight products cut off 13 bits below the largest's exponent, 2^-10 of their sum at most
+        slack = slack + mag * 2.0 ** -10
+    off = np.abs(part - want) - slack * (1 + HALF[out]) - np.abs(want) * (HALF[out] + 2.0 ** -24)
+    assert off.max() <= 0, (np.unravel_index(off.argmax(), off.shape), off.max())
+
+
 @pytest.mark.parametrize("out", ["bf16", "f32"])
 @pytest.mark.parametrize("m,n,k", [(5, 77, 272), (40, 129, 144), (200, 300, 400), (600, 520, 272)])
 def test_product_of_parts_of_larger_arrays(m, n, k, out):
