@@ -73,6 +73,13 @@ def _refuse(gpu, **tensors):
             raise _lib.S2moeError(_lib.EINVAL, f"{name} is on {t.device}, not on {where}")
 
 
+def _current(gpu):
+    """A launch goes to the current GPU, which has to be the cache's."""
+    if torch.cuda.current_device() != gpu:
+        raise _lib.S2moeError(_lib.EINVAL, f"the cache is on GPU {gpu}, the current one is "
+                                           f"GPU {torch.cuda.current_device()}")
+
+
 def _other(stream, device):
     """`stream` as torch's object, or None if it is the current one."""
     if _lib._stream(stream) == _lib._stream(None):
@@ -139,6 +146,7 @@ class KVCache:
         self._ref = ctypes.byref(self.struct)
         self._lib = _lib.load()
         self._lock = threading.Lock()  # the launches of an operation before another's
+        self._rotations = {}  # argument structs of append_rotated by what they hold
         self._status, self._copied = self.status.data_ptr(), self.copied.data_ptr()
         if fresh:
             self.clear()
@@ -194,6 +202,7 @@ class KVCache:
         g = self._gpu
         if not (g == seqs.get_device() == tok_off.get_device() == (g if parent is None else parent.get_device())):
             _refuse(g, seqs=seqs, tok_off=tok_off, **({} if parent is None else {"parent": parent}))
+        _current(g)
         if out is None:
             out = _result(seqs, (n_tokens,), None if stream is None else _other(stream, seqs.device))
         po_out = _ints(out, "out", n_tokens)
@@ -225,6 +234,7 @@ class KVCache:
         if not (g == q.get_device() == k.get_device() == v.get_device() == seqs.get_device()
                 == tok_off.get_device() == pos.get_device() == inv_freq.get_device()):
             _refuse(g, q=q, k=k, v=v, seqs=seqs, tok_off=tok_off, pos=pos, inv_freq=inv_freq)
+        _current(g)
         if out is None:
             out = _result(q, (t, Hq, D), None if stream is None else _other(stream, q.device))
             op, ldqo, to = out.data_ptr(), Hq * D, t
@@ -239,10 +249,15 @@ class KVCache:
                 _refuse(g, k_out=k_out)
         if not (tk == tv == to == tko == t):
             raise ValueError(f"q, k, v, out, k_out hold {t}, {tk}, {tv}, {to}, {tko} tokens")
-        r = _lib.Rotation(Hq, 2 * inv_freq.shape[0], int(neighbours), ldq, ldk, ldv, ldqo, ldko)
+        key = (Hq, 2 * inv_freq.shape[0], int(neighbours), ldq, ldk, ldv, ldqo, ldko)
+        r = self._rotations.get(key)  # of a model's layers all alike
+        if r is None:
+            r = ctypes.byref(_lib.Rotation(*key))
+            if len(self._rotations) < 64:
+                self._rotations[key] = r
         _lib._check(self._lib.s2moe_kv_append_rotated(
-            self._ref, layer, ctypes.byref(r), n, t, ps, po, pp, inv_freq.data_ptr(), qp, kp, vp,
-            op, kop, _lib._stream(stream)))
+            self._ref, layer, r, n, t, ps, po, pp, inv_freq.data_ptr(), qp, kp, vp, op, kop,
+            _lib._stream(stream)))
         return out
 
     def commit(self, seqs, path, n_accept, stream=None):

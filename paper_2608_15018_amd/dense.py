@@ -43,6 +43,8 @@ def _blocks(n):
     return (n + BLOCK - 1) // BLOCK
 
 
+# The checks are on every call's path to the GPU, which at the smallest sizes waits for
+# them: each property is read once, and results made here are not looked at.
 def _matrix(t, name, rows=None, cols=None):
     """(pointer, elements from one row to the next, rows, columns) of a matrix whose
     rows lie together."""
@@ -69,27 +71,42 @@ def _of(t, name, dtype):
         raise TypeError(f"{name}: expected {dtype}, got {t.dtype}")
 
 
-def _device(gpu, **tensors):
-    """Refuses tensors that are not on GPU `gpu`, and a GPU that is not the current one,
-    which the launch would go to."""
-    for name, t in tensors.items():
-        if t is not None and t.get_device() != gpu or gpu < 0:
-            _refuse(gpu, **{name: t})
-    if gpu != torch.cuda.current_device():
+def _handle(gpu, stream):
+    """The stream's handle.  A launch goes to the current GPU, which has to be the
+    tensors'."""
+    if torch.cuda.current_device() != gpu:
         raise _lib.S2moeError(_lib.EINVAL, f"the tensors are on GPU {gpu}, the current one is "
                                            f"GPU {torch.cuda.current_device()}")
+    return _lib._stream(stream)
 
 
-def _empty(like, stream, *wanted):
-    """Tensors of these (shape, dtype) for what `stream` writes, from its pool."""
-    other = None if stream is None else _other(stream, like.device)
+def _empty(like, stream, shape, dtype):
+    """A tensor for what `stream` writes, from its pool."""
+    if stream is None:
+        return like.new_empty(shape, dtype=dtype)
+    other = _other(stream, like.device)
     if other is None:
-        return [like.new_empty(s, dtype=d) for s, d in wanted]
+        return like.new_empty(shape, dtype=dtype)
     with torch.cuda.stream(other):
-        out = [like.new_empty(s, dtype=d) for s, d in wanted]
-    for t in out:
-        t.record_stream(torch.cuda.current_stream())
+        out = like.new_empty(shape, dtype=dtype)
+    out.record_stream(torch.cuda.current_stream())
     return out
+
+
+def _rows_out(out, like, n, cols, gpu, stream):
+    """(Fp8Rows, pointer and stride of its codes, of its scales); made if out is None."""
+    kb = (cols + BLOCK - 1) // BLOCK
+    if out is None:
+        codes, scales = _empty(like, stream, (n, cols), E4M3), _empty(like, stream, (kb, n), _F32)
+        return Fp8Rows(codes, scales), codes.data_ptr(), cols, scales.data_ptr(), n
+    codes, scales = out
+    _of(codes, "codes", E4M3)
+    _of(scales, "scales", _F32)
+    cp, ldc, _, _ = _matrix(codes, "codes", n, cols)
+    sp, lds, _, _ = _matrix(scales, "scales", kb, n)
+    if not gpu == codes.get_device() == scales.get_device():
+        _refuse(gpu, codes=codes, scales=scales)
+    return out, cp, ldc, sp, lds if lds > n else n
 
 
 def add_norm(x, weight, residual=None, eps: float = 1e-6, out=None, out_dtype=None, stream=None):
@@ -105,30 +122,32 @@ def add_norm(x, weight, residual=None, eps: float = 1e-6, out=None, out_dtype=No
         out_dtype = given
     dt = x.dtype if out_dtype is None else out_dtype
     xc, wc, oc = _float(x, "x"), _float(weight, "weight"), _CODES.get(dt)
-    if oc is None:
-        raise TypeError(f"out_dtype: expected float32, bfloat16 or float8_e4m3fn, got {dt}")
+    if oc is None or (oc == _lib.E4M3 and isinstance(out, torch.Tensor)):
+        raise TypeError(f"out: expected float32, bfloat16 or Fp8Rows, got {dt}")
     if weight.dim() != 1 or weight.shape[0] != H or not weight.is_contiguous():
         raise ValueError(f"weight: expected contiguous [{H}], got {tuple(weight.shape)}")
+    gpu = x.get_device()
+    if gpu < 0 or weight.get_device() != gpu:
+        _refuse(gpu, x=x, weight=weight)
     rp, ldr, rc = None, 0, 0
     if residual is not None:
         rc = _float(residual, "residual")
         rp, ldr, _, _ = _matrix(residual, "residual", n, H)
-    eight = oc == _lib.E4M3
-    _device(x.get_device(), x=x, weight=weight, residual=residual)
-    if out is None:
-        out = _empty(x, stream, ((n, H), dt), *([((_blocks(H), n), _F32)] if eight else []))
-        out = Fp8Rows(*out) if eight else out[0]
-    main, scales = out if eight else (out, None)
-    _of(main, "out", dt)
-    op, ldo, _, _ = _matrix(main, "out", n, H)
-    sp, lds = None, 0
-    if eight:
-        _of(scales, "scales", _F32)
-        sp, lds, _, _ = _matrix(scales, "scales", _blocks(H), n)
-        lds = max(lds, n)
-    _device(x.get_device(), out=main, scales=scales)
+        if residual.get_device() != gpu:
+            _refuse(gpu, residual=residual)
+    handle = _handle(gpu, stream)
+    if oc == _lib.E4M3:
+        out, op, ldo, sp, lds = _rows_out(out, x, n, H, gpu, stream)
+    elif out is None:
+        out, ldo, sp, lds = _empty(x, stream, (n, H), dt), H, None, 0
+        op = out.data_ptr()
+    else:
+        op, ldo, _, _ = _matrix(out, "out", n, H)
+        sp, lds = None, 0
+        if out.get_device() != gpu:
+            _refuse(gpu, out=out)
     _lib._check(_lib.load().s2moe_add_norm(n, H, xp, ldx, xc, rp, ldr, rc, weight.data_ptr(), wc,
-                                           eps, op, ldo, oc, sp, lds, _lib._stream(stream)))
+                                           eps, op, ldo, oc, sp, lds, handle))
     return out
 
 
@@ -136,17 +155,12 @@ def quantize(x, out=None, stream=None) -> Fp8Rows:
     """Rows x [n, cols] (float32 or bfloat16) in 8 bits."""
     xc = _float(x, "x")
     xp, ldx, n, K = _matrix(x, "x")
-    _device(x.get_device(), x=x)
-    if out is None:
-        out = Fp8Rows(*_empty(x, stream, ((n, K), E4M3), ((_blocks(K), n), _F32)))
-    codes, scales = out
-    _of(codes, "codes", E4M3)
-    _of(scales, "scales", _F32)
-    cp, ldc, _, _ = _matrix(codes, "codes", n, K)
-    sp, lds, _, _ = _matrix(scales, "scales", _blocks(K), n)
-    _device(x.get_device(), codes=codes, scales=scales)
-    _lib._check(_lib.load().s2moe_quantize(n, K, xp, ldx, xc, cp, ldc, sp, max(lds, n),
-                                           _lib._stream(stream)))
+    gpu = x.get_device()
+    if gpu < 0:
+        _refuse(gpu, x=x)
+    handle = _handle(gpu, stream)
+    out, cp, ldc, sp, lds = _rows_out(out, x, n, K, gpu, stream)
+    _lib._check(_lib.load().s2moe_quantize(n, K, xp, ldx, xc, cp, ldc, sp, lds, handle))
     return out
 
 
@@ -154,12 +168,14 @@ def quantize_weight(w, stream=None) -> Fp8Weight:
     """Weights w [n, k] (float32 or bfloat16) in 8 bits, once at model load."""
     wc = _float(w, "w")
     wp, ldw, n, K = _matrix(w, "w")
-    _device(w.get_device(), w=w)
-    codes, scales = _empty(w, stream, ((n, K), E4M3), ((_blocks(n), _blocks(K)), _F32))
-    _lib._check(_lib.load().s2moe_quantize_weight(n, K, wp, ldw, wc, codes.data_ptr(), K,
-                                                  scales.data_ptr(), _blocks(K),
-                                                  _lib._stream(stream)))
-    return Fp8Weight(codes, scales)
+    gpu, nb, kb = w.get_device(), _blocks(n), _blocks(K)
+    if gpu < 0:
+        _refuse(gpu, w=w)
+    handle = _handle(gpu, stream)
+    out = Fp8Weight(_empty(w, stream, (n, K), E4M3), _empty(w, stream, (nb, kb), _F32))
+    _lib._check(_lib.load().s2moe_quantize_weight(n, K, wp, ldw, wc, out.codes.data_ptr(), K,
+                                                  out.scales.data_ptr(), kb, handle))
+    return out
 
 
 def fp8_matmul(x: Fp8Rows, w: Fp8Weight, out=None, out_dtype=None, stream=None):
@@ -173,20 +189,28 @@ def fp8_matmul(x: Fp8Rows, w: Fp8Weight, out=None, out_dtype=None, stream=None):
     _of(ws, "w.scales", _F32)
     xp, ldx, m, K = _matrix(xc, "x.codes")
     wp, ldw, n, _ = _matrix(wc, "w.codes", None, K)
-    kb = _blocks(K)
+    kb = (K + BLOCK - 1) // BLOCK
     xsp, ldxs, _, _ = _matrix(xs, "x.scales", kb, m)
-    wsp, ldws, _, _ = _matrix(ws, "w.scales", _blocks(n), kb)
+    wsp, ldws, _, _ = _matrix(ws, "w.scales", (n + BLOCK - 1) // BLOCK, kb)
     gpu = xc.get_device()
-    _device(gpu, x=xc, x_scales=xs, w=wc, w_scales=ws, out=out)
+    if gpu < 0 or not gpu == xs.get_device() == wc.get_device() == ws.get_device():
+        _refuse(gpu, x=xc, x_scales=xs, w=wc, w_scales=ws)
+    handle = _handle(gpu, stream)
     if out is None:
         dt = torch.bfloat16 if out_dtype is None else out_dtype
-        if dt not in (torch.bfloat16, _F32):
+        oc = _CODES.get(dt)
+        if oc is None or oc == _lib.E4M3:
             raise TypeError(f"out_dtype: expected torch.float32 or torch.bfloat16, got {dt}")
-        out = _empty(xc, stream, ((m, n), dt))[0]
-    elif out_dtype is not None and out.dtype is not out_dtype:
-        raise TypeError(f"out is {out.dtype}, out_dtype {out_dtype}")
-    oc = _float(out, "out")
-    op, ldo, _, _ = _matrix(out, "out", m, n)
-    _lib._check(_lib.load().s2moe_scaled_matmul(m, n, K, xp, ldx, xsp, max(ldxs, m), wp, ldw, wsp,
-                                                max(ldws, kb), op, ldo, oc, _lib._stream(stream)))
+        out, ldo = _empty(xc, stream, (m, n), dt), n
+        op = out.data_ptr()
+    else:
+        if out_dtype is not None and out.dtype is not out_dtype:
+            raise TypeError(f"out is {out.dtype}, out_dtype {out_dtype}")
+        oc = _float(out, "out")
+        op, ldo, _, _ = _matrix(out, "out", m, n)
+        if out.get_device() != gpu:
+            _refuse(gpu, out=out)
+    _lib._check(_lib.load().s2moe_scaled_matmul(m, n, K, xp, ldx, xsp, ldxs if ldxs > m else m, wp,
+                                                ldw, wsp, ldws if ldws > kb else kb, op, ldo, oc,
+                                                handle))
     return out
