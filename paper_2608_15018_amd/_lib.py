@@ -224,6 +224,17 @@ def _stream(stream) -> int:
     return int(stream)
 
 
+def _stream_on(gpu: int, stream, what: str) -> int:
+    """The handle of `stream`, for a launch on GPU `gpu`, which has to be the current one:
+    a launch goes there."""
+    now = torch.cuda.current_device()
+    if now != gpu:
+        raise S2moeError(EINVAL, f"{what} on GPU {gpu}, the current one is GPU {now}")
+    if stream is None and _raw_stream is not None:
+        return _raw_stream(gpu)
+    return _stream(stream)
+
+
 class Routing:
     """Device buffers of the routing state of one verify batch."""
 

@@ -73,13 +73,6 @@ def _refuse(gpu, **tensors):
             raise _lib.S2moeError(_lib.EINVAL, f"{name} is on {t.device}, not on {where}")
 
 
-def _current(gpu):
-    """A launch goes to the current GPU, which has to be the cache's."""
-    if torch.cuda.current_device() != gpu:
-        raise _lib.S2moeError(_lib.EINVAL, f"the cache is on GPU {gpu}, the current one is "
-                                           f"GPU {torch.cuda.current_device()}")
-
-
 def _other(stream, device):
     """`stream` as torch's object, or None if it is the current one."""
     if _lib._stream(stream) == _lib._stream(None):
@@ -202,14 +195,14 @@ class KVCache:
         g = self._gpu
         if not (g == seqs.get_device() == tok_off.get_device() == (g if parent is None else parent.get_device())):
             _refuse(g, seqs=seqs, tok_off=tok_off, **({} if parent is None else {"parent": parent}))
-        _current(g)
+        handle = _lib._stream_on(g, stream, "the cache is")
         if out is None:
             out = _result(seqs, (n_tokens,), None if stream is None else _other(stream, seqs.device))
         po_out = _ints(out, "out", n_tokens)
         if out.get_device() != g:
             _refuse(g, out=out)
         _lib._check(self._lib.s2moe_kv_positions(self._ref, n, n_tokens, ps, po, pp, po_out,
-                                                 _lib._stream(stream)))
+                                                 handle))
         return out
 
     def append_rotated(self, layer: int, q, k, v, seqs, tok_off, pos, inv_freq,
@@ -234,7 +227,7 @@ class KVCache:
         if not (g == q.get_device() == k.get_device() == v.get_device() == seqs.get_device()
                 == tok_off.get_device() == pos.get_device() == inv_freq.get_device()):
             _refuse(g, q=q, k=k, v=v, seqs=seqs, tok_off=tok_off, pos=pos, inv_freq=inv_freq)
-        _current(g)
+        handle = _lib._stream_on(g, stream, "the cache is")
         if out is None:
             out = _result(q, (t, Hq, D), None if stream is None else _other(stream, q.device))
             op, ldqo, to = out.data_ptr(), Hq * D, t
@@ -257,7 +250,7 @@ class KVCache:
                 self._rotations[key] = r
         _lib._check(self._lib.s2moe_kv_append_rotated(
             self._ref, layer, r, n, t, ps, po, pp, inv_freq.data_ptr(), qp, kp, vp, op, kop,
-            _lib._stream(stream)))
+            handle))
         return out
 
     def commit(self, seqs, path, n_accept, stream=None):

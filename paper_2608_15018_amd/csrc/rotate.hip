@@ -5,6 +5,11 @@
 // by p f_j:  a' = a cos - b sin, b' = b cos + a sin.  The turn is p f_j / 2 pi in 64 bits,
 // whose whole part is dropped before it is rounded to 32, so that far positions keep
 // their angle; sine, cosine and the products are fp32, and each element is rounded once.
+//
+// Bound: memory for prompts (17000 tokens, 32 query heads, 4 of keys and values, 128
+// wide: 68 us, 5.1 TB/s, what a large copy reaches), latency for a step's few tokens (4.5
+// us).  Angles are worked out from the frequencies, a token's pairs by as many lanes, and
+// shared through LDS: a table of them would have to be read.
 #include <type_traits>
 
 #include "attention.h"
@@ -21,6 +26,7 @@ __device__ __forceinline__ void rows_of(const int32_t* tok_off, int i, int n_tok
   *end = min(max(tok_off[i + 1], *begin), n_tokens);
 }
 
+// Latency is all it costs: 2.2 us, with parents 2.6 to 4 (trees of up to 64 nodes).
 // blockIdx.x a request.  Without parents blockIdx.y strides over its tokens.  With them
 // 256 nodes are looked at at a time: `up` is each node's nearest ancestor that is not
 // counted yet, and every step passes twice as many of them.
@@ -129,13 +135,13 @@ __device__ __forceinline__ float2 cos_sin(int pos, float freq) {
   return float2{c, s};
 }
 
-// blockIdx.y below `kv_parts`: new tokens' keys and values, as the append of the cache
-// does it, for every kv_parts-th kv head.  A wave has TW tokens; the first token of a
-// request and every token whose slot begins a group of eight write their group's.  The
-// angles of a group are worked out once for all its heads.  blockIdx.y from `kv_parts` on:
-// the queries, a token a wave, one part of its heads.
+// The first workgroups: new tokens' keys and values, as the append of the cache does it, for
+// every kv_parts-th kv head.  A wave has TW tokens.  With more than one the first token of a
+// request and every token whose slot begins a group of eight write their group's; one goes
+// alone.  The angles of a group are worked out once for all the wave's heads.  The others: the queries, a wave one token and
+// every q_parts-th load of its heads.
 template <typename E, int D, int TW>
-__global__ __launch_bounds__(256) void append_rotated_kernel(KvCache c, RotateArgs a, int kv_parts, int q_parts) {
+__global__ __launch_bounds__(256) void append_rotated_kernel(KvCache c, RotateArgs a, int kv_blocks, int kv_parts, int q_parts) {
   constexpr int N = kPer<E>, kPieces = D / N, kDuos = kPieces / 2, VD = D / 64;
   typedef E E8 __attribute__((ext_vector_type(8)));
   typedef E EV __attribute__((ext_vector_type(VD)));
@@ -144,31 +150,43 @@ __global__ __launch_bounds__(256) void append_rotated_kernel(KvCache c, RotateAr
   const int lane = threadIdx.x & 63, wave = wave_id(), half = a.rot / 2, turned = half / N;
   const bool neighbours = a.neighbours;
   float2(*const cs)[kPairs + 2] = cs_s[wave];
-  if ((int)blockIdx.y >= kv_parts) {
+  if ((int)blockIdx.x >= kv_blocks) {
+    const int block = blockIdx.x - kv_blocks, part = block % q_parts, t = block / q_parts * 4 + wave;
     const int first = max(a.tok_off[0], 0), last = min(a.tok_off[a.n], a.n_tokens);
-    const int duo = lane % kDuos, part = blockIdx.y - kv_parts;
+    if (t < first || t >= last) return;
+    constexpr int kHeads = 64 / kDuos, kAtOnce = 4;  // of a load
+    const int duo = lane % kDuos, h0 = part * kHeads + lane / kDuos, step = q_parts * kHeads;
     const int2 at = pieces_of<E>(duo, a.rot, neighbours);
-#pragma unroll 1
-    for (int x = 0; x < TW; ++x) {
-      const int t = (blockIdx.x * 4 + wave) * TW + x;
-      if (t < first || t >= last) continue;
-      if (lane < half) cs[0][lane] = cos_sin(a.pos[t], a.freq[lane]);
-      __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
-      __builtin_amdgcn_wave_barrier();
-      const u32x4* q = reinterpret_cast<const u32x4*>(reinterpret_cast<const E*>(a.q) + t * a.ldq);
-      u32x4* to = reinterpret_cast<u32x4*>(reinterpret_cast<E*>(a.q_out) + t * a.ldqo);
-#pragma unroll 4
-      for (int h = part * (64 / kDuos) + lane / kDuos; h < a.Hq; h += q_parts * (64 / kDuos)) {
-        u32x4 u = q[h * kPieces + at.x], v = q[h * kPieces + at.y];
-        if (duo < turned) turn<E>(u, v, cs[0] + duo * N, neighbours);
-        to[h * kPieces + at.x] = u;
-        to[h * kPieces + at.y] = v;
+    const u32x4* q = reinterpret_cast<const u32x4*>(reinterpret_cast<const E*>(a.q) + t * a.ldq);
+    u32x4* to = reinterpret_cast<u32x4*>(reinterpret_cast<E*>(a.q_out) + t * a.ldqo);
+    u32x4 u[kAtOnce], v[kAtOnce];
+    const auto load = [&](int h) {
+#pragma unroll
+      for (int i = 0; i < kAtOnce; ++i) {
+        const int g = min(h + i * step, a.Hq - 1);
+        u[i] = q[g * kPieces + at.x];
+        v[i] = q[g * kPieces + at.y];
       }
-      __builtin_amdgcn_wave_barrier();
+    };
+    load(h0);
+    if (lane < half) cs[0][lane] = cos_sin(a.pos[t], a.freq[lane]);
+    __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+    __builtin_amdgcn_wave_barrier();
+    for (int h = h0; h < a.Hq; h += kAtOnce * step) {
+      if (h != h0) load(h);
+#pragma unroll
+      for (int i = 0; i < kAtOnce; ++i) {
+        if (duo < turned) turn<E>(u[i], v[i], cs[0] + duo * N, neighbours);
+        if (h + i * step < a.Hq) {
+          to[(h + i * step) * kPieces + at.x] = u[i];
+          to[(h + i * step) * kPieces + at.y] = v[i];
+        }
+      }
     }
     return;
   }
-  const int t0 = (blockIdx.x * 4 + wave) * TW;
+  const int kv_part = blockIdx.x % kv_parts;
+  const int t0 = (blockIdx.x / kv_parts * 4 + wave) * TW;
   // Requests that begin at or before each token; lane x goes on with token t0 + x.
   int began[TW] = {}, i = -1;
   for (int i0 = 0; i0 < a.n; i0 += 64) {
@@ -185,9 +203,9 @@ __global__ __launch_bounds__(256) void append_rotated_kernel(KvCache c, RotateAr
     if (mine >= begin && mine < end) {
       const bool known = in_range(s, c.max_seqs);
       const int64_t at = (int64_t)(known ? c.length[s] : 0) + mine - begin, nth = at >> c.log_p;
-      if (mine == begin || (at & 7) == 0) {
+      if (TW == 1 || mine == begin || (at & 7) == 0) {
         slot = (int)(at & (c.P - 1));
-        count = min(8 - (slot & 7), end - mine);
+        count = TW == 1 ? 1 : min(8 - (slot & 7), end - mine);
         if (known && at >= 0 && nth < c.max_pages) {
           const int p = c.table[(int64_t)s * c.max_pages + nth];
           if (in_range(p, c.n_pages) && c.refs[p] == 1) page = p;
@@ -205,7 +223,7 @@ __global__ __launch_bounds__(256) void append_rotated_kernel(KvCache c, RotateAr
     }
     __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
     __builtin_amdgcn_wave_barrier();
-    for (int h = blockIdx.y; h < c.Hkv; h += kv_parts) {
+    for (int h = kv_part; h < c.Hkv; h += kv_parts) {
       const int64_t head = a.layer * c.layer_bytes() + to * c.page_bytes() + h * c.head_bytes();
       u32x4* const kt = reinterpret_cast<u32x4*>(c.k + head) + at * kPieces;
 #pragma unroll
@@ -255,12 +273,18 @@ __global__ __launch_bounds__(256) void append_rotated_kernel(KvCache c, RotateAr
 template <typename E, int D>
 void launch_rotated(const KvCache& c, const RotateArgs& a, hipStream_t s) {
   constexpr int kHeads = 64 / (D / kPer<E> / 2);  // of a query load
-  const bool few = a.n_tokens / a.n < 8;
-  const int per = few ? 4 : 32;
-  const int kv_parts = c.Hkv, q_parts = few ? (a.Hq + kHeads - 1) / kHeads : 1;
-  const dim3 grid((a.n_tokens + per - 1) / per, kv_parts + q_parts);
-  if (few) append_rotated_kernel<E, D, 1><<<grid, 256, 0, s>>>(c, a, kv_parts, q_parts);
-  else append_rotated_kernel<E, D, 8><<<grid, 256, 0, s>>>(c, a, kv_parts, q_parts);
+  // Few tokens go alone, a wave each and kv head; groups of eight share angles and write
+  // their values whole.  us alone / in groups, 32 heads over 8 of 128: 8 requests of 8 4.4 / 9.1,
+  // 32 of 16 7.0 / 9.9, 300 of 4 15.8 / 15.6, 64 of 16 12.4 / 11.6, 8 of 512 34 / 23.
+  const bool few = a.n_tokens < 1200;
+  const int most = (a.Hq + kHeads - 1) / kHeads;
+  // With waves enough, two kv heads a wave and half of the query heads: 17000 tokens take
+  // 85 us so, 93 with a kv head each, 101 with all in one, 98 with a quarter of the queries.
+  const int kv_parts = a.n_tokens < 4096 ? c.Hkv : (c.Hkv + 1) / 2, q_parts = few ? most : most < 2 ? most : 2;
+  const int per = few ? 4 : 32, kv_blocks = (a.n_tokens + per - 1) / per * kv_parts;
+  const int grid = kv_blocks + (a.n_tokens + 3) / 4 * q_parts;
+  if (few) append_rotated_kernel<E, D, 1><<<grid, 256, 0, s>>>(c, a, kv_blocks, kv_parts, q_parts);
+  else append_rotated_kernel<E, D, 8><<<grid, 256, 0, s>>>(c, a, kv_blocks, kv_parts, q_parts);
 }
 
 }  // namespace

@@ -71,15 +71,6 @@ def _of(t, name, dtype):
         raise TypeError(f"{name}: expected {dtype}, got {t.dtype}")
 
 
-def _handle(gpu, stream):
-    """The stream's handle.  A launch goes to the current GPU, which has to be the
-    tensors'."""
-    if torch.cuda.current_device() != gpu:
-        raise _lib.S2moeError(_lib.EINVAL, f"the tensors are on GPU {gpu}, the current one is "
-                                           f"GPU {torch.cuda.current_device()}")
-    return _lib._stream(stream)
-
-
 def _empty(like, stream, shape, dtype):
     """A tensor for what `stream` writes, from its pool."""
     if stream is None:
@@ -135,7 +126,7 @@ def add_norm(x, weight, residual=None, eps: float = 1e-6, out=None, out_dtype=No
         rp, ldr, _, _ = _matrix(residual, "residual", n, H)
         if residual.get_device() != gpu:
             _refuse(gpu, residual=residual)
-    handle = _handle(gpu, stream)
+    handle = _lib._stream_on(gpu, stream, "the tensors are")
     if oc == _lib.E4M3:
         out, op, ldo, sp, lds = _rows_out(out, x, n, H, gpu, stream)
     elif out is None:
@@ -158,7 +149,7 @@ def quantize(x, out=None, stream=None) -> Fp8Rows:
     gpu = x.get_device()
     if gpu < 0:
         _refuse(gpu, x=x)
-    handle = _handle(gpu, stream)
+    handle = _lib._stream_on(gpu, stream, "the tensors are")
     out, cp, ldc, sp, lds = _rows_out(out, x, n, K, gpu, stream)
     _lib._check(_lib.load().s2moe_quantize(n, K, xp, ldx, xc, cp, ldc, sp, lds, handle))
     return out
@@ -171,7 +162,7 @@ def quantize_weight(w, stream=None) -> Fp8Weight:
     gpu, nb, kb = w.get_device(), _blocks(n), _blocks(K)
     if gpu < 0:
         _refuse(gpu, w=w)
-    handle = _handle(gpu, stream)
+    handle = _lib._stream_on(gpu, stream, "the tensors are")
     out = Fp8Weight(_empty(w, stream, (n, K), E4M3), _empty(w, stream, (nb, kb), _F32))
     _lib._check(_lib.load().s2moe_quantize_weight(n, K, wp, ldw, wc, out.codes.data_ptr(), K,
                                                   out.scales.data_ptr(), kb, handle))
@@ -195,7 +186,7 @@ def fp8_matmul(x: Fp8Rows, w: Fp8Weight, out=None, out_dtype=None, stream=None):
     gpu = xc.get_device()
     if gpu < 0 or not gpu == xs.get_device() == wc.get_device() == ws.get_device():
         _refuse(gpu, x=xc, x_scales=xs, w=wc, w_scales=ws)
-    handle = _handle(gpu, stream)
+    handle = _lib._stream_on(gpu, stream, "the tensors are")
     if out is None:
         dt = torch.bfloat16 if out_dtype is None else out_dtype
         oc = _CODES.get(dt)

@@ -47,6 +47,7 @@ def lib(monkeypatch):
     r = Recorder()
     monkeypatch.setattr(_lib, "load", lambda: r)
     monkeypatch.setattr(_lib, "_stream", lambda s: 11 if s is None else int(s))
+    monkeypatch.setattr(_lib, "_raw_stream", None)
     monkeypatch.setattr(torch.cuda, "current_device", lambda: 0)
     return r
 
