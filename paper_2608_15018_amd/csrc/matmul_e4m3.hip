@@ -134,11 +134,162 @@ __device__ __forceinline__ void store_tile(const MatmulArgs& a, int my_n, int my
   }
 }
 
-// Up to 16 tokens a tile: the weights' way from memory is what takes time.  A workgroup has
-// 16 TN weight rows; its waves take the blocks of k in turn, so that together they read
-// stretches of the rows, straight into registers, and their sums are added in the waves'
-// order.  Workgroups begin at different blocks: rows that lie 4096 bytes apart, read in
-// step, would come from few of the memory's channels.
+// The same by way of LDS, a stretch of whole rows at a time: results lie 32 bytes of a row to
+// 16 rows in the lanes, and stored so they would take 32 us of 202 at 8192 x 6144 x 4096.
+// `scratch`: the wave's own kScratch<..> bytes, which nothing else uses any more.
+template <int TN, int TM, bool kF32Out>
+constexpr int kScratch = 16 * TM * (16 * TN * (kF32Out ? 4 : 2) + 16);
+template <int TN, int TM, bool kF32Out>
+__device__ __forceinline__ void store_rows(const MatmulArgs& a, int my_n, int my_m, int quarter, int at, const f32x4 (&sum)[TN][TM],
+                                           char* scratch) {
+  constexpr int elt = kF32Out ? 4 : 2, kRow = 16 * TN * elt, kStep = kRow + 16, kPieces = kRow / 16, kAtOnce = 64 / kPieces;
+  if (kAtOnce > 16 * TM || a.ldo * elt % 16 != 0 || my_n + 16 * TN > a.n) {
+    store_tile<TN, TM, kF32Out>(a, my_n, my_m, quarter, at, sum);
+    return;
+  }
+#pragma unroll
+  for (int t = 0; t < TM; ++t)
+#pragma unroll
+    for (int i = 0; i < TN; ++i) {
+      char* const p = scratch + (16 * t + at) * kStep + (16 * i + 4 * quarter) * elt;
+      if constexpr (kF32Out) {
+        *reinterpret_cast<f32x4*>(p) = sum[i][t];
+      } else {
+        const bf16x2 lo = pack2(sum[i][t][0], sum[i][t][1]), hi = pack2(sum[i][t][2], sum[i][t][3]);
+        *reinterpret_cast<bf16x4*>(p) = bf16x4{lo[0], lo[1], hi[0], hi[1]};
+      }
+    }
+  __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+  __builtin_amdgcn_wave_barrier();
+  const int lane = 16 * quarter + at, piece = lane % kPieces;
+#pragma unroll
+  for (int r0 = 0; r0 < 16 * TM; r0 += kAtOnce) {
+    const int r = r0 + lane / kPieces, to = my_m + r;
+    const u32x4 v = *reinterpret_cast<const u32x4*>(scratch + r * kStep + piece * 16);
+    if (to < a.m) *reinterpret_cast<u32x4*>(a.out + (to * a.ldo + my_n) * elt + piece * 16) = v;
+  }
+}
+
+// Up to 32 tokens a tile and weights that do not fill the chip so long: how soon they come is
+// what takes time.  A workgroup has 16 TN weight rows and 16 TM tokens; its waves take the
+// blocks of k in turn, kAhead of them on their way to LDS at any time, each to the wave's own
+// places, so that no wave waits for another before the sums are added, in the waves' order.
+// Eight lanes read 128 bytes of a row, four times the lines a load that the operands'
+// layout would have (16 x 6144 x 4096: 7.2 us, 9.2 with loads straight to registers).
+// Workgroups begin at different blocks: rows that lie 4096 bytes apart, read in step, would
+// come from few of the memory's channels.
+template <int TN, int TM, int kAhead, int kWaves, bool kF32Out>
+__global__ __launch_bounds__(64 * kWaves) void stream_kernel(MatmulArgs a, int tiles_n, int tiles_m) {
+  constexpr int kRows = 16 * (TN + TM), kLoads = 2 * (TN + TM) + 1, kStage = kRows * kBlock + 256;
+  extern __shared__ __attribute__((aligned(1024))) char lds[];
+  const int lane = threadIdx.x & 63, wave = wave_id(), quarter = lane >> 4, at = lane & 15;
+  int tn, tm;
+  if (!tile_of(tiles_n, tiles_m, &tn, &tm)) return;
+  const int n0 = tn * 16 * TN, m0 = tm * 16 * TM;
+  const int steps = (a.k + kBlock - 1) / kBlock, rest = a.k - (steps - 1) * kBlock;
+  const int piece = (lane & 7) ^ (lane >> 3);
+  uint32_t woff[2 * TN], xoff[2 * TM];
+#pragma unroll
+  for (int i = 0; i < 2 * TN; ++i) woff[i] = (uint32_t)min(8 * i + (lane >> 3), a.n - 1 - n0) * (uint32_t)a.ldw + piece * 16;
+#pragma unroll
+  for (int i = 0; i < 2 * TM; ++i) xoff[i] = (uint32_t)min(8 * i + (lane >> 3), a.m - 1 - m0) * (uint32_t)a.ldx + piece * 16;
+  const uint32_t mine = 4u * min(m0 + (lane & (16 * TM - 1)), a.m - 1);
+  const char* const wbase = reinterpret_cast<const char*>(a.w) + n0 * a.ldw;
+  const char* const xbase = reinterpret_cast<const char*>(a.x) + m0 * a.ldx;
+  const float* const ws = a.ws + n0 / kBlock * a.ldws;
+  const int count = wave < steps ? (steps - 1 - wave) / kWaves + 1 : 0;
+  const int turn = count > 0 ? tn % count : 0;
+  const auto block_of = [&](int i) {
+    int j = i + turn;
+    if (j >= count) j -= count;
+    return wave + j * kWaves;
+  };
+  char* const mylds = lds + wave * kAhead * kStage;
+  const uint32_t at0 = lds_address(mylds);
+  float wscale = 0.f;
+  // Block i of the wave's; past its last the last one again.
+  const auto load = [&](int i, int slot) {
+    const int b = block_of(min(i, count - 1));
+    const uint32_t st = at0 + slot * kStage;
+    const uint32_t back = b == steps - 1 && piece * 16 >= rest ? (uint32_t)(piece * 16 - rest + 16) : 0u;
+#pragma unroll
+    for (int l = 0; l < 2 * TN; ++l) load16(wbase + b * kBlock, woff[l] - back, st + l * 1024);
+#pragma unroll
+    for (int l = 0; l < 2 * TM; ++l) load16(xbase + b * kBlock, xoff[l] - back, st + (2 * TN + l) * 1024);
+    load4(reinterpret_cast<const char*>(a.xs + b * a.ldxs), mine, st + kRows * kBlock);
+  };
+  const int lo = at * kBlock + ((quarter ^ (at & 7)) * 16), hi = lo ^ 64;
+  f32x4 sum[TN][TM] = {};
+  if (count > 0) {
+    wscale = ws[block_of(min(lane, count - 1))];
+    arrived(wscale);
+#pragma unroll
+    for (int i = 0; i < kAhead; ++i) load(i, i);
+    int slot = 0;
+    for (int i = 0; i < count; ++i) {
+      if ((i & 63) == 0 && i > 0) {
+        wscale = ws[block_of(min(i + lane, count - 1))];
+        arrived(wscale);
+      }
+      wait_loads<(kAhead - 1) * kLoads>();
+      const int b = block_of(i);
+      const char* const stage = mylds + slot * kStage;
+      const bool last = b == steps - 1 && rest < kBlock;
+      const auto operand = [&](int row) {
+        const char* const p = stage + row * kBlock;
+        return join(*reinterpret_cast<const u32x4*>(p + lo), *reinterpret_cast<const u32x4*>(p + hi));
+      };
+      i32x8 wb[TN], xb[TM];
+      float f[TM];
+      const float g = __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(wscale), i & 63));
+#pragma unroll
+      for (int t = 0; t < TM; ++t) {
+        xb[t] = operand(16 * (TN + t));
+        f[t] = reinterpret_cast<const float*>(stage + kRows * kBlock)[16 * t + at] * g;
+      }
+#pragma unroll
+      for (int n = 0; n < TN; ++n) wb[n] = operand(16 * n);
+      wait_lds();  // this block's place takes a later one
+      load(i + kAhead, slot);
+      slot = slot == kAhead - 1 ? 0 : slot + 1;
+      if (last) {
+#pragma unroll
+        for (int n = 0; n < TN; ++n) wb[n] = cut_off(wb[n], quarter, rest);
+#pragma unroll
+        for (int t = 0; t < TM; ++t) xb[t] = cut_off(xb[t], quarter, rest);
+      }
+#pragma unroll
+      for (int n = 0; n < TN; ++n)
+#pragma unroll
+        for (int t = 0; t < TM; ++t) {
+          const f32x4 y = mma<kF32Out>(wb[n], xb[t]);
+#pragma unroll
+          for (int e = 0; e < 4; ++e) sum[n][t][e] = fmaf(y[e], f[t], sum[n][t][e]);
+        }
+    }
+    wait_loads<0>();
+  }
+  __syncthreads();  // the blocks' places become the sums'
+  f32x4* const part = reinterpret_cast<f32x4*>(lds);
+#pragma unroll
+  for (int n = 0; n < TN; ++n)
+#pragma unroll
+    for (int t = 0; t < TM; ++t) part[(wave * TN * TM + n * TM + t) * 64 + lane] = sum[n][t];
+  __syncthreads();
+#pragma unroll
+  for (int q0 = 0; q0 < TN * TM; q0 += kWaves) {
+    const int q = q0 + wave, n = q / TM, t = q % TM;
+    if (q >= TN * TM) break;
+    f32x4 y[1][1] = {{part[q * 64 + lane]}};
+#pragma unroll
+    for (int v = 1; v < kWaves; ++v) y[0][0] += part[(v * TN * TM + q) * 64 + lane];
+    store_tile<1, 1, kF32Out>(a, n0 + 16 * n, m0 + 16 * t, quarter, at, y);
+  }
+}
+
+// Up to 16 tokens a tile and weights without end: memory bandwidth is what takes time.  As
+// above, but straight into registers, for which nothing has to be set up (16 x 32000 x
+// 4096: 5.5 TB/s of weights, 26 us; 27 to 28 by way of LDS).
 template <int TN, bool kF32Out>
 __global__ __launch_bounds__(512) void few_tokens_kernel(MatmulArgs a, int tiles_n, int tiles_m) {
   constexpr int kWaves = 8;
@@ -315,7 +466,9 @@ __global__ __launch_bounds__(64 * WN * WM) void small_tiles_kernel(MatmulArgs a,
     if (b + 1 < steps) step(b + 1, two, one);
   }
   wait_loads<0>();
-  store_tile<TN, TM, kF32Out>(a, my_n, my_m, quarter, at, sum);
+  wait_lds();
+  barrier();
+  store_rows<TN, TM, kF32Out>(a, my_n, my_m, quarter, at, sum, lds + wave * kScratch<TN, TM, kF32Out>);
 }
 
 // Many tokens: the matrix cores' rate is what takes time.  A workgroup of WN x WM waves has
@@ -473,80 +626,100 @@ __global__ __launch_bounds__(64 * WN * WM) void tiles_kernel(MatmulArgs a, int t
   const int whole = rest == kBlock ? steps : steps - 1;
   for (int b = 0; b < whole; ++b) step(b, std::false_type{});
   if (whole < steps) step(whole, std::true_type{});
-  wait_loads<0>();  // nothing comes to LDS after the workgroup's end
+  wait_loads<0>();  // nothing comes to LDS any more
+  barrier();
 #pragma unroll
   for (int t = 0; t < TM; ++t)
 #pragma unroll
     for (int j = 0; j < 4; ++j) sum[TN - 1][t][j] = fmaf(y[(TN - 1) & 1][t][j], f[t], sum[TN - 1][t][j]);
-  store_tile<TN, TM, kF32Out>(a, my_n, my_m, quarter, at, sum);
-}
-
-template <int TN>
-hipError_t launch_few(const MatmulArgs& a, hipStream_t s) {
-  const int tiles_n = (a.n + 16 * TN - 1) / (16 * TN), tiles_m = (a.m + 15) / 16;
-  const unsigned grid = (tiles_n * tiles_m + 7) / 8 * 8;
-  if (a.f32) few_tokens_kernel<TN, true><<<grid, 512, 0, s>>>(a, tiles_n, tiles_m);
-  else few_tokens_kernel<TN, false><<<grid, 512, 0, s>>>(a, tiles_n, tiles_m);
-  return hipGetLastError();
+  store_rows<TN, TM, kF32Out>(a, my_n, my_m, quarter, at, sum, lds + wave * kScratch<TN, TM, kF32Out>);
 }
 
 template <int WN, int WM, int TN, int TM, typename K>
-hipError_t launch(K kernel, int bytes, std::atomic<uint64_t>& done, const MatmulArgs& a, hipStream_t s) {
+hipError_t launch(K kernel, int waves, int bytes, std::atomic<uint64_t>& done, const MatmulArgs& a, hipStream_t s) {
   constexpr int kN = 16 * TN * WN, kM = 16 * TM * WM;
-  if (const hipError_t e = allow_lds(reinterpret_cast<const void*>(kernel), bytes, done); e != hipSuccess) return e;
+  if (bytes > 65536)
+    if (const hipError_t e = allow_lds(reinterpret_cast<const void*>(kernel), bytes, done); e != hipSuccess) return e;
   const int tiles_n = (a.n + kN - 1) / kN, tiles_m = (a.m + kM - 1) / kM;
-  kernel<<<(tiles_n * tiles_m + 7) / 8 * 8, 64 * WN * WM, bytes, s>>>(a, tiles_n, tiles_m);
+  kernel<<<(tiles_n * tiles_m + 7) / 8 * 8, 64 * waves, bytes, s>>>(a, tiles_n, tiles_m);
   return hipGetLastError();
 }
 
 template <int WN, int WM, int TN, int TM, int kStages, bool kF32Out>
 hipError_t launch_small_tiles(const MatmulArgs& a, hipStream_t s) {
   constexpr int kBytes = kStages * (16 * (TN * WN + TM * WM) * kBlock + WN * WM * 256);
+  static_assert(kBytes >= WN * WM * kScratch<TN, TM, kF32Out>, "results in LDS");
   static std::atomic<uint64_t> done{0};
-  return launch<WN, WM, TN, TM>(small_tiles_kernel<WN, WM, TN, TM, kStages, kF32Out>, kBytes, done, a, s);
+  return launch<WN, WM, TN, TM>(small_tiles_kernel<WN, WM, TN, TM, kStages, kF32Out>, WN * WM, kBytes, done, a, s);
 }
 
 template <int WN, int WM, int TN, int TM, bool kF32Out>
 hipError_t launch_tiles(const MatmulArgs& a, hipStream_t s) {
-  constexpr int kBytes = 16 * (2 * TN * WN + 3 * TM * WM) * kBlock;
+  constexpr int kOps = 16 * (2 * TN * WN + 3 * TM * WM) * kBlock, kOut = WN * WM * kScratch<TN, TM, kF32Out>;
+  constexpr int kBytes = kOps > kOut ? kOps : kOut;
   static std::atomic<uint64_t> done{0};
-  return launch<WN, WM, TN, TM>(tiles_kernel<WN, WM, TN, TM, kF32Out>, kBytes, done, a, s);
+  return launch<WN, WM, TN, TM>(tiles_kernel<WN, WM, TN, TM, kF32Out>, WN * WM, kBytes, done, a, s);
 }
 
-// What a form takes, in us: base + load * (wave + a step's greater of alone and load *
-// shared), with load the tiles of the busiest compute unit, and not less than its way
-// through the memory.  Fitted to 180 sizes for each type of result (1 to 4096 tokens, 512
-// to 32000 weight rows, k 1024 and 4096; the form chosen takes 1.3 % more than the best on
-// average and 20 % at most; one tile size for all would take 1.5 to 8 times as long at
-// either end).
+template <int TN, bool kF32Out>
+hipError_t launch_few(const MatmulArgs& a, hipStream_t s) {
+  static std::atomic<uint64_t> done{0};
+  return launch<1, 1, TN, 1>(few_tokens_kernel<TN, kF32Out>, 8, 0, done, a, s);
+}
+
+template <int TN, int TM, int kAhead, int kWaves, bool kF32Out>
+hipError_t launch_stream(const MatmulArgs& a, hipStream_t s) {
+  constexpr int kBytes = kWaves * kAhead * (16 * (TN + TM) * kBlock + 256);
+  static_assert(kBytes >= kWaves * TN * TM * 1024, "sums in LDS");
+  static std::atomic<uint64_t> done{0};
+  return launch<1, 1, TN, TM>(stream_kernel<TN, TM, kAhead, kWaves, kF32Out>, kWaves, kBytes, done, a, s);
+}
+
+// What a form takes, in us: base + load * wave + a step's greater of alone and load *
+// shared, a step, with load the tiles of the busiest compute unit, and not less than 3 +
+// its weights and results at `rate` MB/us.  Fitted to 180 sizes for each type of result (1
+// to 4096 tokens, 512 to 32000 weight rows, k 1024 and 4096).  The form chosen takes 0.8 %
+// more than the best on average there, 26 % at most.  Without any one of them the average
+// rises by 0.4 to 3.8 points; the best single form would take 1.5 to 8 times as long at either end.
+// fp32 results have no 256 x 256: the sums of its operands in fp16 would not fit.
 struct Form {
   int n, m;  // of a tile
   float base, wave, alone, shared, rate;
 };
-constexpr int kForms = 9;
+constexpr int kForms = 10;
 constexpr Form kBf16Forms[kForms] = {
-    {256, 256, 3.0f, 11.f, 1.3f, 1.66f, 4.4f}, {128, 128, 3.9f, 2.9f, .8f, .57f, 4.4f},
-    {128, 128, 3.0f, 3.2f, .66f, .77f, 4.4f},  {64, 128, 2.6f, 2.0f, .44f, .38f, 4.4f},
-    {64, 64, 3.2f, .6f, .33f, .235f, 4.4f},    {32, 32, 3.0f, .25f, .2f, .155f, 4.4f},
-    {64, 16, 3.4f, .2f, .29f, .335f, 5.2f},    {32, 16, 3.2f, .1f, .19f, .195f, 5.2f},
-    {16, 16, 3.1f, .1f, .125f, .1f, 5.2f}};
+    {256, 256, 1.f, 6.26f, 0.114f, 1.49f, 2.8f},
+    {128, 128, 2.68f, 1.83f, 0.819f, 0.539f, 3.35f},
+    {128, 128, 1.8f, 2.99f, 0.254f, 0.62f, 4.68f},
+    {64, 64, 2.96f, 0.598f, 0.343f, 0.225f, 5.01f},
+    {32, 32, 2.6f, 0.682f, 0.222f, 0.148f, 4.68f},
+    {64, 16, 3.35f, 0.283f, 0.247f, 0.275f, 5.7f},
+    {64, 32, 1.f, 3.56f, 0.0785f, 0.138f, 5.23f},
+    {32, 32, 1.22f, 3.02f, 0.101f, 0.0956f, 4.49f},
+    {32, 16, 2.75f, 0.827f, 0.0747f, 0.0825f, 5.59f},
+    {16, 16, 2.61f, 1.14f, 0.0414f, 0.0502f, 5.04f}};
 constexpr Form kF32Forms[kForms] = {
-    {256, 128, 3.0f, 8.f, 1.65f, 1.75f, 4.4f}, {128, 128, 3.9f, 2.9f, 1.15f, .93f, 4.4f},
-    {128, 128, 3.0f, 3.2f, 1.1f, 1.15f, 4.4f}, {64, 128, 2.6f, 2.0f, .7f, .62f, 4.4f},
-    {64, 64, 3.2f, .6f, .5f, .41f, 4.4f},      {32, 32, 3.0f, .25f, .28f, .2f, 4.4f},
-    {64, 16, 3.4f, .2f, .29f, .335f, 5.2f},    {32, 16, 3.2f, .1f, .19f, .195f, 5.2f},
-    {16, 16, 3.1f, .1f, .125f, .1f, 5.2f}};
+    {256, 256, 1e30f, 0.f, 0.f, 0.f, 1.f},
+    {128, 128, 4.79f, 1.87f, 1.14f, 0.919f, 5.13f},
+    {128, 128, 2.59f, 3.69f, 0.32f, 1.1f, 3.36f},
+    {64, 64, 4.11f, 0.479f, 0.494f, 0.342f, 4.5f},
+    {32, 32, 2.56f, 0.825f, 0.297f, 0.203f, 4.18f},
+    {64, 16, 3.51f, 0.564f, 0.247f, 0.268f, 6.f},
+    {64, 32, 1.f, 3.62f, 0.163f, 0.21f, 4.86f},
+    {32, 32, 1.38f, 2.79f, 0.149f, 0.141f, 4.19f},
+    {32, 16, 2.71f, 0.981f, 0.107f, 0.0871f, 5.99f},
+    {16, 16, 2.59f, 1.17f, 0.0618f, 0.0536f, 4.98f}};
 
 int choose(const MatmulArgs& a, int m, float* us) {
   const Form* const forms = a.f32 ? kF32Forms : kBf16Forms;
   const int steps = (a.k + kBlock - 1) / kBlock;
   const float mb = ((float)a.n * a.k + (float)m * a.n * (a.f32 ? 4 : 2)) * 1e-6f;
-  int best = 0;
+  int best = 1;
   *us = INFINITY;
   for (int i = 0; i < kForms; ++i) {
     const Form& f = forms[i];
     const int64_t tiles = (int64_t)((a.n + f.n - 1) / f.n) * ((m + f.m - 1) / f.m);
-    if (i > 0 && tiles > 1 << 22) continue;  // a launch has less than 2^32 threads
+    if (i > 1 && tiles > 1 << 22) continue;  // a launch has less than 2^32 threads
     const float load = (float)((tiles + 255) / 256);
     const float t = fmaxf(f.base + f.wave * load + steps * fmaxf(f.alone, load * f.shared), 3.f + mb / f.rate);
     if (t < *us) {
@@ -560,15 +733,18 @@ int choose(const MatmulArgs& a, int m, float* us) {
 template <bool kF32Out>
 hipError_t launch_form(int form, const MatmulArgs& a, hipStream_t s) {
   switch (form) {
-    case 0: return launch_tiles<2, 4, 8, kF32Out ? 2 : 4, kF32Out>(a, s);
+    case 0:
+      if constexpr (!kF32Out) return launch_tiles<2, 4, 8, 4, kF32Out>(a, s);
+      [[fallthrough]];
     case 1: return launch_tiles<2, 2, 4, 4, kF32Out>(a, s);
     case 2: return launch_small_tiles<2, 4, 4, 2, 3, kF32Out>(a, s);
-    case 3: return launch_small_tiles<2, 4, 2, 2, 3, kF32Out>(a, s);
-    case 4: return launch_small_tiles<2, 2, 2, 2, 3, kF32Out>(a, s);
-    case 5: return launch_small_tiles<2, 2, 1, 1, 6, kF32Out>(a, s);
-    case 6: return launch_few<4>(a, s);
-    case 7: return launch_few<2>(a, s);
-    default: return launch_few<1>(a, s);
+    case 3: return launch_small_tiles<2, 2, 2, 2, 3, kF32Out>(a, s);
+    case 4: return launch_small_tiles<2, 2, 1, 1, 6, kF32Out>(a, s);
+    case 5: return launch_few<4, kF32Out>(a, s);
+    case 6: return launch_stream<4, 2, 2, 4, kF32Out>(a, s);
+    case 7: return launch_stream<2, 2, 4, 4, kF32Out>(a, s);
+    case 8: return launch_stream<2, 1, 2, 4, kF32Out>(a, s);
+    default: return launch_stream<1, 1, 2, 8, kF32Out>(a, s);
   }
 }
 

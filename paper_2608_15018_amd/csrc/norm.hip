@@ -5,7 +5,12 @@
 // in fp32 from the loads to one rounding of each output.  In 8 bits a block of 128
 // elements has one scale s = max(|y|, 2^-100) / 448, so that its largest element becomes
 // e4m3's largest, and the codes are y / s.  A row is read once: it stays in registers
-// between the sum of squares and the outputs.
+// between the sum of squares and the outputs, a workgroup a row (a wave, up to 512
+// columns), eight elements a lane at a time, so that sixteen lanes have a block.
+//
+// Bound: memory.  8193 rows of 4096, bf16 in, bf16 residual, 8 bits out: 44 us, 5.3 TB/s
+// (a large copy: 5.2); 12289 rows of 4096 from bf16 to 8 bits 31 us, 4.9 TB/s; 251 rows of
+// 2880 with an fp32 residual 4.2 us, a single row 2.4.
 #include <type_traits>
 
 #include "attn_common.h"
@@ -65,16 +70,16 @@ __device__ __forceinline__ void store8(char* row, int col, const float* f) {
   }
 }
 
-// The codes of eight elements whose block's scale is 1 / inv.  |y| inv is at most 448
-// and a rounding of fp32, which e4m3 rounds to 448.
-__device__ __forceinline__ uint2 codes8(const float* y, float inv) {
+// Eight elements z, which are at most 448 and a rounding of fp32: e4m3 rounds that to 448.
+__device__ __forceinline__ uint2 codes8(const float* z) {
   int lo = 0, hi = 0;
-  lo = __builtin_amdgcn_cvt_pk_fp8_f32(y[0] * inv, y[1] * inv, lo, false);
-  lo = __builtin_amdgcn_cvt_pk_fp8_f32(y[2] * inv, y[3] * inv, lo, true);
-  hi = __builtin_amdgcn_cvt_pk_fp8_f32(y[4] * inv, y[5] * inv, hi, false);
-  hi = __builtin_amdgcn_cvt_pk_fp8_f32(y[6] * inv, y[7] * inv, hi, true);
+  lo = __builtin_amdgcn_cvt_pk_fp8_f32(z[0], z[1], lo, false);
+  lo = __builtin_amdgcn_cvt_pk_fp8_f32(z[2], z[3], lo, true);
+  hi = __builtin_amdgcn_cvt_pk_fp8_f32(z[4], z[5], hi, false);
+  hi = __builtin_amdgcn_cvt_pk_fp8_f32(z[6], z[7], hi, true);
   return uint2{(uint32_t)lo, (uint32_t)hi};
 }
+
 __device__ __forceinline__ float most8(const float* y) {
   float top = 0.f;
 #pragma unroll
@@ -82,14 +87,13 @@ __device__ __forceinline__ float most8(const float* y) {
   return top;
 }
 
-// Sixteen lanes' eight elements each, one block: codes and the scale.  `live` lanes have
-// elements, the others zeros.
+// Codes and scale of a block, sixteen lanes' eight elements each, which `most` is the largest
+// of.  `live` lanes have elements, the others zeros.
 __device__ __forceinline__ void store_block(char* codes, float* scales, int64_t lds, int row, int col, bool live,
-                                            const float* y) {
-  const float scale = fmaxf(max16(most8(y)), kLeast) / kLargest;
+                                            const float* z, float most) {
   if (!live) return;
-  *reinterpret_cast<uint2*>(codes + col) = codes8(y, 1.f / scale);
-  if ((threadIdx.x & 15) == 0) scales[(col / kBlock) * lds + row] = scale;
+  *reinterpret_cast<uint2*>(codes + col) = codes8(z);
+  if ((threadIdx.x & 15) == 0) scales[(col / kBlock) * lds + row] = most / kLargest;
 }
 
 // kLanes lanes a row (64, or the whole workgroup), kChunks times eight elements each.
@@ -159,10 +163,16 @@ __global__ __launch_bounds__(256) void add_norm_kernel(NormArgs a) {
       else
         floats<kBf16>(Raw<kBf16>{{ws[c][0]}}, w);
 #pragma unroll
-      for (int i = 0; i < 8; ++i) y[i] = h[c][i] * norm * w[i];
+      for (int i = 0; i < 8; ++i) y[i] = O == kE4m3 ? h[c][i] * w[i] : h[c][i] * norm * w[i];
     }
     if constexpr (O == kE4m3) {
-      store_block(out, a.scales, a.lds, row, col, live, y);
+      // The norm divides a block's elements and its maximum alike: the codes are 448 h w over
+      // the largest |h w|, and the norm's own rounding does not reach them.
+      const float top = max16(most8(y)), most = fmaxf(top * norm, kLeast);
+      const float times = most > kLeast ? kLargest / top : fminf(norm * (kLargest / kLeast), 1e38f);
+#pragma unroll
+      for (int i = 0; i < 8; ++i) y[i] *= times;
+      store_block(out, a.scales, a.lds, row, col, live, y, most);
     } else {
       if (live) store8<O>(out, col, y);
     }
@@ -179,7 +189,11 @@ __global__ __launch_bounds__(256) void quantize_kernel(QuantizeArgs a) {
     const bool live = col < a.cols;
     float y[8] = {};
     if (live) floats<X>(load8<X>(a.x + row * a.ldx * (X == kF32 ? 4 : 2), col), y);
-    store_block(a.codes + row * a.ldc, a.scales, a.lds, row, col, live, y);
+    const float most = fmaxf(max16(most8(y)), kLeast);
+    const float times = kLargest / most;
+#pragma unroll
+    for (int i = 0; i < 8; ++i) y[i] *= times;
+    store_block(a.codes + row * a.ldc, a.scales, a.lds, row, col, live, y, most);
   }
 }
 
@@ -200,13 +214,15 @@ __global__ __launch_bounds__(256) void quantize_weight_kernel(QuantizeArgs a) {
   if ((threadIdx.x & 63) == 0) part[threadIdx.x >> 6] = top;
   __syncthreads();
   top = fmaxf(fmaxf(part[0], part[1]), fmaxf(part[2], part[3]));
-  const float scale = fmaxf(top, kLeast) / kLargest;
-  if (threadIdx.x == 0) a.scales[blockIdx.y * a.lds + blockIdx.x] = scale;
+  const float most = fmaxf(top, kLeast);
+  const float times = kLargest / most;
+  if (threadIdx.x == 0) a.scales[blockIdx.y * a.lds + blockIdx.x] = most / kLargest;
 #pragma unroll
   for (int i = 0; i < 8; ++i) {
     const int row = row0 + 16 * i;
-    if (row < a.n && col < a.cols)
-      *reinterpret_cast<uint2*>(a.codes + row * a.ldc + col) = codes8(y[i], 1.f / scale);
+#pragma unroll
+    for (int j = 0; j < 8; ++j) y[i][j] *= times;
+    if (row < a.n && col < a.cols) *reinterpret_cast<uint2*>(a.codes + row * a.ldc + col) = codes8(y[i]);
   }
 }
 
