@@ -243,6 +243,28 @@ def test_large_products(m, n, k, out):
 
 
 @pytest.mark.parametrize("out", ["bf16", "f32"])
+@pytest.mark.parametrize("m,n,k", [(2048, 5120, 2064), (1024, 5120, 1024), (384, 2048, 1040), (48, 2048, 1040), (16, 9000, 1040)])
+def test_products_while_copies_delay_their_loads(m, n, k, out):
+    """A workgroup's waves read what others of them have loaded: the same bits however long
+    that takes."""
+    g = gen(m + n + k)
+    whole = lambda *s: torch.randint(-2, 3, s, generator=g, device="cuda").float().to(DT["e4m3"])  # noqa: E731
+    one = lambda *s: torch.ones(s, device="cuda")  # noqa: E731
+    kb = do.blocks_of(k)
+    x, w = s2.Fp8Rows(whole(m, k), one(kb, m)), s2.Fp8Weight(whole(n, k), one(do.blocks_of(n), kb))
+    want = (x.codes.float().double() @ w.codes.float().double().t().contiguous()).float().to(DT[out])
+    src, dst = (torch.zeros(2 ** 28, dtype=torch.uint8, device="cuda") for _ in range(2))
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(side):
+        for _ in range(12):
+            dst.copy_(src)
+    got = [s2.fp8_matmul(x, w, out_dtype=DT[out]) for _ in range(24)]
+    torch.cuda.synchronize()
+    assert all(torch.equal(y, want) for y in got)
+
+
+@pytest.mark.parametrize("out", ["bf16", "f32"])
 @pytest.mark.parametrize("m,n,k", [(5, 77, 272), (40, 129, 144), (200, 300, 400), (600, 520, 272)])
 def test_product_of_parts_of_larger_arrays(m, n, k, out):
     """Rows, scales and results inside arrays whose other elements are NaN, and stay."""
