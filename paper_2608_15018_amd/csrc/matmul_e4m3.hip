@@ -80,13 +80,15 @@ __device__ __forceinline__ void arrived(float& x) { asm volatile("" : "+v"(x)); 
 
 // The workgroup's tile: each of the eight dies takes a stretch of the tiles, in strips four
 // tiles of weights wide, so that its second-level cache holds what its workgroups share
-// (8192 x 6144 x 4096: 1 to 4 % less time than tiles dealt out one by one).
+// (8193 x 6144 x 4096 with strips of one, two, four, eight: 191, 178, 175, 175 us; 251 x 5120
+// x 2880, from memory: 13.7, 13.6, 13.3, 14.5).
+constexpr int kStrip = 4;
 __device__ __forceinline__ bool tile_of(int tiles_n, int tiles_m, int* tn, int* tm) {
   const int tiles = tiles_n * tiles_m, per = (tiles + 7) / 8;
   const int nth = blockIdx.x >> 3, tile = (blockIdx.x & 7) * per + nth;
   if (nth >= per || tile >= tiles) return false;
-  const int strip = tile / (4 * tiles_m), in = tile - strip * 4 * tiles_m, wide = min(4, tiles_n - strip * 4);
-  *tn = strip * 4 + in % wide;
+  const int strip = tile / (kStrip * tiles_m), in = tile - strip * kStrip * tiles_m, wide = min(kStrip, tiles_n - strip * kStrip);
+  *tn = strip * kStrip + in % wide;
   *tm = in / wide;
   return true;
 }
@@ -136,6 +138,7 @@ __device__ __forceinline__ void store_tile(const MatmulArgs& a, int my_n, int my
 
 // The same by way of LDS, a stretch of whole rows at a time: results lie 32 bytes of a row to
 // 16 rows in the lanes, and stored so they would take 32 us of 202 at 8192 x 6144 x 4096.
+// Past the caches, which the operands need: 175 us there instead of 183.
 // `scratch`: the wave's own kScratch<..> bytes, which nothing else uses any more.
 template <int TN, int TM, bool kF32Out>
 constexpr int kScratch = 16 * TM * (16 * TN * (kF32Out ? 4 : 2) + 16);
@@ -166,7 +169,7 @@ __device__ __forceinline__ void store_rows(const MatmulArgs& a, int my_n, int my
   for (int r0 = 0; r0 < 16 * TM; r0 += kAtOnce) {
     const int r = r0 + lane / kPieces, to = my_m + r;
     const u32x4 v = *reinterpret_cast<const u32x4*>(scratch + r * kStep + piece * 16);
-    if (to < a.m) *reinterpret_cast<u32x4*>(a.out + (to * a.ldo + my_n) * elt + piece * 16) = v;
+    if (to < a.m) __builtin_nontemporal_store(v, reinterpret_cast<u32x4*>(a.out + (to * a.ldo + my_n) * elt + piece * 16));
   }
 }
 
@@ -682,37 +685,37 @@ hipError_t launch_stream(const MatmulArgs& a, hipStream_t s) {
 // What a form takes, in us: base + load * wave + a step's greater of alone and load *
 // shared, a step, with load the tiles of the busiest compute unit, and not less than 3 +
 // its weights and results at `rate` MB/us.  Fitted to 180 sizes for each type of result (1
-// to 4096 tokens, 512 to 32000 weight rows, k 1024 and 4096).  The form chosen takes 0.8 %
-// more than the best on average there, 26 % at most.  Without any one of them the average
-// rises by 0.4 to 3.8 points; the best single form would take 1.5 to 8 times as long at either end.
-// fp32 results have no 256 x 256: the sums of its operands in fp16 would not fit.
+// to 4096 tokens, 512 to 32000 weight rows, k 1024 and 4096).  The form chosen takes 0.6 %
+// more than the best on average there, 18 % at most.  Without any one of them the average
+// rises by 0.1 to 6.8 points.  fp32 results have no 256 x 256, whose operands in fp16 would
+// not fit beside the sums, and no second 128 x 128, which nothing is faster by.
 struct Form {
   int n, m;  // of a tile
   float base, wave, alone, shared, rate;
 };
 constexpr int kForms = 10;
 constexpr Form kBf16Forms[kForms] = {
-    {256, 256, 1.f, 6.26f, 0.114f, 1.49f, 2.8f},
-    {128, 128, 2.68f, 1.83f, 0.819f, 0.539f, 3.35f},
-    {128, 128, 1.8f, 2.99f, 0.254f, 0.62f, 4.68f},
-    {64, 64, 2.96f, 0.598f, 0.343f, 0.225f, 5.01f},
-    {32, 32, 2.6f, 0.682f, 0.222f, 0.148f, 4.68f},
-    {64, 16, 3.35f, 0.283f, 0.247f, 0.275f, 5.7f},
-    {64, 32, 1.f, 3.56f, 0.0785f, 0.138f, 5.23f},
-    {32, 32, 1.22f, 3.02f, 0.101f, 0.0956f, 4.49f},
-    {32, 16, 2.75f, 0.827f, 0.0747f, 0.0825f, 5.59f},
-    {16, 16, 2.61f, 1.14f, 0.0414f, 0.0502f, 5.04f}};
+    {256, 256, 1.f, 5.61f, 0.835f, 1.47f, 2.84f},
+    {128, 128, 3.35f, 0.9f, 0.742f, 0.511f, 3.65f},
+    {128, 128, 2.33f, 2.35f, 0.219f, 0.62f, 4.79f},
+    {64, 64, 3.65f, 0.304f, 0.331f, 0.221f, 5.2f},
+    {32, 32, 2.43f, 0.808f, 0.225f, 0.145f, 4.74f},
+    {64, 16, 3.77f, 0.169f, 0.19f, 0.273f, 5.87f},
+    {64, 32, 1.f, 3.63f, 0.133f, 0.137f, 5.22f},
+    {32, 32, 1.14f, 3.07f, 0.102f, 0.0919f, 4.53f},
+    {32, 16, 2.74f, 0.806f, 0.0566f, 0.0831f, 5.61f},
+    {16, 16, 2.55f, 1.14f, 0.0581f, 0.0493f, 5.04f}};
 constexpr Form kF32Forms[kForms] = {
     {256, 256, 1e30f, 0.f, 0.f, 0.f, 1.f},
-    {128, 128, 4.79f, 1.87f, 1.14f, 0.919f, 5.13f},
-    {128, 128, 2.59f, 3.69f, 0.32f, 1.1f, 3.36f},
-    {64, 64, 4.11f, 0.479f, 0.494f, 0.342f, 4.5f},
-    {32, 32, 2.56f, 0.825f, 0.297f, 0.203f, 4.18f},
-    {64, 16, 3.51f, 0.564f, 0.247f, 0.268f, 6.f},
-    {64, 32, 1.f, 3.62f, 0.163f, 0.21f, 4.86f},
-    {32, 32, 1.38f, 2.79f, 0.149f, 0.141f, 4.19f},
-    {32, 16, 2.71f, 0.981f, 0.107f, 0.0871f, 5.99f},
-    {16, 16, 2.59f, 1.17f, 0.0618f, 0.0536f, 4.98f}};
+    {128, 128, 4.76f, 1.54f, 0.969f, 0.838f, 3.72f},
+    {128, 128, 1e30f, 0.f, 0.f, 0.f, 1.f},
+    {64, 64, 4.43f, 0.187f, 0.495f, 0.336f, 4.55f},
+    {32, 32, 2.64f, 0.685f, 0.299f, 0.206f, 4.06f},
+    {64, 16, 3.59f, 0.549f, 0.186f, 0.267f, 5.92f},
+    {64, 32, 1.f, 3.73f, 0.0955f, 0.207f, 4.86f},
+    {32, 32, 1.19f, 2.95f, 0.15f, 0.134f, 4.21f},
+    {32, 16, 2.64f, 1.02f, 0.107f, 0.0868f, 5.61f},
+    {16, 16, 2.56f, 1.14f, 0.0688f, 0.0539f, 4.99f}};
 
 int choose(const MatmulArgs& a, int m, float* us) {
   const Form* const forms = a.f32 ? kF32Forms : kBf16Forms;
@@ -740,8 +743,10 @@ hipError_t launch_form(int form, const MatmulArgs& a, hipStream_t s) {
     case 0:
       if constexpr (!kF32Out) return launch_tiles<2, 4, 8, 4, kF32Out>(a, s);
       [[fallthrough]];
+    case 2:
+      if constexpr (!kF32Out) return launch_small_tiles<2, 4, 4, 2, 3, kF32Out>(a, s);
+      [[fallthrough]];
     case 1: return launch_tiles<2, 2, 4, 4, kF32Out>(a, s);
-    case 2: return launch_small_tiles<2, 4, 4, 2, 3, kF32Out>(a, s);
     case 3: return launch_small_tiles<2, 2, 2, 2, 3, kF32Out>(a, s);
     case 4: return launch_small_tiles<2, 2, 1, 1, 6, kF32Out>(a, s);
     case 5: return launch_few<4, kF32Out>(a, s);
