@@ -65,6 +65,15 @@ __device__ __forceinline__ i32x8 cut_off(i32x8 v, int quarter, int rest) {
 __device__ __forceinline__ void load16(const char* base, uint32_t off, uint32_t at) {
   asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %2" : : "s"(at), "v"(off), "s"(base) : "memory", "m0");
 }
+// The same of weights, kOnce: that no other workgroup reads, which leaves the caches to the
+// rest (16 x 32000 x 4096: 24.5 us, 27.3 without; weights that several read take longer so).
+template <bool kOnce>
+__device__ __forceinline__ void load16_w(const char* base, uint32_t off, uint32_t at) {
+  if constexpr (kOnce)
+    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %2 nt" : : "s"(at), "v"(off), "s"(base) : "memory", "m0");
+  else
+    load16(base, off, at);
+}
 __device__ __forceinline__ void load4(const char* base, uint32_t off, uint32_t at) {  // 256 bytes a wave
   asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dword %1, %2" : : "s"(at), "v"(off), "s"(base) : "memory", "m0");
 }
@@ -173,15 +182,15 @@ __device__ __forceinline__ void store_rows(const MatmulArgs& a, int my_n, int my
   }
 }
 
-// Up to 32 tokens a tile and weights that do not fill the chip so long: how soon they come is
-// what takes time.  A workgroup has 16 TN weight rows and 16 TM tokens; its waves take the
-// blocks of k in turn, kAhead of them on their way to LDS at any time, each to the wave's own
-// places, so that no wave waits for another before the sums are added, in the waves' order.
-// Eight lanes read 128 bytes of a row, four times the lines a load that the operands'
-// layout would have (16 x 6144 x 4096: 7.2 us, 9.2 with loads straight to registers).
-// Workgroups begin at different blocks: rows that lie 4096 bytes apart, read in step, would
-// come from few of the memory's channels.
-template <int TN, int TM, int kAhead, int kWaves, bool kF32Out>
+// Up to 32 tokens a tile: how soon the weights come is what takes time, their latency or,
+// of many, their bytes (16 x 32000 x 4096: 24.7 us, 5.3 TB/s of weights).  A workgroup has
+// 16 TN weight rows and 16 TM tokens; its waves take the blocks of k in turn, kAhead of them
+// on their way to LDS at any time, each to the wave's own places, so that no wave waits for
+// another before the sums are added, in the waves' order.  Eight lanes read 128 bytes of a
+// row, four times the lines a load that the operands' layout would have (16 x 6144 x 4096:
+// 7.2 us, 9.2 with loads straight to registers).  Workgroups begin at different blocks: rows
+// that lie 4096 bytes apart, read in step, would come from few of the memory's channels.
+template <int TN, int TM, int kAhead, int kWaves, bool kF32Out, bool kOnce>
 __global__ __launch_bounds__(64 * kWaves) void stream_kernel(MatmulArgs a, int tiles_n, int tiles_m) {
   constexpr int kRows = 16 * (TN + TM), kLoads = 2 * (TN + TM) + 1, kStage = kRows * kBlock + 256;
   extern __shared__ __attribute__((aligned(1024))) char lds[];
@@ -216,7 +225,7 @@ __global__ __launch_bounds__(64 * kWaves) void stream_kernel(MatmulArgs a, int t
     const uint32_t st = at0 + slot * kStage;
     const uint32_t back = b == steps - 1 && piece * 16 >= rest ? (uint32_t)(piece * 16 - rest + 16) : 0u;
 #pragma unroll
-    for (int l = 0; l < 2 * TN; ++l) load16(wbase + b * kBlock, woff[l] - back, st + l * 1024);
+    for (int l = 0; l < 2 * TN; ++l) load16_w<kOnce>(wbase + b * kBlock, woff[l] - back, st + l * 1024);
 #pragma unroll
     for (int l = 0; l < 2 * TM; ++l) load16(xbase + b * kBlock, xoff[l] - back, st + (2 * TN + l) * 1024);
     load4(reinterpret_cast<const char*>(a.xs + b * a.ldxs), mine, st + kRows * kBlock);
@@ -290,9 +299,9 @@ __global__ __launch_bounds__(64 * kWaves) void stream_kernel(MatmulArgs a, int t
   }
 }
 
-// Up to 16 tokens a tile and weights without end: memory bandwidth is what takes time.  As
-// above, but straight into registers, for which nothing has to be set up (16 x 32000 x
-// 4096: 5.5 TB/s of weights, 26 us; 27 to 28 by way of LDS).
+// Up to 16 tokens a tile and several rounds of workgroups: as above, but straight into
+// registers, for which a workgroup has nothing to set up (16 x 16384 x 2048: 9.1 us, 9.5 to
+// 9.9 by way of LDS).
 template <int TN, bool kF32Out>
 __global__ __launch_bounds__(512) void few_tokens_kernel(MatmulArgs a, int tiles_n, int tiles_m) {
   constexpr int kWaves = 8;
@@ -352,7 +361,7 @@ __global__ __launch_bounds__(512) void few_tokens_kernel(MatmulArgs a, int tiles
 // Tiles between: what a step costs beside its products is what takes time.  kStages blocks
 // of k are in LDS or on their way there; while the matrix cores have one block's operands,
 // the waves read the next one's.  Scales of tokens come the same way, 64 words a wave.
-template <int WN, int WM, int TN, int TM, int kStages, bool kF32Out>
+template <int WN, int WM, int TN, int TM, int kStages, bool kF32Out, bool kOnce>
 __global__ __launch_bounds__(64 * WN * WM) void small_tiles_kernel(MatmulArgs a, int tiles_n, int tiles_m) {
   constexpr int kN = 16 * TN * WN, kM = 16 * TM * WM, kWaves = WN * WM;
   constexpr int kLoadsW = kN / 8 / kWaves, kLoadsX = kM / 8 / kWaves, kLoads = kLoadsW + kLoadsX + 1;
@@ -389,7 +398,7 @@ __global__ __launch_bounds__(64 * WN * WM) void small_tiles_kernel(MatmulArgs a,
     const uint32_t st = at0 + to * kStage;
     const uint32_t back = loaded == steps - 1 && piece * 16 >= rest ? (uint32_t)(piece * 16 - rest + 16) : 0u;
 #pragma unroll
-    for (int i = 0; i < kLoadsW; ++i) load16(wp, woff[i] - back, st + (wave * kLoadsW + i) * 1024);
+    for (int i = 0; i < kLoadsW; ++i) load16_w<kOnce>(wp, woff[i] - back, st + (wave * kLoadsW + i) * 1024);
 #pragma unroll
     for (int i = 0; i < kLoadsX; ++i) load16(xp, xoff[i] - back, st + kN * kBlock + (wave * kLoadsX + i) * 1024);
     load4(sp, mine, st + (kN + kM) * kBlock + wave * 256);
@@ -652,12 +661,14 @@ hipError_t launch(K kernel, int waves, int bytes, std::atomic<uint64_t>& done, c
   return hipGetLastError();
 }
 
-template <int WN, int WM, int TN, int TM, int kStages, bool kF32Out>
+template <int WN, int WM, int TN, int TM, int kStages, bool kF32Out, bool kOnce = false>
 hipError_t launch_small_tiles(const MatmulArgs& a, hipStream_t s) {
+  if constexpr (!kOnce)
+    if (a.m <= 16 * TM * WM) return launch_small_tiles<WN, WM, TN, TM, kStages, kF32Out, true>(a, s);
   constexpr int kBytes = kStages * (16 * (TN * WN + TM * WM) * kBlock + WN * WM * 256);
   static_assert(kBytes >= WN * WM * kScratch<TN, TM, kF32Out>, "results in LDS");
   static std::atomic<uint64_t> done{0};
-  return launch<WN, WM, TN, TM>(small_tiles_kernel<WN, WM, TN, TM, kStages, kF32Out>, WN * WM, kBytes, done, a, s);
+  return launch<WN, WM, TN, TM>(small_tiles_kernel<WN, WM, TN, TM, kStages, kF32Out, kOnce>, WN * WM, kBytes, done, a, s);
 }
 
 template <int WN, int WM, int TN, int TM, bool kF32Out>
@@ -674,48 +685,51 @@ hipError_t launch_few(const MatmulArgs& a, hipStream_t s) {
   return launch<1, 1, TN, 1>(few_tokens_kernel<TN, kF32Out>, 8, 0, done, a, s);
 }
 
-template <int TN, int TM, int kAhead, int kWaves, bool kF32Out>
+template <int TN, int TM, int kAhead, int kWaves, bool kF32Out, bool kOnce = false>
 hipError_t launch_stream(const MatmulArgs& a, hipStream_t s) {
+  if constexpr (!kOnce)
+    if (a.m <= 16 * TM) return launch_stream<TN, TM, kAhead, kWaves, kF32Out, true>(a, s);
   constexpr int kBytes = kWaves * kAhead * (16 * (TN + TM) * kBlock + 256);
   static_assert(kBytes >= kWaves * TN * TM * 1024, "sums in LDS");
   static std::atomic<uint64_t> done{0};
-  return launch<1, 1, TN, TM>(stream_kernel<TN, TM, kAhead, kWaves, kF32Out>, kWaves, kBytes, done, a, s);
+  return launch<1, 1, TN, TM>(stream_kernel<TN, TM, kAhead, kWaves, kF32Out, kOnce>, kWaves, kBytes, done, a, s);
 }
 
 // What a form takes, in us: base + load * wave + a step's greater of alone and load *
 // shared, a step, with load the tiles of the busiest compute unit, and not less than 3 +
-// its weights and results at `rate` MB/us.  Fitted to 180 sizes for each type of result (1
-// to 4096 tokens, 512 to 32000 weight rows, k 1024 and 4096).  The form chosen takes 0.6 %
-// more than the best on average there, 18 % at most.  Without any one of them the average
-// rises by 0.1 to 6.8 points.  fp32 results have no 256 x 256, whose operands in fp16 would
-// not fit beside the sums, and no second 128 x 128, which nothing is faster by.
+// its weights and results at `rate` MB/us.  Fitted to 336 sizes for each type of result (1
+// to 4096 tokens, 512 to 32000 weight rows, k from 512 to 6144), foremost to which form is
+// fastest.  The one chosen takes 0.2 % more than the best on average there, 15 % at most
+// (sizes left out of the fit: 0.4 and 27 %); without any one form the average rises by
+// 0.3 to 7.6 points.  fp32 results have no 256 x 256, whose operands in fp16 would not fit
+// beside the sums, and no second 128 x 128, which nothing is faster by.
 struct Form {
   int n, m;  // of a tile
   float base, wave, alone, shared, rate;
 };
 constexpr int kForms = 10;
 constexpr Form kBf16Forms[kForms] = {
-    {256, 256, 1.f, 5.61f, 0.835f, 1.47f, 2.84f},
-    {128, 128, 3.35f, 0.9f, 0.742f, 0.511f, 3.65f},
-    {128, 128, 2.33f, 2.35f, 0.219f, 0.62f, 4.79f},
-    {64, 64, 3.65f, 0.304f, 0.331f, 0.221f, 5.2f},
-    {32, 32, 2.43f, 0.808f, 0.225f, 0.145f, 4.74f},
-    {64, 16, 3.77f, 0.169f, 0.19f, 0.273f, 5.87f},
-    {64, 32, 1.f, 3.63f, 0.133f, 0.137f, 5.22f},
-    {32, 32, 1.14f, 3.07f, 0.102f, 0.0919f, 4.53f},
-    {32, 16, 2.74f, 0.806f, 0.0566f, 0.0831f, 5.61f},
-    {16, 16, 2.55f, 1.14f, 0.0581f, 0.0493f, 5.04f}};
+    {256, 256, 1.f, 5.87f, 0.135f, 1.33f, 3.95f},
+    {128, 128, 4.71f, 0.739f, 0.744f, 0.503f, 3.9f},
+    {128, 128, 2.7f, 3.09f, 0.562f, 0.585f, 4.76f},
+    {64, 64, 2.78f, 0.642f, 0.392f, 0.241f, 5.23f},
+    {32, 32, 2.42f, 0.92f, 0.212f, 0.149f, 4.68f},
+    {64, 16, 3.36f, 0.0518f, 0.135f, 0.275f, 5.95f},
+    {64, 32, 1.12f, 4.58f, 0.0499f, 0.161f, 5.84f},
+    {32, 32, 1.15f, 3.35f, 0.106f, 0.111f, 5.35f},
+    {32, 16, 2.39f, 0.991f, 0.0588f, 0.113f, 6.4f},
+    {16, 16, 2.65f, 1.55f, 0.0423f, 0.0424f, 4.84f}};
 constexpr Form kF32Forms[kForms] = {
     {256, 256, 1e30f, 0.f, 0.f, 0.f, 1.f},
-    {128, 128, 4.76f, 1.54f, 0.969f, 0.838f, 3.72f},
+    {128, 128, 4.09f, 1.26f, 1.08f, 0.845f, 5.83f},
     {128, 128, 1e30f, 0.f, 0.f, 0.f, 1.f},
-    {64, 64, 4.43f, 0.187f, 0.495f, 0.336f, 4.55f},
-    {32, 32, 2.64f, 0.685f, 0.299f, 0.206f, 4.06f},
-    {64, 16, 3.59f, 0.549f, 0.186f, 0.267f, 5.92f},
-    {64, 32, 1.f, 3.73f, 0.0955f, 0.207f, 4.86f},
-    {32, 32, 1.19f, 2.95f, 0.15f, 0.134f, 4.21f},
-    {32, 16, 2.64f, 1.02f, 0.107f, 0.0868f, 5.61f},
-    {16, 16, 2.56f, 1.14f, 0.0688f, 0.0539f, 4.99f}};
+    {64, 64, 3.77f, 0.333f, 0.564f, 0.328f, 4.67f},
+    {32, 32, 2.64f, 0.743f, 0.304f, 0.212f, 4.3f},
+    {64, 16, 3.53f, 0.36f, 0.0738f, 0.267f, 5.79f},
+    {64, 32, 1.16f, 3.9f, 0.162f, 0.197f, 5.58f},
+    {32, 32, 1.14f, 3.12f, 0.141f, 0.15f, 5.59f},
+    {32, 16, 2.55f, 1.26f, 0.0999f, 0.0851f, 6.4f},
+    {16, 16, 2.42f, 1.12f, 0.0731f, 0.061f, 4.82f}};
 
 int choose(const MatmulArgs& a, int m, float* us) {
   const Form* const forms = a.f32 ? kF32Forms : kBf16Forms;

@@ -209,7 +209,9 @@ def test_products_of_small_whole_numbers_are_exact(m, n, k, out):
 # Between them every form of the kernel for either type, whole tiles and a few tokens past them.
 LARGE = [(257, 512, 400), (384, 2048, 1040), (700, 2050, 1024), (768, 5120, 1040), (1024, 5121, 1024), (1536, 5120, 2064), (2048, 2048, 1024),
          (257, 16400, 1024), (1025, 16384, 1040), (384, 32000, 1024), (2052, 6144, 2880), (90, 32000, 272), (33, 20000, 144), (16, 30001, 1168),
-         (1, 9001, 1040), (20, 9000, 272), (27, 5001, 1040), (1, 9000, 272), (17, 9000, 528), (30, 12001, 1168)]
+         (1, 9001, 1040), (20, 9000, 272), (27, 5001, 1040), (1, 9000, 272), (17, 9000, 528), (30, 12001, 1168),
+         (33, 5001, 272), (50, 5001, 2064), (50, 5001, 528), (1, 9000, 4112), (33, 3000, 2064), (33, 3000, 1040), (17, 5001, 2064),
+         (17, 2050, 272)]
 
 
 @pytest.mark.parametrize("out", ["bf16", "f32"])
