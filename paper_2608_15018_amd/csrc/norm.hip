@@ -8,9 +8,10 @@
 // between the sum of squares and the outputs, a workgroup a row (a wave, up to 512
 // columns), eight elements a lane at a time, so that sixteen lanes have a block.
 //
-// Bound: memory.  8193 rows of 4096, bf16 in, bf16 residual, 8 bits out: 44 us, 5.3 TB/s
-// (a large copy: 5.2); 12289 rows of 4096 from bf16 to 8 bits 31 us, 4.9 TB/s; 251 rows of
-// 2880 with an fp32 residual 4.2 us, a single row 2.4.
+// Bound: memory.  8193 rows of 4096, bf16 in, bf16 residual, 8 bits out: 42 us, 5.6 TB/s
+// (a large copy: 5.2; with x read through the caches 47, the residual past them too 43,
+// stores past them 45); 12289 rows of 4096 from bf16 to 8 bits 30 us, 5.1 TB/s (31 through
+// the caches); 251 rows of 2880 with an fp32 residual 4.2 us, a single row 2.3.
 #include <type_traits>
 
 #include "attn_common.h"
@@ -36,17 +37,18 @@ __device__ __forceinline__ float sum16(float x) {
   return x + ror<1>(x);
 }
 
-// Eight neighbouring elements of a row.
+// Eight neighbouring elements of a row; past the caches where nothing reads or writes them
+// again (not a residual).
 template <int T>
 struct Raw {
   u32x4 v[T == kF32 ? 2 : 1];
 };
-template <int T>
+template <int T, bool kOnce = true>
 __device__ __forceinline__ Raw<T> load8(const char* row, int col) {
   Raw<T> r;
   const u32x4* p = reinterpret_cast<const u32x4*>(row + (int64_t)col * (T == kF32 ? 4 : 2));
-  r.v[0] = p[0];
-  if constexpr (T == kF32) r.v[1] = p[1];
+#pragma unroll
+  for (int i = 0; i < (T == kF32 ? 2 : 1); ++i) r.v[i] = kOnce ? __builtin_nontemporal_load(p + i) : p[i];
   return r;
 }
 template <int T>
@@ -114,7 +116,7 @@ __global__ __launch_bounds__(256) void add_norm_kernel(NormArgs a) {
     const int col = (c * kLanes + lane) * 8;
     if (col < a.H) {
       xs[c] = load8<X>(x, col);
-      if constexpr (R != kNone) rs[c] = load8<R>(r, col);
+      if constexpr (R != kNone) rs[c] = load8<R, false>(r, col);
       if (a.w_type == kF32) {
         ws[c][0] = reinterpret_cast<const u32x4*>(a.weight)[col / 4];
         ws[c][1] = reinterpret_cast<const u32x4*>(a.weight)[col / 4 + 1];

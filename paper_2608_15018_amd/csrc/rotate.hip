@@ -7,8 +7,9 @@
 // their angle; sine, cosine and the products are fp32, and each element is rounded once.
 //
 // Bound: memory for prompts (17000 tokens, 32 query heads, 4 of keys and values, 128
-// wide: 68 us, 5.1 TB/s, what a large copy reaches), latency for a step's few tokens (4.5
-// us).  Angles are worked out from the frequencies, a token's pairs by as many lanes, and
+// wide: 61 us, 5.5 TB/s, a large copy 5.2; 67 with queries through the caches, 65 and 71
+// with their loads or stores so, 63 with keys and values past them too), latency for a
+// step's few tokens (4.5 us).  Angles are worked out from the frequencies, a token's pairs by as many lanes, and
 // shared through LDS: a table of them would have to be read.
 #include <type_traits>
 
@@ -164,8 +165,8 @@ __global__ __launch_bounds__(256) void append_rotated_kernel(KvCache c, RotateAr
 #pragma unroll
       for (int i = 0; i < kAtOnce; ++i) {
         const int g = min(h + i * step, a.Hq - 1);
-        u[i] = q[g * kPieces + at.x];
-        v[i] = q[g * kPieces + at.y];
+        u[i] = __builtin_nontemporal_load(q + g * kPieces + at.x);
+        v[i] = __builtin_nontemporal_load(q + g * kPieces + at.y);
       }
     };
     load(h0);
@@ -178,8 +179,8 @@ __global__ __launch_bounds__(256) void append_rotated_kernel(KvCache c, RotateAr
       for (int i = 0; i < kAtOnce; ++i) {
         if (duo < turned) turn<E>(u[i], v[i], cs[0] + duo * N, neighbours);
         if (h + i * step < a.Hq) {
-          to[(h + i * step) * kPieces + at.x] = u[i];
-          to[(h + i * step) * kPieces + at.y] = v[i];
+          __builtin_nontemporal_store(u[i], to + (h + i * step) * kPieces + at.x);
+          __builtin_nontemporal_store(v[i], to + (h + i * step) * kPieces + at.y);
         }
       }
     }
