@@ -212,10 +212,13 @@ LARGE = [(257, 512, 400), (384, 2048, 1040), (700, 2050, 1024), (768, 5120, 1040
          (1, 9001, 1040), (20, 9000, 272), (27, 5001, 1040), (1, 9000, 272), (17, 9000, 528), (30, 12001, 1168),
          (33, 5001, 272), (50, 5001, 2064), (50, 5001, 528), (1, 9000, 4112), (33, 3000, 2064), (33, 3000, 1040), (17, 5001, 2064),
          (17, 2050, 272)]
+# A wave's weight scales are 64 blocks at a time: rows of more than that, for each form.
+LONG = [(1, 48, 70016), (17, 48, 70016), (1, 5001, 33040), (17, 5001, 33040), (17, 2050, 33040), (33, 3000, 33040), (33, 5001, 33040),
+        (33, 9000, 8720), (200, 9000, 8720), (256, 2050, 8720), (600, 5001, 8720), (900, 9000, 8720), (2052, 2050, 8720)]
 
 
 @pytest.mark.parametrize("out", ["bf16", "f32"])
-@pytest.mark.parametrize("m,n,k", LARGE)
+@pytest.mark.parametrize("m,n,k", LARGE + LONG)
 def test_large_products(m, n, k, out):
     """Whole numbers exactly, everywhere; other codes at rows and columns drawn."""
     g = gen(m + n + k)
@@ -341,3 +344,39 @@ def test_a_chain_on_another_stream_and_in_a_graph(m):
         graph.replay()
         torch.cuda.synchronize()
         assert torch.equal(y, want) and torch.equal(r, res), i
+
+
+# -------------------------------------------------------------------------- past 32 bits
+
+
+def test_rows_past_four_gigabytes():
+    """The same rows far behind others and alone, to the same bits."""
+    n, H, tail = 300000, 8192, 3
+    g = gen(5)
+    x = torch.zeros((n, H), dtype=torch.bfloat16, device="cuda")
+    x[-tail:] = randn((tail, H), "bf16", g)
+    w, r = randn((H,), "bf16", g), torch.zeros((n, H), dtype=torch.bfloat16, device="cuda")
+    alone = s2.add_norm(x[-tail:].clone(), w, torch.zeros((tail, H), dtype=torch.bfloat16, device="cuda"), out_dtype=s2.E4M3)
+    far = s2.add_norm(x, w, r, out_dtype=s2.E4M3)
+    assert torch.equal(r[-tail:], x[-tail:]) and not r[:-tail].any()
+    assert torch.equal(far.codes[-tail:].view(torch.uint8), alone.codes.view(torch.uint8)) and torch.equal(far.scales[:, -tail:], alone.scales)
+    del r, far
+    alone, far = s2.quantize(x[-tail:].clone()), s2.quantize(x)
+    assert torch.equal(far.codes[-tail:].view(torch.uint8), alone.codes.view(torch.uint8)) and torch.equal(far.scales[:, -tail:], alone.scales)
+
+
+@pytest.mark.parametrize("m,n", [(40000, 32000), (33, 1000000)])
+def test_products_past_four_gigabytes(m, n):
+    """Results past 2^32 bytes, and weights past 2^32 bytes: exact whole numbers at the end."""
+    k = 272 if m > 1000 else 4368
+    g = gen(m)
+    whole = lambda *s: torch.randint(-2, 3, s, generator=g, device="cuda", dtype=torch.int8).to(DT["e4m3"])  # noqa: E731
+    one = lambda *s: torch.ones(s, device="cuda")  # noqa: E731
+    kb = do.blocks_of(k)
+    x, w = s2.Fp8Rows(whole(m, k), one(kb, m)), s2.Fp8Weight(whole(n, k), one(do.blocks_of(n), kb))
+    got = s2.fp8_matmul(x, w, out_dtype=torch.float32)
+    rows, cols = slice(max(0, m - 300), m), slice(n - 1000, n)
+    want = x.codes[rows].float().double() @ w.codes[cols].float().double().t().contiguous()
+    assert torch.equal(got[rows, cols], want.float())
+    want = x.codes[:40].float().double() @ w.codes[cols].float().double().t().contiguous()
+    assert torch.equal(got[:40, cols], want.float())
