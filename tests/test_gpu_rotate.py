@@ -248,3 +248,35 @@ def test_streams_and_graphs():
                 p = int(c.table[s, j // 32])
                 assert torch.equal(c.k[0, p, :, j % 32], other.k[0, p, :, j % 32])
                 assert torch.equal(c.v[0, p, :, j % 32 // 8, :, j % 8], other.v[0, p, :, j % 32 // 8, :, j % 8])
+
+
+def test_rows_and_pages_past_four_gigabytes():
+    """The last tokens of many, and pages at the end of a long cache, as the same tokens alone
+    in a short one."""
+    n, tail, Hq, Hkv, D, P = 300000, 5, 64, 1, 128, 256
+    long, short = (s2.KVCache(2, 8, D, pages, P, 1, 2) for pages in (5200, 2))
+    for c in (long, short):
+        c.table[0, :2] = ints([c.n_pages - 1, c.n_pages - 2])
+        c.refs[-2:] = 1
+        c.length.fill_(P - 2)
+        c.k.zero_()
+        c.v.zero_()
+    f, g = freqs(D), torch.Generator(device="cuda").manual_seed(3)
+    pos = ints([7, 100, 3, 2000, 65])
+    q, k, v = (torch.randn((tail, h, D), generator=g, device="cuda").to(torch.bfloat16) for h in (16, 8, 8))
+    want = short.append_rotated(1, q, k, v, ints([0]), ints([0, tail]), pos, f)
+    assert torch.equal(long.append_rotated(1, q, k, v, ints([0]), ints([0, tail]), pos, f), want)
+    for t in ("k", "v"):
+        assert torch.equal(getattr(long, t)[1, -2:], getattr(short, t)[1, -2:]) and getattr(long, t)[1, -2:].any()
+        assert not getattr(long, t)[0].any() and not getattr(long, t)[1, :-2].any()
+    del long
+    c = s2.KVCache(1, Hkv, D, 2, P, 1, 2)
+    q = torch.zeros((n, Hq, D), dtype=torch.bfloat16, device="cuda")
+    k = torch.zeros((n, Hkv, D), dtype=torch.bfloat16, device="cuda")
+    q[-tail:].normal_(generator=g)
+    pos_all = torch.zeros(n, dtype=torch.int32, device="cuda")
+    pos_all[-tail:] = pos
+    args = k[-tail:].clone(), k[-tail:].clone(), ints([0]), ints([0, tail]), pos, f
+    want = c.append_rotated(0, q[-tail:].clone(), *args)
+    got = c.append_rotated(0, q, k, k.clone(), ints([0]), ints([0, n]), pos_all, f)
+    assert torch.equal(got[-tail:], want) and not got[:1000].any()
