@@ -551,9 +551,10 @@ s2moe_status s2moe_prompt_attention(const s2moe_attn *attn, int32_t n, int32_t n
 /* h = x + residual, residual <- h, out = h * weight / sqrt(mean(h^2) + eps) of each of
    n rows of `hidden` elements (a multiple of 16, at most 16384).  Sums and the norm
    are fp32, from h before it is rounded to the residual's type; squares are summed as
-   they are, so rows should stay below about 1e17.  residual may be NULL: h = x.  x, residual and weight [hidden] are F32 or BF16,
-   each by itself; out F32, BF16 or E4M3 with `scales` (NULL otherwise), lds >= n.
-   No output may overlap an input or another output.  eps > 0, finite.  n <= 2^22. */
+   they are, so rows should stay below about 1e17.  residual may be NULL: h = x.  x,
+   residual and weight [hidden] are F32 or BF16, each by itself; out F32, BF16 or E4M3 with
+   `scales` (NULL otherwise), lds >= n.  No output may overlap an input or another output.
+   eps > 0, finite.  n <= 2^22. */
 s2moe_status s2moe_add_norm(int32_t n, int32_t hidden, const void *x, int64_t ldx, int32_t x_dtype,
                             void *residual, int64_t ldr, int32_t r_dtype, const void *weight,
                             int32_t w_dtype, float eps, void *out, int64_t ldo, int32_t out_dtype,
@@ -571,8 +572,8 @@ s2moe_status s2moe_quantize_weight(int32_t rows, int32_t cols, const void *w, in
 
 /* out[i][j] = sum_b x_scales[b][i] w_scales[j / 128][b] sum_{k in block b} x[i][k] w[j][k]
    for m rows of x and n rows of w, in fp32, rounded once to out's type (F32 or BF16).
-   x, w: codes; k a multiple of 16, at most 2^18, m, n <= 2^22, m n <= 2^34.  x_scales [ceil(k / 128)]
-   [ldxs], ldxs >= m; w_scales [ceil(n / 128)][ldws], ldws >= ceil(k / 128).  out [m][n],
+   x, w: codes; k a multiple of 16, at most 2^18, m, n <= 2^22, m n <= 2^34.  x_scales
+   [ceil(k / 128)][ldxs], ldxs >= m; w_scales [ceil(n / 128)][ldws], ldws >= ceil(k / 128).  out [m][n],
    16-byte aligned, ldo >= n (any: rows may begin anywhere an element may).  out must
    not overlap an input.  Sums are in a fixed order: equal calls give equal bits.
    F32 results hold fp32 sums of exact products.  BF16 ones come from the 8-bit matrix

@@ -633,6 +633,8 @@ __global__ __launch_bounds__(64 * WN * WM) void tiles_kernel(MatmulArgs a, int t
       }
     }
     third = next;
+    // No product stays behind the barrier: with it would the wait for its operands.
+    __builtin_amdgcn_sched_barrier(0);
     if constexpr (!kTail) {
       wait_loads<0>();
       arrived(fx);
