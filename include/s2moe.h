@@ -449,9 +449,11 @@ typedef struct s2moe_rotation {
    [n_tokens][n_kv_heads][head_dim] as well, whether or not its slot could be
    written (the keys of s2moe_prompt_attention).  q, k, v, q_out and k_out have the
    cache's dtype.  q_out may be q and k_out may be k with the same stride (in place),
-   and otherwise they must not overlap q, k, v or each other.  pos [n_tokens] int32,
+   and otherwise they must overlap no input and not each other.  pos [n_tokens] int32,
    inv_freq [rot_dim / 2] fp32.  Sines, cosines and products are fp32, rounded once.
-   Rows outside the requests are not written. */
+   Rows outside the requests are not written.  A sequence should be named once: the
+   slots of one named twice hold some of either's tokens.  n_tokens (n_kv_heads + 40)
+   <= 2^30. */
 s2moe_status s2moe_kv_append_rotated(const s2moe_kv_cache *cache, int32_t layer,
                                      const s2moe_rotation *rotation, int32_t n, int32_t n_tokens,
                                      const int32_t *seqs, const int32_t *tok_off,

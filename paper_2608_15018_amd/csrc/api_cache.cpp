@@ -272,6 +272,9 @@ s2moe_status s2moe_kv_append_rotated(const s2moe_kv_cache* cache, int32_t layer,
                 r.rot_dim, c.D);
   if (r.neighbours != 0 && r.neighbours != 1)
     return fail(S2MOE_EINVAL, "%s: neighbours = %d must be 0 or 1", fn, r.neighbours);
+  if ((int64_t)n_tokens * (c.Hkv + 40) > (int64_t)1 << 30)  // threads of a launch, below 2^32
+    return fail(S2MOE_EUNSUPPORTED, "%s: n_tokens (n_kv_heads + 40) = %d %d exceeds 2^30", fn,
+                n_tokens, c.Hkv + 40);
   if (n == 0 || n_tokens == 0) return ok();
   S2MOE_REQUIRE_INTS(seqs);
   S2MOE_REQUIRE_INTS(tok_off);
@@ -303,6 +306,15 @@ s2moe_status s2moe_kv_append_rotated(const s2moe_kv_cache* cache, int32_t layer,
                            rows_meet(k_out, lko, wk, v, lv, wk, n_tokens) ||
                            rows_meet(k_out, lko, wk, q_out, lqo, wq, n_tokens)))
     return fail(S2MOE_EINVAL, "%s: k_out overlaps k (other than in place), q, v or q_out", fn);
+  const auto meets_ints = [&](const void* out, int64_t ld, int64_t width) {
+    const int64_t bytes = (n_tokens - 1) * ld + width;
+    return bytes_meet(out, bytes, pos, (int64_t)n_tokens * 4) ||
+           bytes_meet(out, bytes, inv_freq, (int64_t)r.rot_dim * 2) ||
+           bytes_meet(out, bytes, seqs, (int64_t)n * 4) ||
+           bytes_meet(out, bytes, tok_off, ((int64_t)n + 1) * 4);
+  };
+  if (meets_ints(q_out, lqo, wq) || (k_out != nullptr && meets_ints(k_out, lko, wk)))
+    return fail(S2MOE_EINVAL, "%s: q_out or k_out overlaps pos, inv_freq, seqs or tok_off", fn);
   s2moe::RotateArgs a;
   a.layer = layer;
   a.n = n;

@@ -132,7 +132,10 @@ def test_append_rotated(lib):
         # Overlaps: in place with another stride, shifted, over k or v, over each other.
         (dict(qo=Q), INVAL, "q_out overlaps"), (dict(qo=Q + 16, r=rot(ldqo=512)), INVAL, "q_out overlaps"), (dict(qo=K, r=rot(ldqo=512)), INVAL, "q_out overlaps"),
         (dict(ko=K), INVAL, "k_out overlaps"), (dict(ko=V, r=rot(ldko=512)), INVAL, "k_out overlaps"), (dict(ko=Q + 256, r=rot(ldko=512)), INVAL, "k_out overlaps"),
-        (dict(ko=C + 512 * 8), INVAL, "k_out overlaps")])
+        (dict(ko=C + 512 * 8), INVAL, "k_out overlaps"),
+        # Over what both sides read, and more tokens than a launch has threads for.
+        (dict(pos=C + 8 * 512 + 508), INVAL, "overlaps pos"), (dict(f=D), INVAL, "overlaps pos"), (dict(seqs=D + 256), INVAL, "overlaps pos"),
+        (dict(off=C - 8), INVAL, "overlaps pos"), (dict(t=1 << 26), UNSUP, "n_tokens (n_kv_heads + 40)")])
     assert call(n=0) == _lib.OK and call(t=0) == _lib.OK
 
 
