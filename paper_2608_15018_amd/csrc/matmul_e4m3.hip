@@ -361,6 +361,10 @@ __global__ __launch_bounds__(512) void few_tokens_kernel(MatmulArgs a, int tiles
 // Tiles between: what a step costs beside its products is what takes time.  kStages blocks
 // of k are in LDS or on their way there; while the matrix cores have one block's operands,
 // the waves read the next one's.  Scales of tokens come the same way, 64 words a wave.
+// How far ahead loads have to be, and how many workgroups a compute unit holds, decides: of
+// 64 x 64 tiles one a unit takes 12.6 us at 128 x 5120 x 2880 with four blocks, 13.7 with
+// three, two a unit 18.8 and 18.2 at 384; 64 x 96 tiles, three blocks, keep 251 tokens to
+// one a unit: 14.8 us, 18.2 with 64 x 64.
 template <int WN, int WM, int TN, int TM, int kStages, bool kF32Out, bool kOnce>
 __global__ __launch_bounds__(64 * WN * WM) void small_tiles_kernel(MatmulArgs a, int tiles_n, int tiles_m) {
   constexpr int kN = 16 * TN * WN, kM = 16 * TM * WM, kWaves = WN * WM;
@@ -384,7 +388,7 @@ __global__ __launch_bounds__(64 * WN * WM) void small_tiles_kernel(MatmulArgs a,
 #pragma unroll
   for (int i = 0; i < kLoadsX; ++i)
     xoff[i] = (uint32_t)min((wave * kLoadsX + i) * 8 + (lane >> 3), a.m - 1 - m0) * (uint32_t)a.ldx + piece * 16;
-  const uint32_t mine = 4u * min(my_m + (lane & (16 * TM - 1)), a.m - 1);
+  const uint32_t mine = 4u * min(my_m + min(lane, 16 * TM - 1), a.m - 1);
   const float* const ws = a.ws + min(my_n / kBlock, (a.n - 1) / kBlock) * a.ldws;
   float wscale = ws[min(lane, steps - 1)];
   arrived(wscale);
@@ -701,37 +705,41 @@ hipError_t launch_stream(const MatmulArgs& a, hipStream_t s) {
 // shared, a step, with load the tiles of the busiest compute unit, and not less than 3 +
 // its weights and results at `rate` MB/us.  Fitted to 336 sizes for each type of result (1
 // to 4096 tokens, 512 to 32000 weight rows, k from 512 to 6144), foremost to which form is
-// fastest.  The one chosen takes 0.2 % more than the best on average there, 15 % at most
-// (sizes left out of the fit: 0.4 and 27 %); without any one form the average rises by
-// 0.3 to 7.6 points.  fp32 results have no 256 x 256, whose operands in fp16 would not fit
-// beside the sums, and no second 128 x 128, which nothing is faster by.
+// fastest.  The one chosen takes 0.3 % more than the best on average there, 14 % at most
+// (sizes left out of the fit: 0.5 and 26 %); without any one form the average rises by
+// 0.2 to 6.7 points.  fp32 results have no 256 x 256, whose operands in fp16 would not fit
+// beside the sums, no second 128 x 128 and no 64 x 128, which nothing is faster by.
 struct Form {
   int n, m;  // of a tile
   float base, wave, alone, shared, rate;
 };
-constexpr int kForms = 10;
+constexpr int kForms = 12;
 constexpr Form kBf16Forms[kForms] = {
-    {256, 256, 1.f, 5.87f, 0.135f, 1.33f, 3.95f},
-    {128, 128, 4.71f, 0.739f, 0.744f, 0.503f, 3.9f},
-    {128, 128, 2.7f, 3.09f, 0.562f, 0.585f, 4.76f},
-    {64, 64, 2.78f, 0.642f, 0.392f, 0.241f, 5.23f},
-    {32, 32, 2.42f, 0.92f, 0.212f, 0.149f, 4.68f},
-    {64, 16, 3.36f, 0.0518f, 0.135f, 0.275f, 5.95f},
-    {64, 32, 1.12f, 4.58f, 0.0499f, 0.161f, 5.84f},
-    {32, 32, 1.15f, 3.35f, 0.106f, 0.111f, 5.35f},
-    {32, 16, 2.39f, 0.991f, 0.0588f, 0.113f, 6.4f},
-    {16, 16, 2.65f, 1.55f, 0.0423f, 0.0424f, 4.84f}};
+    {256, 256, 1.f, 5.37f, 0.23f, 1.36f, 4.05f},
+    {128, 128, 3.96f, 0.611f, 0.79f, 0.515f, 4.21f},
+    {128, 128, 2.76f, 2.78f, 0.617f, 0.585f, 5.28f},
+    {64, 64, 2.9f, 0.687f, 0.356f, 0.259f, 5.17f},
+    {32, 32, 2.61f, 0.866f, 0.204f, 0.137f, 4.42f},
+    {64, 16, 3.47f, 0.0954f, 0.2f, 0.277f, 6.04f},
+    {64, 32, 1.f, 4.62f, 0.0493f, 0.165f, 5.7f},
+    {32, 32, 1.24f, 3.56f, 0.0887f, 0.0828f, 4.f},
+    {32, 16, 2.55f, 1.16f, 0.0418f, 0.0818f, 6.4f},
+    {16, 16, 2.26f, 1.23f, 0.0145f, 0.0583f, 4.8f},
+    {64, 96, 2.6f, 1.09f, 0.458f, 0.281f, 3.62f},
+    {64, 128, 2.23f, 2.15f, 0.118f, 0.41f, 3.34f}};
 constexpr Form kF32Forms[kForms] = {
     {256, 256, 1e30f, 0.f, 0.f, 0.f, 1.f},
-    {128, 128, 4.09f, 1.26f, 1.08f, 0.845f, 5.83f},
+    {128, 128, 3.23f, 1.64f, 1.04f, 0.76f, 4.43f},
     {128, 128, 1e30f, 0.f, 0.f, 0.f, 1.f},
-    {64, 64, 3.77f, 0.333f, 0.564f, 0.328f, 4.67f},
-    {32, 32, 2.64f, 0.743f, 0.304f, 0.212f, 4.3f},
-    {64, 16, 3.53f, 0.36f, 0.0738f, 0.267f, 5.79f},
-    {64, 32, 1.16f, 3.9f, 0.162f, 0.197f, 5.58f},
-    {32, 32, 1.14f, 3.12f, 0.141f, 0.15f, 5.59f},
-    {32, 16, 2.55f, 1.26f, 0.0999f, 0.0851f, 6.4f},
-    {16, 16, 2.42f, 1.12f, 0.0731f, 0.061f, 4.82f}};
+    {64, 64, 3.44f, 0.532f, 0.546f, 0.372f, 4.9f},
+    {32, 32, 2.65f, 0.832f, 0.301f, 0.201f, 4.41f},
+    {64, 16, 3.52f, 0.448f, 0.236f, 0.259f, 5.87f},
+    {64, 32, 1.07f, 3.85f, 0.0584f, 0.211f, 5.59f},
+    {32, 32, 1.12f, 3.23f, 0.129f, 0.148f, 5.52f},
+    {32, 16, 2.61f, 1.19f, 0.106f, 0.0889f, 6.4f},
+    {16, 16, 2.65f, 1.32f, 0.0501f, 0.0506f, 4.84f},
+    {64, 96, 3.74f, 0.528f, 0.651f, 0.453f, 4.26f},
+    {64, 128, 1e30f, 0.f, 0.f, 0.f, 1.f}};
 
 int choose(const MatmulArgs& a, int m, float* us) {
   const Form* const forms = a.f32 ? kF32Forms : kBf16Forms;
@@ -762,13 +770,17 @@ hipError_t launch_form(int form, const MatmulArgs& a, hipStream_t s) {
     case 2:
       if constexpr (!kF32Out) return launch_small_tiles<2, 4, 4, 2, 3, kF32Out>(a, s);
       [[fallthrough]];
+    case 11:
+      if constexpr (!kF32Out) return launch_small_tiles<2, 4, 2, 2, 4, kF32Out>(a, s);
+      [[fallthrough]];
     case 1: return launch_tiles<2, 2, 4, 4, kF32Out>(a, s);
-    case 3: return launch_small_tiles<2, 2, 2, 2, 3, kF32Out>(a, s);
+    case 3: return launch_small_tiles<2, 2, 2, 2, 4, kF32Out>(a, s);
     case 4: return launch_small_tiles<2, 2, 1, 1, 6, kF32Out>(a, s);
     case 5: return launch_few<4, kF32Out>(a, s);
     case 6: return launch_stream<4, 2, 2, 4, kF32Out>(a, s);
     case 7: return launch_stream<2, 2, 4, 4, kF32Out>(a, s);
     case 8: return launch_stream<2, 1, 2, 4, kF32Out>(a, s);
+    case 10: return launch_small_tiles<2, 2, 2, 3, 3, kF32Out>(a, s);
     default: return launch_stream<1, 1, 2, 8, kF32Out>(a, s);
   }
 }
