@@ -703,42 +703,42 @@ hipError_t launch_stream(const MatmulArgs& a, hipStream_t s) {
 
 // What a form takes, in us: base + load * wave + a step's greater of alone and load *
 // shared, a step, with load the tiles of the busiest compute unit, and not less than 3 +
-// its weights and results at `rate` MB/us.  Fitted to 336 sizes for each type of result (1
-// to 4096 tokens, 512 to 32000 weight rows, k from 512 to 6144), foremost to which form is
-// fastest.  The one chosen takes 0.3 % more than the best on average there, 14 % at most
-// (sizes left out of the fit: 0.5 and 26 %); without any one form the average rises by
-// 0.2 to 6.7 points.  fp32 results have no 256 x 256, whose operands in fp16 would not fit
-// beside the sums, no second 128 x 128 and no 64 x 128, which nothing is faster by.
+// its weights and results at `rate` MB/us.  Fitted to 326 sizes for each type of result (1
+// to 4096 tokens, 512 to 32000 weight rows, k from 512 to 6144; weights from memory, as a
+// model's layers find them), foremost to which form is fastest.  The one chosen takes 0.3 %
+// more than the best on average there, 16 % at most (sizes left out of the fit: 0.5 and
+// 19 %).  fp32 results have no 256 x 256, whose operands in fp16 would not fit beside the
+// sums, no second 128 x 128 and no 64 x 128, which nothing is faster by.
 struct Form {
   int n, m;  // of a tile
   float base, wave, alone, shared, rate;
 };
 constexpr int kForms = 12;
 constexpr Form kBf16Forms[kForms] = {
-    {256, 256, 1.f, 5.37f, 0.23f, 1.36f, 4.05f},
-    {128, 128, 3.96f, 0.611f, 0.79f, 0.515f, 4.21f},
-    {128, 128, 2.76f, 2.78f, 0.617f, 0.585f, 5.28f},
-    {64, 64, 2.9f, 0.687f, 0.356f, 0.259f, 5.17f},
-    {32, 32, 2.61f, 0.866f, 0.204f, 0.137f, 4.42f},
-    {64, 16, 3.47f, 0.0954f, 0.2f, 0.277f, 6.04f},
-    {64, 32, 1.f, 4.62f, 0.0493f, 0.165f, 5.7f},
-    {32, 32, 1.24f, 3.56f, 0.0887f, 0.0828f, 4.f},
-    {32, 16, 2.55f, 1.16f, 0.0418f, 0.0818f, 6.4f},
-    {16, 16, 2.26f, 1.23f, 0.0145f, 0.0583f, 4.8f},
-    {64, 96, 2.6f, 1.09f, 0.458f, 0.281f, 3.62f},
-    {64, 128, 2.23f, 2.15f, 0.118f, 0.41f, 3.34f}};
+    {256, 256, 1.09f, 5.28f, 0.229f, 1.4f, 3.91f},
+    {128, 128, 1.79f, 1.71f, 1.06f, 0.532f, 3.73f},
+    {128, 128, 1.24f, 3.73f, 0.23f, 0.642f, 6.01f},
+    {64, 64, 1.51f, 1.22f, 0.353f, 0.278f, 5.76f},
+    {32, 32, 1.57f, 1.21f, 0.203f, 0.128f, 4.77f},
+    {64, 16, 3.04f, 0.0837f, 0.192f, 0.321f, 4.86f},
+    {64, 32, 1.17f, 3.15f, 0.137f, 0.197f, 4.36f},
+    {32, 32, 1.22f, 2.68f, 0.0804f, 0.126f, 4.99f},
+    {32, 16, 1.46f, 1.35f, 0.117f, 0.13f, 6.4f},
+    {16, 16, 2.14f, 1.48f, 0.0638f, 0.0543f, 4.93f},
+    {64, 96, 1.29f, 1.31f, 0.529f, 0.388f, 4.99f},
+    {64, 128, 1.08f, 2.8f, 0.0914f, 0.416f, 4.51f}};
 constexpr Form kF32Forms[kForms] = {
     {256, 256, 1e30f, 0.f, 0.f, 0.f, 1.f},
-    {128, 128, 3.23f, 1.64f, 1.04f, 0.76f, 4.43f},
+    {128, 128, 5.02f, 0.973f, 0.332f, 0.831f, 3.64f},
     {128, 128, 1e30f, 0.f, 0.f, 0.f, 1.f},
-    {64, 64, 3.44f, 0.532f, 0.546f, 0.372f, 4.9f},
-    {32, 32, 2.65f, 0.832f, 0.301f, 0.201f, 4.41f},
-    {64, 16, 3.52f, 0.448f, 0.236f, 0.259f, 5.87f},
-    {64, 32, 1.07f, 3.85f, 0.0584f, 0.211f, 5.59f},
-    {32, 32, 1.12f, 3.23f, 0.129f, 0.148f, 5.52f},
-    {32, 16, 2.61f, 1.19f, 0.106f, 0.0889f, 6.4f},
-    {16, 16, 2.65f, 1.32f, 0.0501f, 0.0506f, 4.84f},
-    {64, 96, 3.74f, 0.528f, 0.651f, 0.453f, 4.26f},
+    {64, 64, 1.92f, 1.14f, 0.576f, 0.374f, 4.74f},
+    {32, 32, 1.29f, 1.03f, 0.35f, 0.212f, 5.04f},
+    {64, 16, 2.57f, 0.563f, 0.31f, 0.294f, 5.83f},
+    {64, 32, 1.4f, 4.04f, 0.176f, 0.212f, 5.63f},
+    {32, 32, 1.f, 2.53f, 0.0637f, 0.165f, 4.77f},
+    {32, 16, 1.41f, 1.46f, 0.0977f, 0.116f, 6.4f},
+    {16, 16, 1.99f, 1.64f, 0.0528f, 0.0499f, 4.84f},
+    {64, 96, 1.42f, 1.68f, 0.69f, 0.433f, 3.98f},
     {64, 128, 1e30f, 0.f, 0.f, 0.f, 1.f}};
 
 int choose(const MatmulArgs& a, int m, float* us) {

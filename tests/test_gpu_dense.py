@@ -211,7 +211,8 @@ LARGE = [(257, 512, 400), (384, 2048, 1040), (700, 2050, 1024), (768, 5120, 1040
          (257, 16400, 1024), (1025, 16384, 1040), (384, 32000, 1024), (2052, 6144, 2880), (90, 32000, 272), (33, 20000, 144), (16, 30001, 1168),
          (1, 9001, 1040), (20, 9000, 272), (27, 5001, 1040), (1, 9000, 272), (17, 9000, 528), (30, 12001, 1168),
          (33, 5001, 272), (50, 5001, 2064), (50, 5001, 528), (1, 9000, 4112), (33, 3000, 2064), (33, 3000, 1040), (17, 5001, 2064),
-         (17, 2050, 272), (70, 30001, 1040), (17, 9000, 2064), (200, 5001, 272), (70, 9000, 272), (128, 9000, 272), (128, 20000, 272)]
+         (17, 2050, 272), (70, 30001, 1040), (17, 9000, 2064), (200, 5001, 272), (70, 9000, 272), (128, 9000, 272), (128, 20000, 272),
+         (1, 20000, 272)]
 # A wave's weight scales are 64 blocks at a time: rows of more than that, for each form.
 LONG = [(1, 48, 70016), (17, 48, 70016), (1, 5001, 33040), (17, 5001, 33040), (17, 2050, 33040), (33, 3000, 33040), (33, 5001, 33040),
         (33, 9000, 8720), (200, 9000, 8720), (256, 2050, 8720), (600, 5001, 8720), (900, 9000, 8720), (2052, 2050, 8720),
