@@ -497,7 +497,7 @@ __global__ __launch_bounds__(64 * WN * WM) void small_tiles_kernel(MatmulArgs a,
 // while it makes this one's last products, and only two reads stand between a barrier and
 // the first product after it.  All loads of a step have to be there at its end.  Loads of
 // weights two rows of products after those of tokens, not with them: 170 us instead of 179
-// at 8192 x 6144 x 4096 (of a wave's four rows both at the start).
+// at 8192 x 6144 x 4096; a wave that has only four rows loads both at the start (352 and 357).
 template <int WN, int WM, int TN, int TM, bool kF32Out>
 __global__ __launch_bounds__(64 * WN * WM) void tiles_kernel(MatmulArgs a, int tiles_n, int tiles_m) {
   constexpr int kN = 16 * TN * WN, kM = 16 * TM * WM, kWaves = WN * WM;
