@@ -97,7 +97,7 @@ def _rows_out(out, like, n, cols, gpu, stream):
     sp, lds, _, _ = _matrix(scales, "scales", kb, n)
     if not gpu == codes.get_device() == scales.get_device():
         _refuse(gpu, codes=codes, scales=scales)
-    return out, cp, ldc, sp, lds if lds > n else n
+    return out, cp, ldc, sp, lds
 
 
 def add_norm(x, weight, residual=None, eps: float = 1e-6, out=None, out_dtype=None, stream=None):
@@ -201,7 +201,6 @@ def fp8_matmul(x: Fp8Rows, w: Fp8Weight, out=None, out_dtype=None, stream=None):
         op, ldo, _, _ = _matrix(out, "out", m, n)
         if out.get_device() != gpu:
             _refuse(gpu, out=out)
-    _lib._check(_lib.load().s2moe_scaled_matmul(m, n, K, xp, ldx, xsp, ldxs if ldxs > m else m, wp,
-                                                ldw, wsp, ldws if ldws > kb else kb, op, ldo, oc,
-                                                handle))
+    _lib._check(_lib.load().s2moe_scaled_matmul(m, n, K, xp, ldx, xsp, ldxs, wp, ldw, wsp, ldws, op, ldo,
+                                                oc, handle))
     return out
