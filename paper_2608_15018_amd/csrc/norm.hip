@@ -164,6 +164,8 @@ __global__ __launch_bounds__(256) void add_norm_kernel(NormArgs a) {
   }
   const float norm = 1.f / sqrtf(sum / (float)a.H + a.eps);
   if (!mine) return;
+  // The norm's power of two and what is left of it, between 1 and 2.
+  const float power = __uint_as_float(__float_as_uint(norm) & 0x7F800000u), left = norm / power;
   char* out = a.out + row * a.ldo * (O == kF32 ? 4 : O == kBf16 ? 2 : 1);
 #pragma unroll
   for (int c = 0; c < kChunks; ++c) {
@@ -177,15 +179,15 @@ __global__ __launch_bounds__(256) void add_norm_kernel(NormArgs a) {
       else
         floats<kBf16>(Raw<kBf16>{{ws[c][0]}}, w);
 #pragma unroll
-      for (int i = 0; i < 8; ++i) y[i] = O == kE4m3 ? h[c][i] * w[i] : h[c][i] * norm * w[i];
+      for (int i = 0; i < 8; ++i) y[i] = h[c][i] * (O == kE4m3 ? power : norm) * w[i];
     }
     if constexpr (O == kE4m3) {
-      // The norm divides a block's elements and its maximum alike: the codes are 448 h w over
-      // the largest |h w|, and the norm's own rounding does not reach them.
-      const float top = max16(most8(y)), most = fmaxf(top * norm, kLeast);
-      const float times = most > kLeast ? kLargest / top : fminf(norm * (kLargest / kLeast), 1e38f);
-#pragma unroll
-      for (int i = 0; i < 8; ++i) y[i] *= times;
+      // The norm divides a block's elements and its largest alike: the codes are 448 h w over
+      // the largest |h w|, and the norm's own rounding does not reach them.  Its power of two
+      // does, exactly, so that h w is as far from the ends of fp32 as y is.  Of blocks below
+      // the least magnitude it is 448 y over that.
+      const float top = max16(most8(y)), most = fmaxf(top * left, kLeast);
+      divide8(y, most > kLeast ? top : fminf(kLeast / left, 3e38f));
       store_block(out, a.scales, a.lds, row, col, live, y, most);
     } else {
       if (live) store8<O>(out, col, y);
