@@ -3,8 +3,9 @@
 //
 // A token of position p has, of each head, pairs of coordinates (a, b), and pair j turns
 // by p f_j:  a' = a cos - b sin, b' = b cos + a sin.  The turn is p f_j / 2 pi in 64 bits,
-// whose whole part is dropped before it is rounded to 32, so that far positions keep
-// their angle; sine, cosine and the products are fp32, and each element is rounded once.
+// of which the nearest whole number is taken off before it is rounded to 32, so that far
+// positions keep their angle, and angles next to a whole turn their small sine; sine, cosine
+// and the products are fp32, and each element is rounded once.
 //
 // Bound: memory for prompts (17000 tokens, 32 query heads, 4 of keys and values, 128
 // wide: 61 us, 5.5 TB/s, a large copy 5.2; 67 with queries through the caches, 65 and 71
@@ -132,7 +133,7 @@ __device__ __forceinline__ void turn(u32x4& x, u32x4& y, const float2* cs, bool 
 __device__ __forceinline__ float2 cos_sin(int pos, float freq) {
   const double turns = (double)pos * (double)freq * 0.15915494309189535;  // 1 / 2 pi
   float s, c;
-  sincospif(2.f * (float)(turns - floor(turns)), &s, &c);
+  sincospif(2.f * (float)(turns - rint(turns)), &s, &c);
   return float2{c, s};
 }
 
