@@ -423,8 +423,8 @@ s2moe_status s2moe_kv_append(const s2moe_kv_cache *cache, int32_t layer, int32_t
    node j's ancestors within the tree.  Trees may have any number of nodes; a node
    whose parent is neither -1 nor an earlier node counts as one below the last kept
    token.  One call serves all layers of a step.  pos, parent: [n_tokens] int32,
-   parent may be NULL; pos must overlap no input.  Rows of pos outside the requests
-   are not written.  n_tokens <= 2^28. */
+   parent may be NULL; pos must overlap no input and no array of the cache.  Rows of
+   pos outside the requests are not written.  n_tokens <= 2^28. */
 s2moe_status s2moe_kv_positions(const s2moe_kv_cache *cache, int32_t n, int32_t n_tokens,
                                 const int32_t *seqs, const int32_t *tok_off,
                                 const int32_t *parent, int32_t *pos, void *stream);
@@ -449,11 +449,11 @@ typedef struct s2moe_rotation {
    [n_tokens][n_kv_heads][head_dim] as well, whether or not its slot could be
    written (the keys of s2moe_prompt_attention).  q, k, v, q_out and k_out have the
    cache's dtype.  q_out may be q and k_out may be k with the same stride (in place),
-   and otherwise they must overlap no input and not each other.  pos [n_tokens] int32,
-   inv_freq [rot_dim / 2] fp32.  Sines, cosines and products are fp32, rounded once.
-   Rows outside the requests are not written.  A sequence should be named once: the
-   slots of one named twice hold some of either's tokens.  n_tokens (n_kv_heads + 40)
-   <= 2^30. */
+   and otherwise they must overlap no input, no array of the cache and not each other.
+   pos [n_tokens] int32, inv_freq [rot_dim / 2] fp32.  Sines, cosines and products are
+   fp32, rounded once.  Rows outside the requests are not written.  A sequence should be
+   named once: the slots of one named twice hold some of either's tokens.
+   n_tokens (n_kv_heads + 40) <= 2^30. */
 s2moe_status s2moe_kv_append_rotated(const s2moe_kv_cache *cache, int32_t layer,
                                      const s2moe_rotation *rotation, int32_t n, int32_t n_tokens,
                                      const int32_t *seqs, const int32_t *tok_off,

@@ -98,6 +98,15 @@ s2moe_status check_tokens(const char* fn, int32_t n_tokens) {
   return S2MOE_OK;
 }
 
+// Whether `n` bytes at `p` meet one of the cache's arrays.
+bool meets_cache(const s2moe::KvCache& c, const void* p, int64_t n) {
+  const int64_t pool = c.L * c.layer_bytes();
+  return bytes_meet(p, n, c.k, pool) || bytes_meet(p, n, c.v, pool) ||
+         bytes_meet(p, n, c.table, (int64_t)c.max_seqs * c.max_pages * 4) ||
+         bytes_meet(p, n, c.length, (int64_t)c.max_seqs * 4) ||
+         bytes_meet(p, n, c.refs, (int64_t)c.n_pages * 4);
+}
+
 s2moe_status check_attn(const char* fn, const s2moe_attn* attn) {
   if (attn == nullptr) return fail(S2MOE_EINVAL, "%s: attn is NULL", fn);
   const s2moe_attn& t = *attn;
@@ -245,6 +254,8 @@ s2moe_status s2moe_kv_positions(const s2moe_kv_cache* cache, int32_t n, int32_t 
       bytes_meet(pos, bytes, tok_off, ((int64_t)n + 1) * 4) ||
       (parent != nullptr && bytes_meet(pos, bytes, parent, bytes)))
     return fail(S2MOE_EINVAL, "%s: pos overlaps seqs, tok_off or parent", fn);
+  if (meets_cache(c, pos, bytes))
+    return fail(S2MOE_EINVAL, "%s: pos overlaps an array of the cache", fn);
   return hip_status(fn, s2moe::launch_positions(c, n, n_tokens, seqs, tok_off, parent, pos,
                                                 static_cast<hipStream_t>(stream)));
 }
@@ -315,6 +326,9 @@ s2moe_status s2moe_kv_append_rotated(const s2moe_kv_cache* cache, int32_t layer,
   };
   if (meets_ints(q_out, lqo, wq) || (k_out != nullptr && meets_ints(k_out, lko, wk)))
     return fail(S2MOE_EINVAL, "%s: q_out or k_out overlaps pos, inv_freq, seqs or tok_off", fn);
+  if (meets_cache(c, q_out, (n_tokens - 1) * lqo + wq) ||
+      (k_out != nullptr && meets_cache(c, k_out, (n_tokens - 1) * lko + wk)))
+    return fail(S2MOE_EINVAL, "%s: q_out or k_out overlaps an array of the cache", fn);
   s2moe::RotateArgs a;
   a.layer = layer;
   a.n = n;
