@@ -542,8 +542,10 @@ s2moe_status s2moe_prompt_attention(const s2moe_attn *attn, int32_t n, int32_t n
    block is its largest magnitude / 448 (2^-100 / 448 where it is less than 2^-100),
    so that the largest code is 448 exactly.  The scales of one block of all rows lie
    together, which is how a product reads them.  Weights are codes [n][k] and
-   scales [ceil(n / 128)][ceil(k / 128)], one for 128 x 128 elements.  A row with an
-   infinity or NaN has unspecified values, and no other row is touched by it.
+   scales [ceil(n / 128)][ceil(k / 128)], one for 128 x 128 elements.  Codes are rounded
+   to the nearest from fp32, half way ones to the even one.  A row with an infinity or NaN
+   has unspecified values, and no other row is touched by it; of weights, no row but those
+   of its 128 x 128 block.
 
    Strides ld* are in elements from one row to the next, at most 2^22; rows of
    inputs and of codes begin at multiples of 16 bytes.  Scales need 4-byte alignment
@@ -581,7 +583,11 @@ s2moe_status s2moe_quantize_weight(int32_t rows, int32_t cols, const void *w, in
    F32 results hold fp32 sums of exact products.  BF16 ones come from the 8-bit matrix
    instructions, twice as fast where the matrix cores are the bound, which cut each
    product off 13 bits below the largest exponent among its eight neighbours: about
-   1.4e-5 of the result on normal data, where bf16's own rounding is 1.7e-3. */
+   1.4e-5 of the result on normal data, where bf16's own rounding is 1.7e-3, and at most
+   2^-10 of the sum of the products' magnitudes (2^-7 where a code below 2^-6 makes the
+   largest of eight neighbours), which is more than a rounding where a sum cancels: then
+   take F32.  A block's two scales are multiplied in fp32 first; their product should lie
+   within its normal range. */
 s2moe_status s2moe_scaled_matmul(int32_t m, int32_t n, int32_t k, const void *x, int64_t ldx,
                                  const float *x_scales, int64_t ldxs, const void *w, int64_t ldw,
                                  const float *w_scales, int64_t ldws, void *out, int64_t ldo,

@@ -276,12 +276,16 @@ template <typename E, int D>
 void launch_rotated(const KvCache& c, const RotateArgs& a, hipStream_t s) {
   constexpr int kHeads = 64 / (D / kPer<E> / 2);  // of a query load
   // Few tokens go alone, a wave each and kv head; groups of eight share angles and write
-  // their values whole.  us alone / in groups, 32 heads over 8 of 128: 8 requests of 8 4.4 / 9.1,
-  // 32 of 16 7.0 / 9.9, 300 of 4 15.8 / 15.6, 64 of 16 12.4 / 11.6, 8 of 512 34 / 23.
+  // their values whole.  us alone / in groups, 32 heads over 8 of 128: 8 requests of 8 4.4 / 6.5,
+  // 32 of 16 6.9 / 7.3, 300 of 4 16.0 / 16.5, 1024 of 1 18.8 / 24.2, 1 of 1300 15.6 / 10.3, 8 of
+  // 512 35 / 20.  Requests of eight and more cross over at 600 tokens already (64 of 16: 12.2 /
+  // 8.7), single tokens never do.
   const bool few = a.n_tokens < 1200;
   const int most = (a.Hq + kHeads - 1) / kHeads;
-  // With waves enough, two kv heads a wave and half of the query heads: 17000 tokens take
-  // 85 us so, 93 with a kv head each, 101 with all in one, 98 with a quarter of the queries.
+  // With waves enough, two kv heads a wave and half of the query heads: 17000 tokens, 32 heads
+  // over 4 of 128, take 63.4 us so, 67.0 with a kv head each, 63.9 with all four in one, 61.7
+  // with all of the queries and 72.4 with a quarter; 8000, 64 heads over 8 of 64, 36.7, 40.1
+  // with a kv head each and 36.7 with all of the queries; 3500, 32 over 4, 17.9 and 16.9.
   const int kv_parts = a.n_tokens < 4096 ? c.Hkv : (c.Hkv + 1) / 2, q_parts = few ? most : most < 2 ? most : 2;
   const int per = few ? 4 : 32, kv_blocks = (a.n_tokens + per - 1) / per * kv_parts;
   const int grid = kv_blocks + (a.n_tokens + 3) / 4 * q_parts;

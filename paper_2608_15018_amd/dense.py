@@ -171,7 +171,8 @@ def quantize_weight(w, stream=None) -> Fp8Weight:
 
 def fp8_matmul(x: Fp8Rows, w: Fp8Weight, out=None, out_dtype=None, stream=None):
     """x [m, k] times the transpose of w [n, k]: [m, n] in out_dtype (torch.bfloat16 by
-    default, or torch.float32)."""
+    default, or torch.float32).  Sums that cancel keep their precision in float32 only: for
+    bfloat16 results products are cut off 13 bits below the largest of eight neighbours."""
     xc, xs = x
     wc, ws = w
     _of(xc, "x.codes", E4M3)
