@@ -47,3 +47,31 @@ def test_blocks_of_every_size(dtype):
     rows = s2.quantize(x)
     assert torch.equal(torch.cat([t.codes.view(torch.uint8) for t in got]), rows.codes.view(torch.uint8))
     assert torch.equal(torch.cat([t.scales for t in got]), rows.scales.t())
+
+
+@pytest.mark.parametrize("bad", [float("nan"), float("inf"), -float("inf")])
+def test_weights_that_are_not_finite_stay_in_their_block(bad):
+    w, x = randn((300, 400), "f32", gen(24)), s2.quantize(randn((20, 400), "f32", gen(25)))
+    clean = s2.quantize_weight(w)
+    w[130, 270] = bad
+    dirty = s2.quantize_weight(w)
+    a, b = (t.codes.view(torch.uint8).clone() for t in (clean, dirty))
+    a[128:256, 256:384] = b[128:256, 256:384] = 0
+    assert torch.equal(a, b)
+    s, t = clean.scales.clone(), dirty.scales.clone()
+    s[1, 2] = t[1, 2] = 0
+    assert torch.equal(s, t)
+    y, z = (s2.fp8_matmul(x, t, out_dtype=torch.float32) for t in (clean, dirty))
+    assert torch.equal(y[:, :128], z[:, :128]) and torch.equal(y[:, 256:], z[:, 256:]) and torch.isnan(z[:, 130]).all()
+
+
+@pytest.mark.parametrize("bad", [float("nan"), float("inf")])
+def test_rows_that_are_not_finite_touch_no_other(bad):
+    x = randn((6, 400), "bf16", gen(26))
+    clean = s2.quantize(x)
+    x[3, 200] = bad
+    dirty = s2.quantize(x)
+    rest = [0, 1, 2, 4, 5]
+    assert torch.equal(clean.codes.view(torch.uint8)[rest], dirty.codes.view(torch.uint8)[rest])
+    assert torch.equal(clean.scales[:, rest], dirty.scales[:, rest])
+    assert torch.isnan(dirty.codes.float()[3, 200])
